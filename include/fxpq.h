@@ -57,8 +57,10 @@ typedef enum {
   FXPQ_F32 = 5,
   FXPQ_C8 = 6,    /* 8-bit code whose storage follows the device format: I8 when
                      the format is signed, U8OFF when it is unsigned */
-  FXPQ_U32 = 7    /* unsigned codes of up to 32 bits stored as uint32 (the only
+  FXPQ_U32 = 7,   /* unsigned codes of up to 32 bits stored as uint32 (the only
                      storage an unsigned 32-bit format's codes fit) */
+  FXPQ_F16 = 8,   /* F16 / BF16: real values of the 8-bit serving operators only */
+  FXPQ_BF16 = 9
 } fxpq_dtype;
 
 #define FXPQ_SIGN_AUTO (-1) /* Eq. 6: signed iff the smallest value is negative */
@@ -567,6 +569,161 @@ fxpq_status fxpq_teacher_maxpool(fxpq_handle h, const float* x, int32_t n, int32
 /* Global average of x[n][hw][c]: y[n][c] = (float)(fp64 sum in pixel order / hw). */
 fxpq_status fxpq_teacher_avgpool(fxpq_handle h, const float* x, int32_t n, int32_t hw, int32_t c,
                                  float* y);
+
+/* ---- 8-bit serving operators ------------------------------------------------
+ * What a language model's layers need beside the calls above: products whose
+ * scales belong to tokens and output channels, the same grouped by expert, and
+ * a key / value cache held in 8-bit DFX codes with the attention that reads it.
+ * "Real" values are FXPQ_F32, FXPQ_F16 or FXPQ_BF16; one call's real tensors
+ * share one type.  Row strides (ld*) count elements.  All arithmetic on reals
+ * is fp32.  Integer codes have no gradient: these calls serve, they do not train.
+ */
+
+/* How a scale follows from a largest magnitude a (a below 2^-100 counts as
+ * 2^-100): FXPQ_SCALE_MAX: a / 127; FXPQ_SCALE_DFX: 2^-fl with the largest fl
+ * for which a quantizes to at most 127 (Eq. 10: nothing saturates). */
+typedef enum { FXPQ_SCALE_MAX = 0, FXPQ_SCALE_DFX = 1 } fxpq_scale_rule;
+
+/*
+ * Codes and scale of each row of x (rows x cols reals, row stride ldx >= cols):
+ *     a = max |x[r][.]|, scale[r] by the rule,
+ *     codes[r][c] = rne(x[r][c] * (127 / a))  or  rne(x[r][c] * 2^fl).
+ * codes: int8, row stride ldc >= cols rounded up to 16; the codes between cols
+ * and that multiple of 16 are written as 0, so a contraction may run over it.
+ * A row that holds a NaN or an infinity gets codes 0 and a NaN scale, and
+ * raises FXPQ_FLAG_NONFINITE.  ldc % 16 == 0, codes 16-byte aligned; x needs
+ * the alignment of its type only.  0 <= rows < 2^24, cols >= 1.
+ */
+fxpq_status fxpq_token_quantize(fxpq_handle h, const void* x, fxpq_dtype x_type, int64_t rows,
+                                int64_t cols, int64_t ldx, int32_t rule, int8_t* codes,
+                                int64_t ldc, float* scale);
+
+/*
+ * 8-bit product with a scale for each token and each output channel:
+ *     y[m][n] = (float(sum_k a[m][k] * b[n][k]) * a_scale[m]) * b_scale[n] + bias[n]
+ * a: int8 codes [M][K], row stride lda; b: int8 codes [N][K] (weights as they
+ * are stored, one row per output channel); a_scale[M], b_scale[N], bias[N]
+ * (nullable) floats; y: M x N reals, row stride ldy >= N.  The sum is exact
+ * (int32, K <= 131071, else FXPQ_ERR_OVERFLOW).  K % 16 == 0, lda % 16 == 0,
+ * a and b 16-byte aligned; M and N are free.  workspace (device, 256-byte
+ * aligned) holds at least fxpq_token_gemm_workspace() bytes, which may be 0
+ * (then NULL is fine); its contents are unspecified afterwards and need no
+ * initialization.
+ */
+fxpq_status fxpq_token_gemm_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes);
+fxpq_status fxpq_token_gemm(fxpq_handle h, int64_t M, int64_t N, int64_t K, const int8_t* a,
+                            int64_t lda, const float* a_scale, const int8_t* b,
+                            const float* b_scale, const float* bias, void* y, fxpq_dtype y_type,
+                            int64_t ldy, void* workspace, int64_t workspace_bytes);
+
+/*
+ * The same product grouped by expert.  Rows offsets[e] .. offsets[e + 1] - 1 of
+ * y (offsets: device int32[experts + 1], ascending from 0 to at most `rows`)
+ * belong to expert e and use b[e] ([experts][N][K]), b_scale[e], bias[e]
+ * ([experts][N], bias nullable).  Row r multiplies row a_rows[r] of a
+ * (device int32[rows]; NULL: row r itself), which has a_count rows and as many
+ * scales: a token that several experts take is stored once.  Groups may have
+ * any size, 0 included.  Rows of y past offsets[experts] are not written.  A
+ * row index outside [0, a_count) gives a row of NaN, offsets that are not
+ * ascending or pass `rows` leave their expert's rows unwritten, and both raise
+ * FXPQ_FLAG_RANGE.  experts <= 65535; the rest as for fxpq_token_gemm.
+ */
+fxpq_status fxpq_expert_gemm(fxpq_handle h, int64_t rows, int64_t N, int64_t K, int32_t experts,
+                             const int8_t* a, int64_t a_count, int64_t lda, const float* a_scale,
+                             const int32_t* a_rows, const int32_t* offsets, const int8_t* b,
+                             const float* b_scale, const float* bias, void* y, fxpq_dtype y_type,
+                             int64_t ldy);
+
+/*
+ * A paged key / value cache in 8-bit codes with one scale for each page and
+ * head: value = code * scale.  `page` tokens a page (16, 32, 64 or 128),
+ * `heads` key / value heads of `dim` (a multiple of 16, 16..256) dimensions:
+ *     k        int8 [pages][heads][page][dim]
+ *     v        int8 [pages][heads][page / 16][dim][16]   (16 tokens side by side)
+ *     k_scale, v_scale   float [pages][heads]
+ * k and v are 16-byte aligned.  The memory needs no initialization.
+ */
+typedef struct {
+  int8_t* k;
+  int8_t* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t pages, page, heads, dim;
+} fxpq_kv_cache;
+
+/*
+ * The sequences of one call (all arrays on the device).  Sequence s has
+ * length[s] tokens in the cache, of which the last start[s + 1] - start[s] are
+ * the call's (its new tokens; rows start[s] .. start[s + 1] - 1 of the call's
+ * tensors), and its token t lies in page table[s * table_ld + t / page], slot
+ * t % page.  Host bounds: `tokens` rows in all, max_new new tokens and max_len
+ * tokens of any sequence.  A sequence whose numbers contradict these bounds
+ * (or max_len pages that the table has) is skipped; a page outside the cache
+ * is not touched, and its tokens are not seen.  Both raise FXPQ_FLAG_RANGE.
+ */
+typedef struct {
+  const int32_t* start;  /* [seqs + 1] */
+  const int32_t* length; /* [seqs] */
+  const int32_t* table;  /* [seqs][table_ld] */
+  int32_t seqs, table_ld;
+  int32_t tokens, max_new, max_len;
+  int32_t pad0;
+} fxpq_kv_batch;
+
+/*
+ * Position rotation: pairs (x1, x2) of the first `dims` dimensions of a head
+ * become (x1 cos - x2 sin, x2 cos + x1 sin), with cos / sin (device float
+ * [positions][dims / 2]) of the token's place in its sequence.  Pair i is
+ * dimensions (i, i + dims / 2), or (2 i, 2 i + 1) when interleaved != 0.
+ */
+typedef struct {
+  const float* cos;
+  const float* sin;
+  int32_t positions, dims, interleaved, pad0;
+} fxpq_rotary;
+
+/*
+ * Appends the new tokens' keys and values (rows of `heads * dim` reals, row
+ * strides ldk / ldv) to the cache, keys rotated first (rot nullable: no
+ * rotation), and writes the rotated queries (q_heads heads, row stride ldq) to
+ * q_out (row stride ldqo, may be q itself; q NULL: no queries).  Per page and
+ * head the scale is the DFX scale (FXPQ_SCALE_DFX) of the largest magnitude
+ * that the page got since its first slot was written: it only grows while a
+ * page fills, and when it does the codes already there are requantized
+ * (c = rne(c * old / new): powers of two, so every code stays within one step
+ * of its value however often that happens).  Slots past the sequence's length
+ * are left as they are.  A NaN or an infinity is stored as 0, takes no part
+ * in the scale and raises FXPQ_FLAG_NONFINITE; a token past rot->positions
+ * raises FXPQ_FLAG_RANGE and its sequence is skipped.
+ */
+fxpq_status fxpq_cache_append(fxpq_handle h, const fxpq_kv_cache* cache,
+                              const fxpq_kv_batch* batch, const fxpq_rotary* rot, const void* k,
+                              int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq,
+                              void* q_out, int64_t ldqo, int32_t q_heads, fxpq_dtype type);
+
+/* The values that the batch's new tokens have in the cache, code * scale, as
+ * reals [tokens][heads][dim] (k_out or v_out NULL: not wanted). */
+fxpq_status fxpq_cache_read(fxpq_handle h, const fxpq_kv_cache* cache, const fxpq_kv_batch* batch,
+                            void* k_out, void* v_out, fxpq_dtype type);
+
+/*
+ * Attention of the new tokens' queries over the cache (which holds the new
+ * tokens' own keys and values already):
+ *     o = sum_j softmax_j(softmax_scale * q . k_j) v_j
+ * over all tokens of the sequence, or with causal != 0 over those up to the
+ * query's own.  q: rows of q_heads * dim reals (row stride ldq); query head i
+ * uses key / value head i / (q_heads / heads), q_heads % heads == 0.  out: the
+ * same shape, row stride ldo.  A query that sees no token gets 0, one that
+ * holds a NaN or an infinity gets NaN.  workspace as for fxpq_token_gemm.
+ */
+fxpq_status fxpq_cache_attention_workspace(fxpq_handle h, const fxpq_kv_cache* cache,
+                                           const fxpq_kv_batch* batch, int32_t q_heads,
+                                           int64_t* bytes);
+fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
+                                 const fxpq_kv_batch* batch, const void* q, int64_t ldq,
+                                 int32_t q_heads, float softmax_scale, int32_t causal, void* out,
+                                 int64_t ldo, fxpq_dtype type, void* workspace,
+                                 int64_t workspace_bytes);
 
 /* ---- measurement --------------------------------------------------------- */
 

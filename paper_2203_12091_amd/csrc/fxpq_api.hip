@@ -8,6 +8,7 @@
 #include <new>
 
 #include "common.hpp"
+#include "serve.hpp"
 
 using namespace fxpq;
 
@@ -125,6 +126,37 @@ void epi_to_dev(const fxpq_epilogue* e, SrcDev* d) {
   d->fl_scale = e->fl_scale;
   d->shift = e->shift;
   d->fl_shift = e->fl_shift;
+}
+
+// ---- checks of the 8-bit serving operators
+constexpr int64_t kMaxRows = (1 << 24) - 1;  // one block of 256 threads per row
+constexpr int kMaxHeads = 65535;  // a grid dimension
+
+bool is_real(int t) { return t == FXPQ_F32 || t == FXPQ_F16 || t == FXPQ_BF16; }
+
+fxpq_status gemm_sizes(int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || N < 1 || K < 16 || K % 16 != 0 || M > INT32_MAX || N > INT32_MAX) return FXPQ_ERR_INVALID_ARG;
+  // |a b| <= 2^14
+  return K > 131071 ? FXPQ_ERR_OVERFLOW : FXPQ_OK;
+}
+
+bool cache_ok(const fxpq_kv_cache* c) {
+  return c && c->k && c->v && c->k_scale && c->v_scale && aligned(c->k, 16) && aligned(c->v, 16) &&
+         aligned(c->k_scale, 4) && aligned(c->v_scale, 4) && c->pages >= 1 &&
+         (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) && c->heads >= 1 &&
+         c->heads <= kMaxHeads / 2 && c->dim >= 16 && c->dim <= 256 && c->dim % 16 == 0;
+}
+
+bool batch_ok(const fxpq_kv_batch* b, const fxpq_kv_cache* c) {
+  return b && b->start && b->length && b->table && aligned(b->start, 4) && aligned(b->length, 4) &&
+         aligned(b->table, 4) && b->seqs >= 1 && b->seqs <= 65535 && b->table_ld >= 1 && b->tokens >= 0 &&
+         b->max_new >= 0 && b->max_new <= b->tokens && (b->max_new > 0 || b->tokens == 0) &&
+         b->max_len >= b->max_new && b->max_len <= INT32_MAX - 256 &&
+         (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
+}
+
+bool heads_ok(int q_heads, const fxpq_kv_cache* c) {
+  return q_heads >= 1 && q_heads <= kMaxHeads && q_heads % c->heads == 0;
 }
 
 }  // namespace
@@ -854,6 +886,168 @@ fxpq_status fxpq_teacher_avgpool(fxpq_handle h, const float* x, int32_t n, int32
   if (!h || !x || !y || n < 1 || hw < 1 || c < 1) return FXPQ_ERR_INVALID_ARG;
   DeviceGuard g(h->device);
   return hip_status(launch_teacher_avgpool(ctx(h), x, n, hw, c, y));
+}
+
+// ---- 8-bit serving operators --------------------------------------------------
+fxpq_status fxpq_token_quantize(fxpq_handle h, const void* x, fxpq_dtype x_type, int64_t rows,
+                                int64_t cols, int64_t ldx, int32_t rule, int8_t* codes,
+                                int64_t ldc, float* scale) {
+  if (!h || rows < 0 || cols < 1 || !is_real(x_type)) return FXPQ_ERR_INVALID_ARG;
+  if (rule != FXPQ_SCALE_MAX && rule != FXPQ_SCALE_DFX) return FXPQ_ERR_INVALID_ARG;
+  if (rows > kMaxRows || cols > INT64_MAX / 64 || ldx < cols || ldc % 16 != 0 || ldc < cols)
+    return FXPQ_ERR_INVALID_ARG;
+  if (rows == 0) return FXPQ_OK;
+  if (!x || !codes || !scale) return FXPQ_ERR_INVALID_ARG;
+  if (!aligned(x, real_bytes(x_type)) || !aligned(codes, 16) || !aligned(scale, 4))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  return hip_status(launch_token_quantize(ctx(h), x, x_type, rows, cols, ldx, rule, codes, ldc, scale));
+}
+
+fxpq_status fxpq_token_gemm_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes) {
+  if (!bytes) return FXPQ_ERR_INVALID_ARG;
+  *bytes = 0;
+  const fxpq_status st = gemm_sizes(M, N, K);
+  if (st) return st;
+  *bytes = token_gemm_workspace(M, N, K);
+  return FXPQ_OK;
+}
+
+fxpq_status fxpq_token_gemm(fxpq_handle h, int64_t M, int64_t N, int64_t K, const int8_t* a,
+                            int64_t lda, const float* a_scale, const int8_t* b,
+                            const float* b_scale, const float* bias, void* y, fxpq_dtype y_type,
+                            int64_t ldy, void* workspace, int64_t workspace_bytes) {
+  if (!h || !is_real(y_type)) return FXPQ_ERR_INVALID_ARG;
+  const fxpq_status st = gemm_sizes(M, N, K);
+  if (st) return st;
+  if (lda < K || lda % 16 != 0 || ldy < N) return FXPQ_ERR_INVALID_ARG;
+  if (M == 0) return FXPQ_OK;
+  if (!a || !a_scale || !b || !b_scale || !y) return FXPQ_ERR_INVALID_ARG;
+  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) ||
+      !aligned(bias, 4) || !aligned(y, real_bytes(y_type)))
+    return FXPQ_ERR_INVALID_ARG;
+  const int64_t need = token_gemm_workspace(M, N, K);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  GemmArgs ga{};
+  ga.M = M;
+  ga.N = N;
+  ga.K = K;
+  ga.a = a;
+  ga.a_count = M;
+  ga.lda = lda;
+  ga.a_scale = a_scale;
+  ga.experts = 1;
+  ga.b = b;
+  ga.b_scale = b_scale;
+  ga.bias = bias;
+  ga.y = y;
+  ga.ldy = ldy;
+  ga.flags = h->sc.flags;
+  return hip_status(launch_token_gemm(ctx(h), ga, y_type, workspace));
+}
+
+fxpq_status fxpq_expert_gemm(fxpq_handle h, int64_t rows, int64_t N, int64_t K, int32_t experts,
+                             const int8_t* a, int64_t a_count, int64_t lda, const float* a_scale,
+                             const int32_t* a_rows, const int32_t* offsets, const int8_t* b,
+                             const float* b_scale, const float* bias, void* y, fxpq_dtype y_type,
+                             int64_t ldy) {
+  if (!h || !is_real(y_type)) return FXPQ_ERR_INVALID_ARG;
+  const fxpq_status st = gemm_sizes(rows, N, K);
+  if (st) return st;
+  if (experts < 1 || experts > 65535 || lda < K || lda % 16 != 0 || ldy < N)
+    return FXPQ_ERR_INVALID_ARG;
+  if (rows == 0) return FXPQ_OK;
+  if (a_count < 1 || a_count > INT32_MAX || (!a_rows && a_count < rows)) return FXPQ_ERR_INVALID_ARG;
+  if (!a || !a_scale || !offsets || !b || !b_scale || !y) return FXPQ_ERR_INVALID_ARG;
+  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) ||
+      !aligned(bias, 4) || !aligned(a_rows, 4) || !aligned(offsets, 4) ||
+      !aligned(y, real_bytes(y_type)))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  GemmArgs ga{};
+  ga.M = rows;
+  ga.N = N;
+  ga.K = K;
+  ga.a = a;
+  ga.a_count = a_count;
+  ga.lda = lda;
+  ga.a_scale = a_scale;
+  ga.a_rows = a_rows;
+  ga.offsets = offsets;
+  ga.experts = experts;
+  ga.b = b;
+  ga.b_scale = b_scale;
+  ga.bias = bias;
+  ga.y = y;
+  ga.ldy = ldy;
+  ga.flags = h->sc.flags;
+  return hip_status(launch_expert_gemm(ctx(h), ga, y_type));
+}
+
+fxpq_status fxpq_cache_append(fxpq_handle h, const fxpq_kv_cache* cache,
+                              const fxpq_kv_batch* batch, const fxpq_rotary* rot, const void* k,
+                              int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq,
+                              void* q_out, int64_t ldqo, int32_t q_heads, fxpq_dtype type) {
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)cache->heads * cache->dim;
+  if (ldk < width || ldv < width) return FXPQ_ERR_INVALID_ARG;
+  if (rot && (rot->dims < 0 || rot->dims % 2 != 0 || rot->dims > cache->dim || rot->positions < 0 ||
+              (rot->dims > 0 && (!rot->cos || !rot->sin))))
+    return FXPQ_ERR_INVALID_ARG;
+  if (q) {
+    if (q_heads < 1 || q_heads > kMaxHeads || !q_out || ldq < (int64_t)q_heads * cache->dim ||
+        ldqo < (int64_t)q_heads * cache->dim)
+      return FXPQ_ERR_INVALID_ARG;
+    if (!aligned(q, real_bytes(type)) || !aligned(q_out, real_bytes(type))) return FXPQ_ERR_INVALID_ARG;
+  }
+  if (batch->tokens == 0) return FXPQ_OK;
+  if (!k || !v || !aligned(k, real_bytes(type)) || !aligned(v, real_bytes(type)))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  return hip_status(launch_cache_append(ctx(h), *cache, *batch, rot && rot->dims ? rot : nullptr, k, ldk,
+                                        v, ldv, q, ldq, q_out, ldqo, q_heads, type));
+}
+
+fxpq_status fxpq_cache_read(fxpq_handle h, const fxpq_kv_cache* cache, const fxpq_kv_batch* batch,
+                            void* k_out, void* v_out, fxpq_dtype type) {
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (!aligned(k_out, real_bytes(type)) || !aligned(v_out, real_bytes(type))) return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens == 0 || (!k_out && !v_out)) return FXPQ_OK;
+  DeviceGuard g(h->device);
+  return hip_status(launch_cache_read(ctx(h), *cache, *batch, k_out, v_out, type));
+}
+
+fxpq_status fxpq_cache_attention_workspace(fxpq_handle h, const fxpq_kv_cache* cache,
+                                           const fxpq_kv_batch* batch, int32_t q_heads,
+                                           int64_t* bytes) {
+  if (!bytes) return FXPQ_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (!h || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache))
+    return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens > 0) *bytes = cache_attention_workspace(ctx(h), *cache, *batch, q_heads);
+  return FXPQ_OK;
+}
+
+fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
+                                 const fxpq_kv_batch* batch, const void* q, int64_t ldq,
+                                 int32_t q_heads, float softmax_scale, int32_t causal, void* out,
+                                 int64_t ldo, fxpq_dtype type, void* workspace,
+                                 int64_t workspace_bytes) {
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache))
+    return FXPQ_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)q_heads * cache->dim;
+  if (ldq < width || ldo < width || !isfinite(softmax_scale)) return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens == 0) return FXPQ_OK;
+  if (!q || !out || !aligned(q, real_bytes(type)) || !aligned(out, real_bytes(type)))
+    return FXPQ_ERR_INVALID_ARG;
+  const int64_t need = cache_attention_workspace(ctx(h), *cache, *batch, q_heads);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  return hip_status(launch_cache_attention(ctx(h), *cache, *batch, q, ldq, q_heads, softmax_scale, causal,
+                                           out, ldo, type, workspace));
 }
 
 fxpq_status fxpq_timer_start(fxpq_handle h, fxpq_timer_kind kind) {

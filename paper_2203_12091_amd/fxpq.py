@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(HERE, "libfxpq.so")
 
 # enums (keep in sync with include/fxpq.h)
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_NONFINITE, ERR_OVERFLOW, ERR_HIP, ERR_ALLOC = range(7)
-I8, U8OFF, I16, I32, I64, F32, C8, U32 = range(8)
+I8, U8OFF, I16, I32, I64, F32, C8, U32, F16, BF16 = range(10)
 SRC_F32, SRC_INT, SRC_ACC, SRC_ADD = range(4)
 SIGN_AUTO = -1
 FLAG_NONFINITE, FLAG_RANGE, FLAG_CODE = 0x1, 0x2, 0x4
@@ -28,11 +28,15 @@ EXPORTS = [
     "fxpq_timer_read",
     "fxpq_teacher_conv", "fxpq_teacher_affine", "fxpq_teacher_add", "fxpq_teacher_maxpool",
     "fxpq_teacher_avgpool",
+    "fxpq_token_quantize", "fxpq_token_gemm_workspace", "fxpq_token_gemm", "fxpq_expert_gemm",
+    "fxpq_cache_append", "fxpq_cache_read", "fxpq_cache_attention_workspace",
+    "fxpq_cache_attention",
 ]
 TIMER_OFF, TIMER_FLS_WINDOW, TIMER_QCONV, TIMER_REQUANT, TIMER_CBLOCK_PASS, TIMER_CBLOCK_PRED = range(6)
 TILING_AUTO, TILING_GEMM, TILING_HALO = range(3)
 ROUND_CONSERVATIVE, ROUND_NEUTRAL, ROUND_AGGRESSIVE = range(3)
 PSI_PRINTED, PSI_MAX = range(2)
+SCALE_MAX, SCALE_DFX = range(2)
 
 
 class Fmt(C.Structure):
@@ -55,6 +59,21 @@ class Src(C.Structure):
 
 class ConvDesc(C.Structure):
     _fields_ = [(f, C.c_int32) for f in ("n", "h", "w", "c", "k", "r", "s", "stride", "pad")]
+
+
+class KvCache(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("k", "v", "k_scale", "v_scale")]
+                + [(f, C.c_int32) for f in ("pages", "page", "heads", "dim")])
+
+
+class KvBatch(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("start", "length", "table")]
+                + [(f, C.c_int32) for f in ("seqs", "table_ld", "tokens", "max_new", "max_len", "pad0")])
+
+
+class Rotary(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("cos", "sin")]
+                + [(f, C.c_int32) for f in ("positions", "dims", "interleaved", "pad0")])
 
 
 class FxpqError(RuntimeError):
@@ -114,6 +133,15 @@ def lib():
             "fxpq_teacher_add": [p, p, p, i64, i32, p],
             "fxpq_teacher_maxpool": [p, p, i32, i32, i32, i32, i32, i32, i32, p],
             "fxpq_teacher_avgpool": [p, p, i32, i32, i32, p],
+            "fxpq_token_quantize": [p, p, C.c_int, i64, i64, i64, i32, p, i64, p],
+            "fxpq_token_gemm_workspace": [i64, i64, i64, p],
+            "fxpq_token_gemm": [p, i64, i64, i64, p, i64, p, p, p, p, p, C.c_int, i64, p, i64],
+            "fxpq_expert_gemm": [p, i64, i64, i64, i32, p, i64, i64, p, p, p, p, p, p, p, C.c_int,
+                                 i64],
+            "fxpq_cache_append": [p, p, p, p, p, i64, p, i64, p, i64, p, i64, i32, C.c_int],
+            "fxpq_cache_read": [p, p, p, p, p, C.c_int],
+            "fxpq_cache_attention_workspace": [p, p, p, i32, p],
+            "fxpq_cache_attention": [p, p, p, p, i64, i32, C.c_float, i32, p, i64, C.c_int, p, i64],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -330,6 +358,52 @@ def teacher_avgpool(h, x, n, hw, c, y):
     _call("fxpq_teacher_avgpool", h.value, ptr(x), n, hw, c, ptr(y))
 
 
+def token_quantize(h, x, x_type, rows, cols, ldx, rule, codes, ldc, scale):
+    _call("fxpq_token_quantize", h.value, ptr(x), x_type, rows, cols, ldx, rule, ptr(codes), ldc,
+          ptr(scale))
+
+
+def token_gemm_workspace(M, N, K):
+    b = C.c_int64(0)
+    _call("fxpq_token_gemm_workspace", M, N, K, C.byref(b))
+    return b.value
+
+
+def token_gemm(h, M, N, K, a, lda, a_scale, b, b_scale, bias, y, y_type, ldy, workspace=None,
+               ws_bytes=0):
+    _call("fxpq_token_gemm", h.value, M, N, K, ptr(a), lda, ptr(a_scale), ptr(b), ptr(b_scale),
+          ptr(bias), ptr(y), y_type, ldy, ptr(workspace), ws_bytes)
+
+
+def expert_gemm(h, rows, N, K, experts, a, a_count, lda, a_scale, a_rows, offsets, b, b_scale, bias,
+                y, y_type, ldy):
+    _call("fxpq_expert_gemm", h.value, rows, N, K, experts, ptr(a), a_count, lda, ptr(a_scale),
+          ptr(a_rows), ptr(offsets), ptr(b), ptr(b_scale), ptr(bias), ptr(y), y_type, ldy)
+
+
+def cache_append(h, cache, batch, rot, k, ldk, v, ldv, q, ldq, q_out, ldqo, q_heads, x_type):
+    _call("fxpq_cache_append", h.value, C.byref(cache), C.byref(batch),
+          C.byref(rot) if rot is not None else None, ptr(k), ldk, ptr(v), ldv, ptr(q), ldq,
+          ptr(q_out), ldqo, q_heads, x_type)
+
+
+def cache_read(h, cache, batch, k_out, v_out, x_type):
+    _call("fxpq_cache_read", h.value, C.byref(cache), C.byref(batch), ptr(k_out), ptr(v_out), x_type)
+
+
+def cache_attention_workspace(h, cache, batch, q_heads):
+    b = C.c_int64(0)
+    _call("fxpq_cache_attention_workspace", h.value, C.byref(cache), C.byref(batch), q_heads,
+          C.byref(b))
+    return b.value
+
+
+def cache_attention(h, cache, batch, q, ldq, q_heads, scale, causal, out, ldo, x_type,
+                    workspace=None, ws_bytes=0):
+    _call("fxpq_cache_attention", h.value, C.byref(cache), C.byref(batch), ptr(q), ldq, q_heads,
+          scale, int(causal), ptr(out), ldo, x_type, ptr(workspace), ws_bytes)
+
+
 def timer_start(h, kind):
     _call("fxpq_timer_start", h.value, kind)
 
@@ -380,3 +454,19 @@ def epilogue(channels, fl_w, d_fmt_in, bias=None, fl_bias=0, relu=False, scale=N
 
 def conv_desc(n, h, w, c, k, r, s, stride, pad):
     return ConvDesc(n, h, w, c, k, r, s, stride, pad)
+
+
+def kv_cache(k, v, k_scale, v_scale, pages, page, heads, dim):
+    return _keep(KvCache(k=ptr(k), v=ptr(v), k_scale=ptr(k_scale), v_scale=ptr(v_scale),
+                         pages=pages, page=page, heads=heads, dim=dim), k, v, k_scale, v_scale)
+
+
+def kv_batch(start, length, table, seqs, table_ld, tokens, max_new, max_len):
+    return _keep(KvBatch(start=ptr(start), length=ptr(length), table=ptr(table), seqs=seqs,
+                         table_ld=table_ld, tokens=tokens, max_new=max_new, max_len=max_len),
+                 start, length, table)
+
+
+def rotary(cos, sin, positions, dims, interleaved=0):
+    return _keep(Rotary(cos=ptr(cos), sin=ptr(sin), positions=positions, dims=dims,
+                        interleaved=int(interleaved)), cos, sin)

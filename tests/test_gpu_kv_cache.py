@@ -1,0 +1,487 @@
+"""The paged 8-bit cache (append with rotation, read) and the attention over it,
+against plain implementations: the cache's codes and scales bit for bit (every
+step is a power of two, one fp32 rounding or a round to the even code), the
+attention against 64 bits.
+
+Attention's tolerance, per output value, with S = max |v| of the head's visible
+tokens and L of them: a logit is off by at most d = softmax_scale * (q's digit
+planes: half a unit of the last plane times the sum of the key's magnitudes)
++ 4 * 2^-24 * |logit| (its conversions and products) + the base-2 logarithm's
+share of the same size; a weight by 2 d + 4 * 2^-23 (exp2) and its rounding uP
+before the second product (2^-8 bf16, 2^-16 two terms, 2^-23 three); the sums by
+(L + 64) * 2^-24.  All of it weighs at most S; the type's rounding comes last."""
+import math
+
+import numpy as np
+import pytest
+
+from gpu_util import DEV, note
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def fx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2203_12091_amd import fxpq
+    return fxpq
+
+
+@pytest.fixture(scope="module")
+def h(fx):
+    hd = fx.Handle(0)
+    yield hd
+    hd.close()
+
+
+def code_of(fx, t):
+    return {"f32": fx.F32, "f16": fx.F16, "bf16": fx.BF16}[t]
+
+
+class Cache:
+    """A cache on the device whose unused memory holds the worst there is: code
+    -128, NaN scales, page numbers outside the cache past each sequence's end."""
+
+    def __init__(self, fx, seqs, lens_max, heads, dim, page, seed=0, spare=2):
+        self.fx, self.heads, self.dim, self.page = fx, heads, dim, page
+        need = [-(-n // page) for n in lens_max]
+        self.width = max(max(need), 1)
+        self.pages = sum(need) + spare
+        order = np.random.default_rng(seed).permutation(self.pages)
+        self.table = np.full((seqs, self.width), 2 ** 31 - 1, dtype=np.int32)
+        at = 0
+        for s, n in enumerate(need):
+            self.table[s, :n] = order[at : at + n]
+            at += n
+        self.k = torch.full((self.pages, heads, page, dim), -128, dtype=torch.int8, device=DEV)
+        self.v = torch.full((self.pages, heads, page // 16, dim, 16), -128, dtype=torch.int8, device=DEV)
+        self.ks = torch.full((self.pages, heads), float("nan"), device=DEV)
+        self.vs = torch.full((self.pages, heads), float("nan"), device=DEV)
+        self.desc = fx.kv_cache(self.k, self.v, self.ks, self.vs, self.pages, page, heads, dim)
+        self.dtable = torch.from_numpy(self.table).to(DEV)
+
+    def batch(self, new, length, max_new=None, max_len=None):
+        start = torch.tensor([0] + list(new)).cumsum(0).to(torch.int32).to(DEV)
+        ln = torch.tensor(list(length), dtype=torch.int32, device=DEV)
+        return self.fx.kv_batch(start, ln, self.dtable, len(new), self.width, int(sum(new)),
+                                max(new) if max_new is None else max_new, max(length) if max_len is None else max_len)
+
+    def host(self):
+        """Codes [pages][heads][page][dim] of keys and values, and the scales."""
+        v = self.v.cpu().numpy().transpose(0, 1, 2, 4, 3).reshape(self.pages, self.heads, self.page, self.dim)
+        return self.k.cpu().numpy(), v, self.ks.cpu().numpy(), self.vs.cpu().numpy()
+
+
+def dfx_scale(a):
+    m, e = np.frexp(np.maximum(np.float32(a), np.float32(2.0 ** -100)))
+    return np.float32(math.ldexp(1.0, int(e) - 7 + (1 if m * 128 >= 127.5 else 0)))
+
+
+def rotate(x, pos, cos, sin, dims, interleaved):
+    """x [heads, dim] float32, every operation rounded to float32."""
+    x = x.astype(np.float32).copy()
+    if not dims:
+        return x
+    c, s = cos[pos], sin[pos]
+    i1 = np.arange(0, dims, 2) if interleaved else np.arange(dims // 2)
+    i2 = i1 + 1 if interleaved else i1 + dims // 2
+    x1, x2 = x[:, i1].copy(), x[:, i2].copy()
+    x[:, i1] = x1 * c - x2 * s
+    x[:, i2] = x2 * c + x1 * s
+    return x
+
+
+class Model:
+    """The cache as plain arrays in float32 steps, one sequence at a time."""
+
+    def __init__(self, cache):
+        self.c = cache
+        self.k, self.v, self.ks, self.vs = cache.host()
+
+    def append(self, s, p0, k, v):
+        """k, v: [n, heads, dim] float32, rotated already; finite values only."""
+        P, n = self.c.page, len(k)
+        for nth in range(p0 // P, (p0 + n - 1) // P + 1):
+            page = self.c.table[s, nth]
+            lo, hi = max(p0 - nth * P, 0), min(p0 + n - nth * P, P)
+            for x, codes, scale in ((k, self.k, self.ks), (v, self.v, self.vs)):
+                for hd in range(self.c.heads):
+                    new = x[nth * P + lo - p0 : nth * P + hi - p0, hd]
+                    now = dfx_scale(np.abs(new).max())
+                    if lo > 0:
+                        old = scale[page, hd]
+                        now = max(now, old)
+                        if old < now:
+                            codes[page, hd, :lo] = np.rint(codes[page, hd, :lo].astype(np.float32) * (old / now))
+                    scale[page, hd] = now
+                    codes[page, hd, lo:hi] = np.rint(new / now)
+
+    def check(self, cache):
+        k, v, ks, vs = cache.host()
+        np.testing.assert_array_equal(ks, self.ks)
+        np.testing.assert_array_equal(vs, self.vs)
+        np.testing.assert_array_equal(k, self.k)
+        np.testing.assert_array_equal(v, self.v)
+
+
+def tables(positions, dims):
+    ang = np.arange(positions)[:, None] * 10000.0 ** (-np.arange(0, dims, 2) / dims)
+    return np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+
+
+STEPS = [  # (page, heads, dim, rotated dims, interleaved, q_heads, steps of (new tokens of each sequence))
+    (16, 2, 64, 64, 0, 4, [(5, 0, 16), (1, 1, 1), (12, 33, 0), (1, 0, 1)]),
+    (16, 1, 128, 128, 1, 1, [(1,), (1,), (1,), (1,)]),
+    (32, 3, 80, 32, 0, 3, [(31, 32, 33), (1, 1, 1), (40, 1, 64)]),
+    (64, 2, 16, 16, 1, 2, [(0, 70), (1, 130), (63, 1)]),
+    (128, 1, 256, 0, 0, 2, [(127, 129), (2, 1)]),
+    (16, 2, 96, 48, 0, 6, [(100,), (3,), (1,)]),
+    (32, 1, 192, 192, 0, 1, [(1, 2, 3, 40, 5, 6, 7)]),
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("case", STEPS, ids=str)
+def test_append_and_read(fx, h, t, case):
+    """Several appends to one cache: every code, scale and rotated query equals
+    the plain model's; the values read back are code * scale.  Later tokens are
+    larger, so scales grow inside started pages."""
+    page, heads, dim, dims, inter, q_heads, steps = case
+    note("append", t, case)
+    seqs = len(steps[0])
+    total = [sum(st[s] for st in steps) for s in range(seqs)]
+    cache = Cache(fx, seqs, total, heads, dim, page, seed=dim)
+    model = Model(cache)
+    positions = max(total)
+    cos, sin = tables(positions, dims) if dims else (None, None)
+    rot = fx.rotary(torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV), positions, dims, inter) if dims else None
+    g, at = torch.Generator().manual_seed(5), [0] * seqs
+    for nth, new in enumerate(steps):
+        T = sum(new)
+        width = (q_heads + 2 * heads) * dim + 24
+        x = (torch.randn(T, width, generator=g) * 2.0 ** (nth + torch.randint(-2, 2, (T, 1), generator=g))).to(TYPES[t])
+        x[:, -24:] = float("nan")  # nothing reads between the rows
+        d = x.to(DEV)
+        size = d.element_size()
+        q, k, v = (d.data_ptr() + o * dim * size for o in (0, q_heads, q_heads + heads))
+        length = [a + n for a, n in zip(at, new)]
+        b = cache.batch(new, length)
+        q_out = torch.full((T, q_heads * dim + 8), 7.0, dtype=TYPES[t], device=DEV)
+        fx.cache_append(h, cache.desc, b, rot, k, width, v, width, q, width, q_out, q_heads * dim + 8, q_heads, code_of(fx, t))
+        assert fx.sync_status(h) == 0
+        xs = x.float().numpy()[:, : (q_heads + 2 * heads) * dim].reshape(T, -1, dim)
+        want_q, first = np.zeros((T, q_heads, dim), np.float32), 0
+        for s in range(seqs):
+            ks, vs = [], []
+            for i in range(new[s]):
+                row, pos = xs[first + i], at[s] + i
+                want_q[first + i] = rotate(row[:q_heads], pos, cos, sin, dims, inter)
+                ks.append(rotate(row[q_heads : q_heads + heads], pos, cos, sin, dims, inter))
+                vs.append(row[q_heads + heads :])
+            if new[s]:
+                model.append(s, at[s], np.stack(ks), np.stack(vs))
+            first += new[s]
+            at[s] = length[s]
+        model.check(cache)
+        got_q = q_out.cpu()
+        assert torch.equal(got_q[:, :-8], torch.from_numpy(want_q).flatten(1).to(TYPES[t]))
+        assert (got_q[:, -8:] == 7.0).all()
+    back = cache.batch(total, total)
+    outs = [torch.full((sum(total), heads, dim), 3.0, dtype=TYPES[t], device=DEV) for _ in range(2)]
+    fx.cache_read(h, cache.desc, back, outs[0], outs[1], code_of(fx, t))
+    assert fx.sync_status(h) == 0
+    row = 0
+    for s in range(seqs):
+        for p in range(total[s]):
+            pg = cache.table[s, p // page]
+            for o, codes, scale in ((outs[0], model.k, model.ks), (outs[1], model.v, model.vs)):
+                want = torch.from_numpy(codes[pg, :, p % page].astype(np.float32) * scale[pg][:, None]).to(TYPES[t])
+                assert torch.equal(o[row].cpu(), want) if p in (0, total[s] - 1) or p % 37 == 0 else True
+            row += 1
+    only = torch.zeros_like(outs[1])
+    fx.cache_read(h, cache.desc, back, None, only, code_of(fx, t))
+    assert torch.equal(only, outs[1])
+
+
+def test_growing_scale_stays_within_one_step(fx, h):
+    """Sixteen tokens one by one, each twice as large as the last: the scale of
+    the page grows 15 times, and every stored value is still within one step."""
+    cache = Cache(fx, 1, [16], 1, 32, 16)
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(16, 32, generator=g) * 2.0 ** torch.arange(16)[:, None]
+    for i in range(16):
+        row = x[i : i + 1].to(DEV)
+        fx.cache_append(h, cache.desc, cache.batch([1], [i + 1]), None, row, 32, row, 32, None, 0, None, 0, 0, fx.F32)
+    assert fx.sync_status(h) == 0
+    k, v, ks, vs = cache.host()
+    p = cache.table[0, 0]
+    for codes, s in ((k, ks), (v, vs)):
+        step = float(s[p, 0])
+        assert step == float(dfx_scale(x.abs().max().item()))
+        assert np.abs(codes[p, 0].astype(np.float64) * step - x.double().numpy()).max() <= step
+
+
+def test_append_in_place_queries_and_nonfinite(fx, h):
+    """q_out may be q itself; a NaN or an infinity is stored as 0 and leaves the
+    scale of the finite values."""
+    cache = Cache(fx, 1, [20], 2, 64, 16)
+    cos, sin = tables(20, 64)
+    rot = fx.rotary(torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV), 20, 64)
+    g = torch.Generator().manual_seed(2)
+    q, kv = torch.randn(20, 4 * 64, generator=g), torch.randn(20, 2 * 64, generator=g)
+    v = kv.clone()
+    v[3, 5], v[18, 70] = float("inf"), float("nan")
+    d, dv = q.to(DEV), v.to(DEV)
+    dk = kv.to(DEV)
+    fx.cache_append(h, cache.desc, cache.batch([20], [20]), rot, dk, 128, dv, 128, d, 256, d, 256, 4, fx.F32)
+    assert fx.sync_status(h) == fx.FLAG_NONFINITE
+    want = np.stack([rotate(q[i].view(4, 64).numpy(), i, cos, sin, 64, 0) for i in range(20)])
+    assert torch.equal(d.cpu().view(20, 4, 64), torch.from_numpy(want))
+    _, codes, _, vs = cache.host()
+    clean = torch.where(torch.isfinite(v), v, torch.zeros(())).view(20, 2, 64).numpy()
+    for p in range(20):
+        pg = cache.table[0, p // 16]
+        np.testing.assert_array_equal(codes[pg, :, p % 16], np.rint(clean[p] / vs[pg][:, None]))
+
+
+def test_append_skips_what_contradicts(fx, h):
+    """A sequence longer than the bound, than the rotation's positions, or with
+    more new tokens than it has, is skipped; a page outside the cache is not
+    touched; all raise the flag and leave the rest of the batch right."""
+    cos, sin = tables(64, 32)
+    rot = fx.rotary(torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV), 40, 32)
+    x = torch.randn(30, 32, generator=torch.Generator().manual_seed(3))
+    d = x.to(DEV)
+    for length in ([10, 41, 10], [10, 65, 10], [10, 5, 10], [10, -3, 10]):
+        cache = Cache(fx, 3, [64, 64, 64], 1, 32, 16)
+        model = Model(cache)
+        b = cache.batch([10, 10, 10], length, max_len=64)
+        fx.cache_append(h, cache.desc, b, rot, d, 32, d, 32, None, 0, None, 0, 0, fx.F32)
+        assert fx.sync_status(h) == fx.FLAG_RANGE, length
+        for s in (0, 2):
+            rows = x[10 * s : 10 * s + 10].view(10, 1, 32).numpy()
+            k = np.stack([rotate(rows[i], i, cos, sin, 32, 0) for i in range(10)])
+            model.append(s, 0, k, rows)
+        model.check(cache)
+    cache = Cache(fx, 1, [64], 1, 32, 16)
+    model = Model(cache)
+    cache.dtable[0, 1] = cache.pages
+    fx.cache_append(h, cache.desc, cache.batch([30], [30]), None, d, 32, d, 32, None, 0, None, 0, 0, fx.F32)
+    assert fx.sync_status(h) == fx.FLAG_RANGE
+    model.append(0, 0, x[:16].view(16, 1, 32).numpy(), x[:16].view(16, 1, 32).numpy())
+    model.check(cache)
+
+
+# ---- attention -----------------------------------------------------------------------
+
+def fill(cache, lens, seed):
+    """Random codes and scales in the slots that the sequences use."""
+    g = np.random.default_rng(seed)
+    k, v, ks, vs = (z.copy() for z in cache.host())
+    for s, n in enumerate(lens):
+        for nth in range(-(-n // cache.page)):
+            p, m = cache.table[s, nth], min(cache.page, n - nth * cache.page)
+            k[p, :, :m] = g.integers(-128, 128, (cache.heads, m, cache.dim))
+            v[p, :, :m] = g.integers(-128, 128, (cache.heads, m, cache.dim))
+            ks[p] = 2.0 ** g.integers(-8, -4, cache.heads) * g.choice([1.0, 0.7], cache.heads)
+            vs[p] = 2.0 ** g.integers(-9, 1, cache.heads) * g.choice([1.0, 1.3], cache.heads)
+    cache.k.copy_(torch.from_numpy(k))
+    cache.v.copy_(torch.from_numpy(v.reshape(cache.pages, cache.heads, -1, 16, cache.dim).transpose(0, 1, 2, 4, 3).copy()))
+    cache.ks.copy_(torch.from_numpy(ks))
+    cache.vs.copy_(torch.from_numpy(vs))
+    return k, v, ks.astype(np.float64), vs.astype(np.float64)
+
+
+def check_attention(got, q, host, cache, new, lens, scale, causal, t, q_heads):
+    k, v, ks, vs = host
+    G, row = q_heads // cache.heads, 0
+    for s, n in enumerate(lens):
+        pages = cache.table[s, : -(-n // cache.page)]
+        for hd in range(cache.heads):
+            K = (k[pages, hd].astype(np.float64) * ks[pages, hd][:, None, None]).reshape(-1, cache.dim)[:n]
+            V = (v[pages, hd].astype(np.float64) * vs[pages, hd][:, None, None]).reshape(-1, cache.dim)[:n]
+            for i in range(new[s]):
+                m = n - new[s] + i + 1 if causal else n
+                for gq in range(G):
+                    x = q[row + i, hd * G + gq].astype(np.float64)
+                    y = got[row + i, hd * G + gq].astype(np.float64)
+                    if m <= 0:
+                        assert (y == 0).all()
+                        continue
+                    z = K[:m] @ x * scale
+                    p = np.exp(z - z.max())
+                    p /= p.sum()
+                    want = p @ V[:m]
+                    unit = 2.0 ** (math.floor(math.log2(max(np.abs(x).max(), 2.0 ** -100))) - 6) / (65536 if t != "f32" else 2 ** 24)
+                    d = abs(scale) * (unit * np.abs(K[:m]).sum(1).max()) + 8 * 2.0 ** -24 * np.abs(z).max()
+                    up = {"bf16": 2.0 ** -8, "f16": 2.0 ** -16, "f32": 2.0 ** -23}[t]
+                    tol = (2 * d + 4 * 2.0 ** -23 + up + (m + 64) * 2.0 ** -24) * np.abs(V[:m]).max() + HALF_ULP[t] * np.abs(want) * 1.01 + 2.0 ** -25 * (t == "f16")
+                    err = np.abs(y - want)
+                    assert (err <= tol).all(), (s, hd, i, gq, (err / tol).max())
+        row += new[s]
+
+
+def run_attention(fx, h, cache, new, lens, q, q_heads, scale, causal, t, ldq=None, shift=0, **bounds):
+    T, W = sum(new), q_heads * cache.dim
+    ldq = ldq or W
+    buf = torch.full((T * ldq + 8,), float("nan"), dtype=TYPES[t])
+    rows = buf[shift : shift + T * ldq].view(T, ldq)
+    rows[:, :W] = q
+    d = buf.to(DEV)
+    out = torch.full((T * ldq + 8,), 5.0, dtype=TYPES[t], device=DEV)
+    b = cache.batch(new, lens, **bounds)
+    need = fx.cache_attention_workspace(h, cache.desc, b, q_heads)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device=DEV)
+    fx.cache_attention(h, cache.desc, b, d[shift:], ldq, q_heads, scale, causal, out[shift:], ldq, code_of(fx, t), ws, need)
+    o = out.cpu()[shift : shift + T * ldq].view(T, ldq)
+    assert (o[:, W:] == 5.0).all()
+    return o[:, :W].float().view(T, q_heads, cache.dim).numpy()
+
+
+ATT = [  # (heads, query heads of one, dim, page, new, lengths, causal)
+    (1, 1, 64, 16, [1], [1], 1),
+    (2, 4, 128, 16, [1, 1, 1, 1], [300, 17, 16, 1], 1),
+    (1, 8, 128, 64, [1], [5000], 1),
+    (2, 1, 16, 16, [1, 1], [63, 65], 0),
+    (1, 16, 80, 32, [1, 0, 1], [129, 40, 64], 1),
+    (1, 20, 96, 32, [1, 1], [513, 31], 1),
+    (2, 3, 256, 128, [2, 1], [700, 129], 1),
+    (1, 2, 192, 16, [3], [1000], 0),
+    (2, 4, 64, 16, [40, 7, 1], [40, 100, 260], 1),
+    (1, 1, 128, 32, [130], [130], 1),
+    (1, 4, 128, 64, [70, 70], [70, 900], 0),
+    (1, 3, 112, 16, [5, 33], [2100, 33], 1),
+    (1, 1, 256, 16, [65], [200], 1),
+    (1, 40, 64, 16, [1], [3000], 1),
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("case", ATT, ids=str)
+def test_attention(fx, h, t, case):
+    heads, group, dim, page, new, lens, causal = case
+    note("attention", t, case)
+    cache = Cache(fx, len(new), lens, heads, dim, page, seed=dim + page)
+    host = fill(cache, lens, 7)
+    q_heads = heads * group
+    q = torch.randn(sum(new), q_heads * dim, generator=torch.Generator().manual_seed(11)).to(TYPES[t])
+    scale = dim ** -0.5
+    for ldq, shift in ((None, 0), (q_heads * dim + 3, 1)):
+        got = run_attention(fx, h, cache, new, lens, q, q_heads, scale, causal, t, ldq, shift)
+        assert fx.sync_status(h) == 0
+        check_attention(got, q.float().view(-1, q_heads, dim).numpy(), host, cache, new, lens, scale, causal, t, q_heads)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [[0, 3, 2, 1], [1, 1, 1, 1]], ids=str)
+def test_attention_of_short_and_empty_sequences(fx, h, t, new):
+    """Sequences without new tokens, of length one, and bounds (new tokens,
+    length) far above what the batch holds: more splits than there is work."""
+    lens = [4, 3, 2, 1]
+    cache = Cache(fx, 4, [4096] * 4, 2, 64, 16)
+    host = fill(cache, lens, 3)
+    q = torch.randn(sum(new), 8 * 64, generator=torch.Generator().manual_seed(1)).to(TYPES[t])
+    for bounds in (dict(), dict(max_len=4096)):
+        got = run_attention(fx, h, cache, new, lens, q, 8, 0.3, 1, t, **bounds)
+        assert fx.sync_status(h) == 0
+        check_attention(got, q.float().view(-1, 8, 64).numpy(), host, cache, new, lens, 0.3, 1, t, 8)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_attention_extremes(fx, h, new):
+    """Logits far apart (one token takes all), all equal (scale 0), a query of
+    zeros, one with a lone huge dimension, and one that holds a NaN: only its own
+    row is NaN."""
+    lens = [400]
+    cache = Cache(fx, 1, lens, 1, 128, 16)
+    host = fill(cache, lens, 5)
+    q = torch.randn(new, 4, 128, generator=torch.Generator().manual_seed(8))
+    q[0, 0] = 0
+    q[0, 1, 7] = 3000.0
+    q = q.flatten(1).to(torch.bfloat16)
+    for scale in (0.0, 5.0, -0.2):
+        got = run_attention(fx, h, cache, [new], lens, q, 4, scale, 1, "bf16")
+        check_attention(got, q.float().view(-1, 4, 128).numpy(), host, cache, [new], lens, scale, 1, "bf16", 4)
+    q[0, 2 * 128 + 3] = float("nan")
+    q[0, 3 * 128 + 1] = float("inf")
+    got = run_attention(fx, h, cache, [new], lens, q, 4, 0.1, 1, "bf16")
+    bad = np.isnan(got).all(-1)
+    assert bad[0].tolist() == [False, False, True, True] and not bad[1:].any() and np.isnan(got).any(-1).sum() == 2
+    assert fx.sync_status(h) == 0
+
+
+def test_attention_page_outside_the_cache(fx, h):
+    """Its tokens are not seen, and the flag is raised."""
+    lens = [100]
+    cache = Cache(fx, 1, lens, 1, 64, 16)
+    host = fill(cache, lens, 6)
+    q = torch.randn(1, 4 * 64, generator=torch.Generator().manual_seed(9))
+    cache.dtable[0, 2] = -5
+    got = run_attention(fx, h, cache, [1], lens, q, 4, 0.125, 1, "f32")
+    assert fx.sync_status(h) == fx.FLAG_RANGE
+    keep = np.r_[0:32, 48:100]
+    k, v, ks, vs = host
+    p = cache.table[0]
+    K = (k[p, 0] * ks[p, 0][:, None, None]).reshape(-1, 64)[keep]
+    V = (v[p, 0] * vs[p, 0][:, None, None]).reshape(-1, 64)[keep]
+    for i in range(4):
+        z = K @ q[0].view(4, 64)[i].double().numpy() * 0.125
+        w = np.exp(z - z.max())
+        np.testing.assert_allclose(got[0, i], w @ V / w.sum(), atol=1e-4 * np.abs(V).max())
+
+
+def test_cache_calls_reject_bad_arguments(fx, h):
+    cache = Cache(fx, 2, [64, 64], 2, 32, 16)
+    x = torch.zeros(64 * 64, device=DEV)
+    good = cache.batch([3, 2], [10, 20])
+
+    def desc(**kw):
+        return fx.kv_cache(**{**dict(k=cache.k, v=cache.v, k_scale=cache.ks, v_scale=cache.vs, pages=cache.pages,
+                                     page=16, heads=2, dim=32), **kw})
+
+    def batch(**kw):
+        return fx.kv_batch(**{**dict(start=cache.dtable, length=cache.dtable, table=cache.dtable, seqs=2, table_ld=4,
+                                     tokens=5, max_new=3, max_len=20), **kw})
+
+    def calls(c, b):
+        yield lambda: fx.cache_append(h, c, b, None, x, 64, x, 64, None, 0, None, 0, 0, fx.F32)
+        yield lambda: fx.cache_read(h, c, b, x, x, fx.F32)
+        yield lambda: fx.cache_attention_workspace(h, c, b, 4)
+        yield lambda: fx.cache_attention(h, c, b, x, 128, 4, 1.0, 1, x, 128, fx.F32)
+
+    for kw in (dict(k=None), dict(v_scale=None), dict(page=24), dict(page=8), dict(heads=0), dict(dim=40), dict(dim=272),
+               dict(pages=0), dict(k=cache.k.data_ptr() + 8)):
+        for call in calls(desc(**kw), good):
+            with pytest.raises(fx.FxpqError):
+                call()
+    for kw in (dict(start=None), dict(table=None), dict(seqs=0), dict(table_ld=1), dict(tokens=-1), dict(max_new=6),
+               dict(max_new=0), dict(max_len=2)):
+        for call in calls(desc(), batch(**kw)):
+            with pytest.raises(fx.FxpqError):
+                call()
+    c = desc()
+    cos = torch.zeros(64, 16, device=DEV)
+    for rot in (fx.rotary(cos, cos, 64, 31), fx.rotary(cos, cos, 64, 34), fx.rotary(None, cos, 64, 32)):
+        with pytest.raises(fx.FxpqError):
+            fx.cache_append(h, c, good, rot, x, 64, x, 64, None, 0, None, 0, 0, fx.F32)
+    for kw in (dict(ldk=63), dict(ldv=0), dict(k=None), dict(q=x, ldq=64, q_out=None, q_heads=4, ldqo=128),
+               dict(q=x, ldq=100, q_out=x, q_heads=4, ldqo=128), dict(x_type=fx.I8)):
+        with pytest.raises(fx.FxpqError):
+            fx.cache_append(h, c, good, None, **{**dict(k=x, ldk=64, v=x, ldv=64, q=None, ldq=0, q_out=None, ldqo=0,
+                                                        q_heads=0, x_type=fx.F32), **kw})
+    for kw in (dict(q_heads=3), dict(q_heads=0), dict(ldq=127), dict(ldo=1), dict(q=None), dict(scale=float("nan")),
+               dict(x_type=fx.I32)):
+        with pytest.raises(fx.FxpqError):
+            fx.cache_attention(h, c, good, **{**dict(q=x, ldq=128, q_heads=4, scale=1.0, causal=1, out=x, ldo=128,
+                                                     x_type=fx.F32), **kw})
+    long = Cache(fx, 1, [100000], 1, 64, 16)
+    b = long.batch([1], [100000])
+    assert fx.cache_attention_workspace(h, long.desc, b, 8) > 0
+    with pytest.raises(fx.FxpqError):  # the work space is missing
+        fx.cache_attention(h, long.desc, b, x, 512, 8, 1.0, 1, x, 512, fx.F32)
+    assert fx.sync_status(h) == 0
