@@ -84,22 +84,33 @@ __global__ __launch_bounds__(256) void k_token_quantize(const T* __restrict__ x,
 // 16 zero bytes: what a tile reads past the depth.
 __device__ int4 kZero16[1] = {{0, 0, 0, 0}};
 
-// One depth step of a tile: 128 bytes of every row, as eight 16-byte chunks.
-// Chunk c of row r sits at position c ^ ((r >> 1) & 7): the 16 rows that one
-// pass of a ds_read_b128 takes then cover all 64 banks once.
-constexpr int kStep = 128;
+// One depth step of a tile: KS bytes of every row, as 16-byte chunks.  Chunk c
+// of row r sits at position c ^ f(r), f stepping once in every 256 bytes: the 16
+// rows that one pass of a ds_read_b128 takes then cover all 64 banks once.
+template <int KS>
 __device__ inline int slab_off(int row, int chunk) {
-  return row * kStep + ((chunk ^ ((row >> 1) & 7)) << 4);
+  return row * KS + ((chunk ^ ((row / (256 / KS)) & (KS / 16 - 1))) << 4);
+}
+
+// The same for the rows of a wave's part of the output on their way to memory,
+// RB bytes each.
+template <int RB>
+__device__ inline int out_off(int row, int chunk) {
+  constexpr int per = RB < 256 ? 256 / RB : 1;
+  return row * RB + ((chunk ^ ((row / per) & (RB / 16 - 1))) << 4);
 }
 
 // Output tile BM tokens x BN channels; WR x WC waves, each (BM / WR) x (BN / WC)
-// in 32 x 32 matrix-core tiles.  Both operands go through a two-stage LDS ring
-// filled by global -> LDS loads: the next step's are issued before this step's
-// products, which cover their latency.
-template <int BM, int BN, int WR, int WC, bool GROUP, typename T>
+// in 32 x 32 matrix-core tiles.  Both operands go through an LDS ring of NS
+// stages of KS bytes of depth, filled by global -> LDS loads NS - 1 steps ahead.
+// T = int: a block takes the blockIdx.y-th share of the depth and leaves its sums
+// in g.y, [share][M][ldy], for k_gemm_join.
+template <int BM, int BN, int WR, int WC, int KS, int NS, bool GROUP, typename T>
 __global__ __launch_bounds__(WR* WC * 64) void k_gemm_tile(GemmArgs g) {
   constexpr int NW = WR * WC, TM = BM / WR / 32, TN = BN / WC / 32;
-  constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // 1 KB loads of a wave and step
+  constexpr int kPiece = 1024 / KS;  // rows of one load (1 KB) of a wave
+  constexpr int LA = BM / kPiece / NW, LB = BN / kPiece / NW;  // loads of a wave and step
+  static_assert(BM % (kPiece * NW) == 0 && BN % (kPiece * NW) == 0, "whole loads for every wave");
   extern __shared__ __attribute__((aligned(1024))) int8_t smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -170,37 +181,56 @@ __global__ __launch_bounds__(WR* WC * 64) void k_gemm_tile(GemmArgs g) {
   }
   const int64_t n0 = (int64_t)tn * BN;
 
-  // this lane's part of each 1 KB load: row `lane >> 3` of eight, one chunk
+  int64_t depth = g.K;
+  const int8_t* a = g.a;
+  T* y = static_cast<T*>(g.y);
+  if constexpr (__is_same(T, int)) {
+    const int64_t k0 = blockIdx.y * g.share;
+    depth = min(g.share, g.K - k0);
+    a += k0;
+    b += k0;
+    y += (int64_t)blockIdx.y * g.M * g.ldy;
+  }
+
+  // this lane's part of each 1 KB load: one chunk of one row
+  constexpr int kChunks = KS / 16;
   const int8_t* src[LA + LB];
-  int chunk[LA + LB];
 #pragma unroll
   for (int i = 0; i < LA + LB; ++i) {
     const bool is_a = i < LA;
     const int piece = wave + NW * (is_a ? i : i - LA);
-    const int r = piece * 8 + (lane >> 3);
-    chunk[i] = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    const int r = piece * kPiece + lane / kChunks;
+    const int chunk = ((lane % kChunks) ^ ((r / (256 / KS)) & (kChunks - 1))) * 16;
     if (is_a) {
       int64_t m = min(m0 + r, m_end - 1);  // rows past the end: any row, never stored
       if (GROUP && g.a_rows) {
         const int64_t to = g.a_rows[m];
         m = to < 0 || to >= g.a_count ? 0 : to;
       }
-      src[i] = g.a + m * g.lda;
+      src[i] = a + m * g.lda + chunk;
     } else {
-      src[i] = b + min(n0 + r, g.N - 1) * g.K;
+      src[i] = b + min(n0 + r, g.N - 1) * g.K + chunk;
     }
   }
-  constexpr int kStage = (BM + BN) * kStep;
-  const int64_t steps = (g.K + kStep - 1) / kStep;
-  auto fill = [&](int64_t step, int stage) {
-    const int64_t k0 = step * kStep;
-    int8_t* sa = smem + stage * kStage;
+  constexpr int kStage = (BM + BN) * KS;
+  const int steps = (int)((depth + KS - 1) / KS);
+  // load i of a step's LA + LB
+  auto fill_one = [&](int step, int stage, int i) {
+    dma16(src[i] + (int64_t)step * KS,
+          smem + stage * kStage + wave * 1024 + (i < LA ? NW * i * 1024 : BM * KS + NW * (i - LA) * 1024));
+  };
+  auto fill = [&](int step, int stage) {
+    const int64_t k0 = (int64_t)step * KS;
 #pragma unroll
     for (int i = 0; i < LA + LB; ++i) {
-      const int piece = wave + NW * (i < LA ? i : i - LA);
-      int8_t* to = sa + (i < LA ? 0 : BM * kStep) + piece * 1024;
-      const int64_t k = k0 + chunk[i];
-      dma16(k < g.K ? src[i] + k : reinterpret_cast<const int8_t*>(kZero16), to);
+      if (k0 + KS <= depth) {
+        fill_one(step, stage, i);
+      } else {  // past the depth: zeros
+        const int r = (wave + NW * (i < LA ? i : i - LA)) * kPiece + lane / kChunks;
+        const int chunk = ((lane % kChunks) ^ ((r / (256 / KS)) & (kChunks - 1))) * 16;
+        dma16(k0 + chunk < depth ? src[i] + k0 : reinterpret_cast<const int8_t*>(kZero16),
+              smem + stage * kStage + wave * 1024 + (i < LA ? NW * i * 1024 : BM * KS + NW * (i - LA) * 1024));
+      }
     }
   };
 
@@ -212,74 +242,350 @@ __global__ __launch_bounds__(WR* WC * 64) void k_gemm_tile(GemmArgs g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
   const int wm = wave / WC, wn = wave % WC;
-  const int row0 = wm * (BM / WR) + (lane & 31), col0 = wn * (BN / WC) + (lane & 31);
-  fill(0, 0);
-  for (int64_t s = 0; s < steps; ++s) {
-    wait_vmcnt<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last step's LDS reads are done
-    ring_barrier();  // this stage has landed for every wave, and the other one is free
-    if (s + 1 < steps) fill(s + 1, (int)((s + 1) & 1));
-    const int8_t* sa = smem + (int)(s & 1) * kStage;
-    const int8_t* sb = sa + BM * kStep;
+  // LDS bytes of this lane's chunk 0 or 1 of its first token and channel row (row
+  // l % 32 of a 32-row tile, whose f is the same for every tile); the column kk of
+  // a step is at that address ^ 32 kk
+  const int sw = slab_off<KS>(lane & 31, lane >> 5);
+  const int a_at = wm * (BM / WR) * KS + sw, b_at = BM * KS + wn * (BN / WC) * KS + sw;
+  // The operands of one 32-byte column of the step, two sets in turn: while one
+  // feeds the matrix cores the next is read.  The last column's products run
+  // across the barrier, with the next stage's first operands and the loads of
+  // the stage after it already under way.
+  v4i af[2][TM], bf[2][TN];
+  auto fetch_one = [&](int set, int stage, int kk, int i) {
+    const int at = ((i < TM ? a_at : b_at) + stage * kStage) ^ (kk << 5);
+    if (i < TM) af[set][i] = *reinterpret_cast<const v4i*>(smem + at + i * 32 * KS);
+    else bf[set][i - TM] = *reinterpret_cast<const v4i*>(smem + at + (i - TM) * 32 * KS);
+  };
+  // The products of one set; between(n) runs after the n-th of kProducts: what is
+  // issued there (LDS reads, loads) goes out while the matrix cores work.
+  // Weights are the first operand: a lane then holds four neighbouring channels
+  // of one token in neighbouring registers.
+  constexpr int kProducts = TM * TN, kReads = TM + TN, kLoads = LA + LB;
+  auto multiply = [&](int set, auto between) {
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      v4i af[TM], bf[TN];
-      const int c = kk * 2 + (lane >> 5);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-        af[i] = *reinterpret_cast<const v4i*>(sa + slab_off(row0 + 32 * i, c));
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-        bf[j] = *reinterpret_cast<const v4i*>(sb + slab_off(col0 + 32 * j, c));
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[i], bf[j], acc[i][j], 0, 0, 0);
-    }
-  }
-
-  // lane l, register r: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32
-  T* y = static_cast<T*>(g.y);
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t m = m0 + wm * (BM / WR) + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-      if (m >= m_end) continue;
-      int64_t am = m;
-      bool bad = false;
-      if (GROUP && g.a_rows) {
-        am = g.a_rows[m];
-        bad = am < 0 || am >= g.a_count;
-      }
-      const float sa = bad ? __builtin_nanf("") : g.a_scale[am];
-      if (bad && lane == 0) raise_flag(g.flags, FXPQ_FLAG_RANGE);
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int64_t n = n0 + col0 + 32 * j;
-        if (n < g.N) {
-          const float p = (float)acc[i][j][r] * sa * b_scale[n];
-          y[m * g.ldy + n] = (T)(bias ? p + bias[n] : p);
-        }
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[set][j], af[set][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        between(i * TN + j);
+        __builtin_amdgcn_sched_barrier(0);
       }
+  };
+  auto sync = [&](bool more) {
+    // all but the loads of the NS - 2 stages after the next one have landed
+    if (more) wait_vmcnt<(NS - 2) * (LA + LB)>();
+    else wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's LDS reads are done
+    ring_barrier();
+  };
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < steps) fill(s, s);
+  sync(steps >= NS - 1);
+#pragma unroll
+  for (int i = 0; i < kReads; ++i) fetch_one(0, 0, 0, i);
+  if (NS - 1 < steps) fill(NS - 1, NS - 1);
+  constexpr int kCols = KS / 32;
+  auto columns = [&](int stage) {  // all but the step's last column
+#pragma unroll
+    for (int kk = 0; kk < kCols - 1; ++kk)
+      multiply(kk & 1, [&](int n) {
+#pragma unroll
+        for (int i = n * kReads / kProducts; i < (n + 1) * kReads / kProducts; ++i)
+          fetch_one((kk + 1) & 1, stage, kk + 1, i);
+      });
+  };
+  int stage = 0, s = 0;
+  const int whole = (int)(depth / KS);
+  for (; s + NS < whole; ++s) {  // the step that is loaded lies inside the depth
+    columns(stage);
+    const int next = stage + 1 == NS ? 0 : stage + 1;
+    sync(true);  // the next stage has landed, and every wave has read all of this one
+    multiply((kCols - 1) & 1, [&](int n) {
+#pragma unroll
+      for (int i = n * kReads / kProducts; i < (n + 1) * kReads / kProducts; ++i) fetch_one(0, next, 0, i);
+#pragma unroll
+      for (int i = n * kLoads / kProducts; i < (n + 1) * kLoads / kProducts; ++i) fill_one(s + NS, stage, i);
+    });
+    stage = next;
+  }
+  for (; s < steps; ++s) {
+    columns(stage);
+    const int next = stage + 1 == NS ? 0 : stage + 1;
+    if (s + 1 < steps) {
+      sync(s + NS <= steps);
+      if (s + NS < steps) fill(s + NS, stage);
+#pragma unroll
+      for (int i = 0; i < kReads; ++i) fetch_one(0, next, 0, i);
+    }
+    multiply((kCols - 1) & 1, [](int) {});
+    stage = next;
+  }
+
+  // lane l, register r: channel 8 (r / 4) + 4 (l / 32) + r % 4, token l % 32.
+  // Each 32-token slab of the wave's part goes through the wave's own share of
+  // the LDS (the ring is done with) and leaves as whole 16-byte pieces of rows.
+  constexpr int kW = TN * 32, RB = kW * (int)sizeof(T);  // channels of a slab row, its bytes
+  constexpr int E = 16 / (int)sizeof(T);
+  static_assert(NW * 32 * RB <= NS * kStage, "the slabs fit the ring's LDS");
+  __syncthreads();
+  int8_t* slab = smem + wave * 32 * RB;
+  const int64_t c0 = n0 + wn * kW;  // kW == BN / WC
+  const bool vec = (uintptr_t)y % 16 == 0 && g.ldy * sizeof(T) % 16 == 0;
+  float sb[TN][16], bi[TN][16];
+  auto channels = [&](const float* from, float(&to)[TN][16]) {
+    if ((uintptr_t)from % 16 == 0 && n0 + BN <= g.N) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const v4f v = *reinterpret_cast<const v4f*>(from + c0 + 32 * j + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[j][4 * q + r] = v[r];
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          to[j][r] = from[min(c0 + 32 * j + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, g.N - 1)];
+    }
+  };
+  if constexpr (!__is_same(T, int)) {
+    channels(b_scale, sb);
+    if (bias) channels(bias, bi);
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t first = m0 + wm * (BM / WR) + 32 * i;
+    if (first >= m_end) break;
+    const int64_t m = min(first + (lane & 31), m_end - 1);
+    int64_t am = m;
+    bool bad = false;
+    if (GROUP && g.a_rows) {
+      am = g.a_rows[m];
+      bad = am < 0 || am >= g.a_count;
+      if (bad) raise_flag(g.flags, FXPQ_FLAG_RANGE);
+    }
+    float sa = 0.0f;
+    if constexpr (!__is_same(T, int)) sa = bad ? __builtin_nanf("") : g.a_scale[am];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        Reals<T, 4> v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (__is_same(T, int)) {
+            v.v[r] = acc[i][j][4 * q + r];
+          } else {
+            const float p = (float)acc[i][j][4 * q + r] * sa * sb[j][4 * q + r];
+            v.v[r] = (T)(bias ? p + bi[j][4 * q + r] : p);
+          }
+        }
+        const int n = 32 * j + 8 * q + 4 * (lane >> 5);
+        *reinterpret_cast<Reals<T, 4>*>(reinterpret_cast<T*>(slab + out_off<RB>(lane & 31, n / E)) + n % E) = v;
+      }
+    // the wave's own LDS accesses complete in order: no barrier
+    constexpr int kRowChunks = RB / 16;
+#pragma unroll
+    for (int k = 0; k < 32 * kRowChunks / 64; ++k) {
+      const int at = k * 64 + lane, row = at / kRowChunks, chunk = at % kRowChunks;
+      const Reals<T, E> v = *reinterpret_cast<const Reals<T, E>*>(slab + out_off<RB>(row, chunk));
+      const int64_t to = first + row, n = c0 + chunk * E;
+      if (to >= m_end || n >= g.N) continue;
+      T* p = y + to * g.ldy + n;
+      if (vec && n + E <= g.N) {
+        *reinterpret_cast<Reals<T, E>*>(p) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (n + e < g.N) p[e] = v.v[e];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The sums of a split depth, [shares][M][ldw] integers in any order, scaled and
+// rounded: four channels of one row a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, const int* part, int64_t ldw, int shares) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, quads = ldw / 4;
+  const int64_t m = i / quads, n = i % quads * 4;
+  if (m >= g.M) return;
+  v4i sum = {0, 0, 0, 0};
+  for (int s = 0; s < shares; ++s) sum += *reinterpret_cast<const v4i*>(part + ((int64_t)s * g.M + m) * ldw + n);
+  const float sa = g.a_scale[m];
+  T* y = static_cast<T*>(g.y) + m * g.ldy + n;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (n + r < g.N) {
+      const float p = (float)sum[r] * sa * g.b_scale[n + r];
+      y[r] = (T)(g.bias ? p + g.bias[n + r] : p);
     }
 }
 
-template <int BM, int BN, int WR, int WC, bool GROUP, typename T>
-hipError_t run_tile(const Ctx& c, const GemmArgs& g) {
+// ---- at most 16 rows: the weights are the work ------------------------------------
+// One block per 16 output channels; its eight waves deal the depth among them in
+// 128-byte steps and read both operands straight into the matrix cores' registers
+// (lane: channel or row l % 16, 16 bytes of the depth): nothing waits for a
+// barrier before the end, where the eight partial sums are joined.
+constexpr int kFewRows = 16;
+
+template <bool GROUP, typename T>
+__global__ __launch_bounds__(512) void k_gemm_few(GemmArgs g) {
+  constexpr int kWaves = 8, kStep = 128;
+  constexpr int U = 4;  // steps whose loads are in flight together
+  __shared__ v4i part[kWaves][64];
+  const int lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  int64_t lo = 0, hi = g.M;
+  const int8_t* b = g.b;
+  const float *b_scale = g.b_scale, *bias = g.bias;
+  if constexpr (GROUP) {
+    const int64_t e = blockIdx.y;
+    lo = g.offsets[e];
+    hi = g.offsets[e + 1];
+    if (lo < 0 || hi < lo || hi > g.M) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(g.flags, FXPQ_FLAG_RANGE);
+      return;
+    }
+    if (lo == hi) return;
+    b += e * g.N * g.K;
+    b_scale += e * g.N;
+    if (bias) bias += e * g.N;
+  }
+  const int64_t m = lo + n;  // this lane's row, as an operand and as a result
+  int64_t am = min(m, hi - 1);
+  bool bad = false;
+  if (GROUP && g.a_rows) {
+    am = g.a_rows[am];
+    bad = am < 0 || am >= g.a_count;
+    am = bad ? 0 : am;
+  }
+  const int8_t* a_row = g.a + am * g.lda;
+  const int8_t* w_row = b + min(n0 + n, g.N - 1) * g.K;
+  const int64_t steps = (g.K + kStep - 1) / kStep;
+  v4i acc = {0, 0, 0, 0};
+  for (int64_t s = wave; s < steps; s += kWaves * U) {
+    v4i w[U][2], x[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t at = (s + u * kWaves) * kStep + k * 64 + q * 16;
+        const bool in = at < g.K;  // past the depth: zero weights, any codes
+        w[u][k] = *reinterpret_cast<const v4i*>(in ? w_row + at : reinterpret_cast<const int8_t*>(kZero16));
+        x[u][k] = *reinterpret_cast<const v4i*>(a_row + (in ? at : 0));
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][k], x[u][k], acc, 0, 0, 0);
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0 || m >= hi) return;
+  if (bad) raise_flag(g.flags, FXPQ_FLAG_RANGE);
+  // lane l: channels 4 (l / 16) + 0..3 of row l % 16
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) acc += part[w][lane];
+  const float sa = bad ? __builtin_nanf("") : g.a_scale[am];
+  T* y = static_cast<T*>(g.y) + m * g.ldy;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t c = n0 + 4 * q + r;
+    if (c < g.N) {
+      const float p = (float)acc[r] * sa * b_scale[c];
+      y[c] = (T)(bias ? p + bias[c] : p);
+    }
+  }
+}
+
+template <bool GROUP, typename T>
+hipError_t run_few(const Ctx& c, const GemmArgs& g) {
+  k_gemm_few<GROUP, T><<<dim3((unsigned)((g.N + 15) / 16), GROUP ? (unsigned)g.experts : 1u), dim3(512), 0,
+                         c.stream>>>(g);
+  return hipGetLastError();
+}
+
+template <int BM, int BN, int WR, int WC, int KS, int NS, bool GROUP, typename T>
+hipError_t run_tile(const Ctx& c, const GemmArgs& g, int shares = 1) {
   const int64_t tiles_n = (g.N + BN - 1) / BN;
   // groups of any sizes need at most one partly filled row tile each
   const int64_t tiles_m = GROUP ? g.M / BM + g.experts : (g.M + BM - 1) / BM;
   if (tiles_m * tiles_n * WR * WC * 64 > 0xFFFFFFFF) return hipErrorInvalidValue;
-  constexpr int bytes = 2 * (BM + BN) * kStep;
-  auto* f = k_gemm_tile<BM, BN, WR, WC, GROUP, T>;
+  constexpr int bytes = NS * (BM + BN) * KS;
+  auto* f = k_gemm_tile<BM, BN, WR, WC, KS, NS, GROUP, T>;
   // more than 64 KB of LDS has to be asked for
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != hipSuccess) return e;
-  f<<<dim3((unsigned)(tiles_m * tiles_n)), dim3(WR * WC * 64), bytes, c.stream>>>(g);
+  f<<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(WR * WC * 64), bytes, c.stream>>>(g);
   return hipGetLastError();
+}
+
+// A product whose depth is split among `shares` blocks of each tile.
+template <int BM, int BN, int WR, int WC, int KS, int NS, typename T>
+hipError_t run_split(const Ctx& c, const GemmArgs& g, int shares, void* ws) {
+  GemmArgs p = g;
+  p.share = ((g.K + shares - 1) / shares + KS - 1) / KS * KS;
+  shares = (int)((g.K + p.share - 1) / p.share);
+  p.y = ws;
+  p.ldy = (g.N + 3) / 4 * 4;
+  const hipError_t e = run_tile<BM, BN, WR, WC, KS, NS, false, int>(c, p, shares);
+  if (e != hipSuccess) return e;
+  k_gemm_join<T><<<dim3((unsigned)((g.M * (p.ldy / 4) + 255) / 256)), dim3(256), 0, c.stream>>>(
+      g, static_cast<const int*>(ws), p.ldy, shares);
+  return hipGetLastError();
+}
+
+// ---- which tiles ---------------------------------------------------------------------
+constexpr int64_t kCus = 256;  // of an MI355X; the work space's size must not need a handle
+
+// Time of a product by its tiles' shape, in us at a depth of 4096 (measured): the
+// 256 x 256 tile has a CU to itself, the others share it with a second block, which
+// costs less than twice the time of one.
+enum Tile { T64, T128x64, T128, T256 };
+double tile_cost(Tile t, double tiles) {
+  constexpr double one[] = {11.5, 16, 24, 43}, two[] = {17, 27, 41, 86};
+  const double rounds = floor(tiles / (2 * kCus)), rest = tiles - rounds * 2 * kCus;
+  return rounds * two[t] + (rest == 0 ? 0 : rest <= kCus ? one[t] : two[t]);
+}
+
+// Row tiles of groups: each expert fills its last one in part.
+double tiles_of(double rows, int64_t N, int bm, int bn, double experts) {
+  return (experts ? rows / bm + 0.75 * experts : ceil(rows / bm)) * (double)((N + bn - 1) / bn);
+}
+
+Tile best_tile(int64_t M, int64_t N, double experts, bool large) {
+  const double cost[] = {tile_cost(T64, tiles_of((double)M, N, 64, 64, experts)),
+                         tile_cost(T128x64, tiles_of((double)M, N, 128, 64, experts)),
+                         tile_cost(T128, tiles_of((double)M, N, 128, 128, experts)),
+                         tile_cost(T256, tiles_of((double)M, N, 256, 256, experts))};
+  int best = T64;
+  for (int t = T128x64; t <= (large ? T256 : T128); ++t)
+    if (cost[t] < cost[best]) best = t;
+  return (Tile)best;
+}
+
+// At most 16 rows: 6.5 us against 10.6 by 64 x 64 tiles (1 x 4096 x 4096), as long
+// as no CU gets more than one block (8 x 8192 x 1024: 6.5 against 5.1).
+bool few_rows(int64_t M, int64_t N) { return M <= kFewRows && N <= 16 * kCus; }
+
+// Where 64 x 64 tiles leave CUs idle and the depth is long, blocks share it: each
+// at least 2048 deep (64 x 4096 x 9216: 20.2 us whole, 13.4 in four; 64 x 1000 x
+// 2048: 7.2 whole, 8.4 in two).
+int depth_shares(int64_t M, int64_t N, int64_t K) {
+  if (few_rows(M, N)) return 1;
+  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+  int64_t shares = kCus / tiles;
+  if (shares > K / 2048) shares = K / 2048;
+  return (int)(shares < 1 ? 1 : shares > 8 ? 8 : shares);
 }
 
 }  // namespace
@@ -301,17 +607,41 @@ hipError_t launch_token_quantize(const Ctx& c, const void* x, int x_type, int64_
 }
 
 int64_t token_gemm_workspace(int64_t M, int64_t N, int64_t K) {
-  (void)M, (void)N, (void)K;
-  return 0;
+  const int shares = depth_shares(M, N, K);
+  return shares > 1 ? (int64_t)shares * M * ((N + 3) / 4 * 4) * 4 : 0;
 }
 
 hipError_t launch_token_gemm(const Ctx& c, const GemmArgs& g, int y_type, void* ws) {
-  (void)ws;
-  return for_real(y_type, [&](auto zero) { return run_tile<128, 128, 2, 2, false, decltype(zero)>(c, g); });
+  return for_real(y_type, [&](auto zero) {
+    using T = decltype(zero);
+    if (few_rows(g.M, g.N)) return run_few<false, T>(c, g);
+    const int shares = depth_shares(g.M, g.N, g.K);
+    if (shares > 1) return run_split<64, 64, 2, 2, 128, 4, T>(c, g, shares, ws);
+    switch (best_tile(g.M, g.N, 0, true)) {
+      case T64: return run_tile<64, 64, 2, 2, 128, 4, false, T>(c, g);
+      case T128x64: return run_tile<128, 64, 2, 2, 128, 3, false, T>(c, g);
+      case T128: return run_tile<128, 128, 2, 2, 128, 2, false, T>(c, g);
+      default: return run_tile<256, 256, 2, 4, 128, 2, false, T>(c, g);
+    }
+  });
 }
 
 hipError_t launch_expert_gemm(const Ctx& c, const GemmArgs& g, int y_type) {
-  return for_real(y_type, [&](auto zero) { return run_tile<128, 128, 2, 2, true, decltype(zero)>(c, g); });
+  return for_real(y_type, [&](auto zero) {
+    using T = decltype(zero);
+    if (few_rows(g.M, g.N)) return run_few<true, T>(c, g);
+    // 128 rows of 32 experts (4096 x 2048 weights): 58.7 us by 32 x 64 tiles, 65.1 by
+    // 64 x 64, 93 by the kernel for few rows; 1024 rows of 16: 56.6, 56.1 and (128 x
+    // 128) 51.5; 2048 of 16: 128 x 128 57.6, 256 x 256 70.4; 8192 of 16: 136 and 123
+    const int64_t mean = g.M / g.experts;
+    if (mean <= 32) return run_tile<32, 64, 1, 2, 128, 4, true, T>(c, g);
+    switch (best_tile(g.M, g.N, g.experts, mean >= 192)) {
+      case T64: return run_tile<64, 64, 2, 2, 128, 4, true, T>(c, g);
+      case T128x64: return run_tile<128, 64, 2, 2, 128, 3, true, T>(c, g);
+      case T128: return run_tile<128, 128, 2, 2, 128, 2, true, T>(c, g);
+      default: return run_tile<256, 256, 2, 4, 128, 2, true, T>(c, g);
+    }
+  });
 }
 
 }  // namespace fxpq

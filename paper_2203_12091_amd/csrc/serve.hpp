@@ -83,6 +83,7 @@ struct GemmArgs {
   const float* bias;
   void* y;
   int64_t ldy;
+  int64_t share;  // of the depth, for one block (split products)
   unsigned* flags;
 };
 

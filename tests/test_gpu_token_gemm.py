@@ -163,6 +163,26 @@ def test_token_gemm(fx, h, m, n, k, t):
     assert torch.equal(y.cpu(), got)
 
 
+@pytest.mark.parametrize("m,n,k", [(20, 70, 4112), (64, 203, 9216), (17, 16, 20000), (130, 1025, 2064), (400, 2100, 272),
+                                   (1000, 4100, 144), (4000, 2100, 144), (16, 4096, 1040), (16, 4097, 1040)])
+def test_token_gemm_every_tile(fx, h, m, n, k):
+    """Sizes that reach each tile shape, the split depth (its last share shorter)
+    and both sides of the few-rows rule; bf16 results, reference sums in 64 bits on
+    the device."""
+    note("token_gemm tiles", m, n, k)
+    a = torch.randint(-128, 128, (m, k), device=DEV, dtype=torch.int16).to(torch.int8)
+    b = torch.randint(-128, 128, (n, k), device=DEV, dtype=torch.int16).to(torch.int8)
+    sa, sb, bias = torch.rand(m, device=DEV), torch.rand(n, device=DEV), torch.randn(n, device=DEV)
+    y = torch.zeros(m, n, device=DEV)
+    need = fx.token_gemm_workspace(m, n, k)
+    ws = torch.full((max(need, 16),), 0x5A, dtype=torch.uint8, device=DEV)
+    fx.token_gemm(h, m, n, k, a, k, sa, b, sb, bias, y, fx.F32, n, ws, need)
+    assert fx.sync_status(h) == 0
+    p = (a.double() @ b.double().t()) * sa.double()[:, None] * sb.double()
+    want = p + bias.double()
+    assert ((y.double() - want).abs() <= 2.0 ** -24 * (4 * p.abs() + 3 * want.abs())).all()
+
+
 def test_token_gemm_deepest_sum(fx, h):
     """All codes -128 at the deepest contraction: 2^14 a term, just inside int32."""
     k = 131056
@@ -225,6 +245,25 @@ def test_expert_gemm(fx, h, counts, t, n, k, gather, biased):
                             bias[i].numpy() if biased else None)
         check(got[lo:hi].float().numpy(), p, want, t, biased)
     assert (got[used:] == 9.0).all()
+
+
+@pytest.mark.parametrize("e,rows,n,k,skew", [(4, 4000, 515, 272, 1.0), (8, 900, 130, 144, 2.0), (16, 2000, 300, 400, 0.0),
+                                             (3, 16, 200, 1040, 1.0)])
+def test_expert_gemm_large_groups(fx, h, e, rows, n, k, skew):
+    note("expert_gemm large", e, rows, n, k, skew)
+    w = torch.tensor([(1 + i) ** -skew for i in range(e)])
+    off = torch.cat([torch.zeros(1), (w.cumsum(0) / w.sum() * rows).round()]).to(torch.int32)
+    a = torch.randint(-128, 128, (rows, k), device=DEV, dtype=torch.int16).to(torch.int8)
+    b = torch.randint(-128, 128, (e, n, k), device=DEV, dtype=torch.int16).to(torch.int8)
+    sa, sb = torch.rand(rows, device=DEV), torch.rand(e, n, device=DEV)
+    pick = torch.randperm(rows, device=DEV).to(torch.int32)
+    y = torch.zeros(rows, n, device=DEV)
+    fx.expert_gemm(h, rows, n, k, e, a, rows, k, sa, pick, off.to(DEV), b, sb, None, y, fx.F32, n)
+    assert fx.sync_status(h) == 0
+    for i in range(e):
+        at = pick[int(off[i]) : int(off[i + 1])].long()
+        want = (a[at].double() @ b[i].double().t()) * sa[at].double()[:, None] * sb[i].double()
+        assert ((y[int(off[i]) : int(off[i + 1])].double() - want).abs() <= 2.0 ** -24 * 4 * want.abs()).all()
 
 
 def test_expert_gemm_bad_rows_and_offsets(fx, h):
