@@ -32,6 +32,7 @@ struct AttnArgs {
   int col_tiles;        // blocks along a sequence's query columns
   int splits;           // blocks along the cache
   int split_chunks;     // 64-token chunks of one split
+  int page_log2;
   int vec;              // q and out rows are 16-byte aligned
   float* part_o;        // [splits][tokens][q_heads][dim]
   float* part_ml;       // [splits][tokens][q_heads][2]: running maximum and sum
@@ -54,6 +55,35 @@ __device__ inline void codes_to_bf16(int w, int& lo, int& hi) {
               d = (float)(int8_t)(w >> 24);
   lo = (int)__builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
   hi = (int)__builtin_amdgcn_perm(__builtin_bit_cast(unsigned, d), __builtin_bit_cast(unsigned, c), 0x07060302u);
+}
+
+// Four dimensions of one query column: the result, or its share where the cache
+// is split.
+template <typename T>
+__device__ inline void emit(const AttnArgs& a, const SeqDev& s, int head, int split, int col, int d, float mx,
+                            float sum, const float (&v)[4]) {
+  const int i = col / a.group;
+  if (i >= s.fresh || d >= a.c.dim) return;
+  const int64_t row = s.first + (int64_t)i;
+  const int hq = head * a.group + col % a.group;
+  if (a.splits > 1) {
+    const int64_t r = ((int64_t)split * a.b.tokens + row) * a.q_heads + hq;
+    *reinterpret_cast<float4*>(a.part_o + r * a.c.dim + d) = float4{v[0], v[1], v[2], v[3]};
+    if (d == 0) {
+      a.part_ml[2 * r] = mx;
+      a.part_ml[2 * r + 1] = sum;
+    }
+    return;
+  }
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* to = static_cast<T*>(a.out) + row * a.ldo + (int64_t)hq * a.c.dim + d;
+  const float y[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+  if (a.vec) {
+    store_reals<T, 4>(to, y);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[k] = (T)y[k];
+  }
 }
 
 // DB: 64-dimension blocks of a head; NC: 16-column query tiles of a wave; SPLIT_Q:
@@ -161,12 +191,12 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
   }
   const int first_limit = a.causal ? pos0 + col0 / a.group : s.len - 1;
   const int32_t* table = a.b.table + (int64_t)blockIdx.z * a.b.table_ld;
-  const int last_nth = (s.len - 1) / P;
+  const int last_nth = (s.len - 1) >> a.page_log2;
   const int stride = TOK ? 4 : 1;
 
   // page of a group of 16 tokens, 0 where it has none (then nothing is seen of it)
   auto page_of = [&](int t) {
-    const int nth = t / P;
+    const int nth = t >> a.page_log2;
     return nth <= last_nth ? table[nth] : -1;
   };
   const int kg = n >> 2;  // group of the K rows that this lane loads
@@ -175,7 +205,7 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
     const int t0 = chunk * 64 + kg * 16;
     int page = page_of(t0);
     page = page < 0 || page >= a.c.pages ? 0 : page;
-    const int8_t* base = a.c.k + k_offset(a.c, page, head, t0 % P + (n & 3));
+    const int8_t* base = a.c.k + k_offset(a.c, page, head, (t0 & (P - 1)) + (n & 3));
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -194,7 +224,7 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
     const int page = there ? named : 0;
     const int64_t at = (int64_t)page * a.c.heads + head;
     const float ks = there ? a.c.k_scale[at] : 0.0f, vs = there ? a.c.v_scale[at] : 0.0f;
-    const int8_t* vbase = a.c.v + v_offset(a.c, page, head, t0 % P, 0);
+    const int8_t* vbase = a.c.v + v_offset(a.c, page, head, (t0 & (P - 1)), 0);
 #pragma unroll
     for (int j = 0; j < DT; ++j)
       vr[j] = *reinterpret_cast<const v4i*>(vbase + min(j * 16, D - 16) * 16 + n * 16);
@@ -292,37 +322,13 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
   }
 
   // lane: column n of tile c, dimensions 16 j + 4 g + 0..3
-  auto emit = [&](int col, int d, float mx, float sum, const float(&v)[4]) {
-    const int i = col / a.group;
-    if (i >= s.fresh || d >= D) return;
-    const int64_t row = s.first + (int64_t)i;
-    const int hq = head * a.group + col % a.group;
-    if (a.splits > 1) {
-      const int64_t r = ((int64_t)split * a.b.tokens + row) * a.q_heads + hq;
-      *reinterpret_cast<float4*>(a.part_o + r * D + d) = float4{v[0], v[1], v[2], v[3]};
-      if (d == 0) {
-        a.part_ml[2 * r] = mx;
-        a.part_ml[2 * r + 1] = sum;
-      }
-      return;
-    }
-    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T* to = static_cast<T*>(a.out) + row * a.ldo + (int64_t)hq * D + d;
-    const float y[4] = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
-    if (a.vec) {
-      store_reals<T, 4>(to, y);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) to[k] = (T)y[k];
-    }
-  };
   if constexpr (!TOK) {
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int j = 0; j < DT; ++j) {
         const float v[4] = {o[c][j][0], o[c][j][1], o[c][j][2], o[c][j][3]};
-        emit(col0 + c * 16 + n, j * 16 + g * 4, m[c], l[c], v);
+        emit<T>(a, s, head, split, col0 + c * 16 + n, j * 16 + g * 4, m[c], l[c], v);
       }
   } else {
     // join the four waves: each one's statistics and sums through LDS
@@ -354,14 +360,331 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] += f * ow[k];
       }
-      emit(tile0 + col, d, mx, sum, v);
+      emit<T>(a, s, head, split, tile0 + col, d, mx, sum, v);
+    }
+  }
+}
+
+// ---- many query columns ----------------------------------------------------------
+// A block of four waves, 16 NC columns each, goes over the cache together: every
+// thread loads its share of the next 64 tokens' codes while the waves work on the
+// current ones, converts it and leaves it in LDS in the operand types, K as T's own
+// matrix-core type (bf16 for f32), V as bf16 (both hold a code exactly).  q goes in
+// as QT terms of that type (exact for f16 and bf16), P as PT bf16 terms.
+template <typename T>
+struct OperandK {
+  typedef __bf16 type;
+};
+template <>
+struct OperandK<_Float16> {
+  typedef _Float16 type;
+};
+
+__device__ inline v4f mfma_k(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+__device__ inline v4f mfma_k(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Four code bytes as two pairs of f16: byte u = code + 128 in the low bits of
+// 1024.0 is 1024 + u, and 1024 + u - 1152 is the code, exactly.
+__device__ inline void codes_to_f16(int w, int& lo, int& hi) {
+  const unsigned u = (unsigned)w ^ 0x80808080u;
+  const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
+  const v2h a = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u));
+  const v2h b = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u));
+  lo = __builtin_bit_cast(int, a - off);
+  hi = __builtin_bit_cast(int, b - off);
+}
+template <typename KT>
+__device__ inline void codes_to(v4i w, v4i& first, v4i& second) {
+  int lo, hi;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (__is_same(KT, _Float16)) codes_to_f16(w[i], lo, hi);
+    else codes_to_bf16(w[i], lo, hi);
+    (i < 2 ? first : second)[2 * (i & 1)] = lo;
+    (i < 2 ? first : second)[2 * (i & 1) + 1] = hi;
+  }
+}
+
+// LDS byte of 16-byte chunk c of K row `tok` (DB * 128 bytes).  A tile's 16 rows
+// are tokens 16 (i / 4) + 4 t + i % 4: the swizzle steps through those.
+template <int DB>
+__device__ inline int k_lds(int tok, int c) {
+  const int f = DB == 1 ? ((tok >> 1) & 1) | ((tok >> 4) & 3) << 1 : (tok & 3) | ((tok >> 4) & 3) << 2;
+  return tok * DB * 128 + ((c ^ f) << 4);
+}
+// LDS byte of chunk c (8 tokens) of V row d: 64 tokens, 128 bytes.
+__device__ inline int v_lds(int d, int c) { return d * 128 + ((c ^ ((d >> 1) & 7)) << 4); }
+
+template <typename T, int DB, int NC, int QT, int PT>
+__global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
+  typedef typename OperandK<T>::type KT;
+  typedef KT v8k __attribute__((ext_vector_type(8)));
+  constexpr int DT = DB * 4, kSteps = DB * 2;  // 16-dimension tiles of O; 32-dimension steps of S
+  constexpr int kK = 64 * DB * 128, kV = DB * 64 * 128;  // LDS bytes of a chunk's K and V
+  constexpr int kCols = NC * 16 * 4;
+  extern __shared__ __attribute__((aligned(256))) int8_t lds[];
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // heads are the fastest index: blocks are dealt to the 8 XCDs round-robin, so one
+  // XCD's L2 holds the keys and values of few heads
+  const int head = blockIdx.x % a.c.heads, part = blockIdx.x / a.c.heads, D = a.c.dim, P = a.c.page;
+  const SeqDev s = seq_of(a.b, P, blockIdx.z);
+  if (!s.ok) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    return;
+  }
+  // the last columns see the most tokens: first
+  const int tile = a.col_tiles - 1 - part % a.col_tiles, split = part / a.col_tiles;
+  const int tile0 = tile * kCols;
+  if (tile0 >= s.fresh * a.group) return;
+  const int total = tile_chunks(a, s, tile0, kCols);
+  const int begin = split * a.split_chunks, end = min(begin + a.split_chunks, total);
+  if (a.splits > 1 && begin >= end) return;
+  const int col0 = tile0 + wave * NC * 16;
+  const int pos0 = s.len - s.fresh;
+  // chunks that this wave's own columns see
+  const int wave_end = min(end, tile_chunks(a, s, col0, NC * 16));
+
+  v8k q[NC][kSteps][QT];
+  int limit[NC];
+  const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int col = col0 + c * 16 + n, i = col / a.group;
+    const bool real = i < s.fresh;
+    limit[c] = a.causal ? pos0 + i : s.len - 1;
+    const T* row = static_cast<const T*>(a.q) + (s.first + (int64_t)(real ? i : 0)) * a.ldq +
+                   (int64_t)(head * a.group + col % a.group) * D;
+#pragma unroll
+    for (int b = 0; b < kSteps; ++b) {
+      const int d = b * 32 + g * 8;
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+      if (real && d < D) {
+        if (a.vec) {
+          constexpr int W = 16 / sizeof(T);
+#pragma unroll
+          for (int k = 0; k < 8; k += W) {
+            float u[W];
+            load_reals<T, W>(row + d + k, u);
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[k + j] = u[j];
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = (float)row[d + k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        // the leading bits, cut, as long as a term follows; a row with an infinity
+        // has no softmax: NaN, as for a NaN
+        float rest = finite(x[k]) ? x[k] * sign : __builtin_nanf("");
+#pragma unroll
+        for (int p = 0; p < QT; ++p) {
+          const float cut = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, rest) & 0xFFFF0000u);
+          q[c][b][p][k] = (KT)(p + 1 < QT ? cut : rest);
+          rest -= cut;
+        }
+      }
+    }
+  }
+
+  float m[NC], l[NC];
+  v4f o[NC][DT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m[c] = kNoMax;
+    l[c] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
+  }
+  const int first_limit = a.causal ? pos0 + col0 / a.group : s.len - 1;
+  const int32_t* table = a.b.table + (int64_t)blockIdx.z * a.b.table_ld;
+  const int last_nth = (s.len - 1) >> a.page_log2;
+  // page of a group of 16 tokens; 0 (and nothing is seen of it) where it has none
+  auto page_of = [&](int t) {
+    const int nth = t >> a.page_log2;
+    return nth <= last_nth ? table[nth] : -1;
+  };
+
+  // This thread's share of a chunk: K pieces of 16 dimensions of a token, V pieces
+  // of 16 tokens of a dimension, DB of each (64 tokens x DB * 4 pieces, and DB * 64
+  // dimensions x 4 groups, over 256 threads).
+  v4i kr[DB], vr[DB];
+  auto load = [&](int chunk) {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      const int at = i * 256 + (int)threadIdx.x;
+      const int tok = at / (DB * 4), d = min(at % (DB * 4) * 16, D - 16);
+      const int t = chunk * 64 + tok;
+      int page = page_of(t);
+      page = page < 0 || page >= a.c.pages ? 0 : page;
+      kr[i] = *reinterpret_cast<const v4i*>(a.c.k + k_offset(a.c, page, head, (t & (P - 1))) + d);
+      const int grp = at / (DB * 64), dv = min(at % (DB * 64), D - 1);
+      const int t0 = chunk * 64 + grp * 16;
+      page = page_of(t0);
+      page = page < 0 || page >= a.c.pages ? 0 : page;
+      vr[i] = *reinterpret_cast<const v4i*>(a.c.v + v_offset(a.c, page, head, (t0 & (P - 1)), dv));
+    }
+  };
+  auto store = [&](int buf) {
+    int8_t* to = lds + buf * (kK + kV);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      const int at = i * 256 + (int)threadIdx.x;
+      v4i lo, hi;
+      const int tok = at / (DB * 4), piece = at % (DB * 4);
+      codes_to<KT>(kr[i], lo, hi);
+      if (piece * 16 >= D) lo = hi = v4i{0, 0, 0, 0};  // past the head: 0 times q's 0
+      *reinterpret_cast<v4i*>(to + k_lds<DB>(tok, 2 * piece)) = lo;
+      *reinterpret_cast<v4i*>(to + k_lds<DB>(tok, 2 * piece + 1)) = hi;
+      const int grp = at / (DB * 64), d = at % (DB * 64);
+      codes_to<__bf16>(vr[i], lo, hi);
+      *reinterpret_cast<v4i*>(to + kK + v_lds(d, 2 * grp)) = lo;
+      *reinterpret_cast<v4i*>(to + kK + v_lds(d, 2 * grp + 1)) = hi;
+    }
+  };
+
+  // scales of this lane's 16 tokens of a chunk, and whether its page exists
+  auto scales = [&](int chunk, float& ks, float& vs) {
+    const int t0 = chunk * 64 + g * 16;
+    const int named = page_of(t0);
+    const bool there = named >= 0 && named < a.c.pages;
+    if (!there && t0 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    const int64_t at = (int64_t)(there ? named : 0) * a.c.heads + head;
+    ks = there ? a.c.k_scale[at] : 0.0f;
+    vs = there ? a.c.v_scale[at] : 0.0f;
+    return there;
+  };
+
+  if (begin < end) {
+    load(begin);
+    store(0);
+  }
+  const float to_log2 = a.scale * sign;
+  for (int chunk = begin; chunk < end; ++chunk) {
+    const int buf = (chunk - begin) & 1;
+    __syncthreads();  // this chunk is in LDS, and the other buffer has been read
+    if (chunk + 1 < end) load(chunk + 1);
+    if (chunk < wave_end) {
+      float ks, vs;
+      const bool there = scales(chunk, ks, vs);
+      const int8_t* kb = lds + buf * (kK + kV);
+      const int8_t* vb = kb + kK;
+      float x[NC][16];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v4f sum[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) sum[c] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < kSteps; ++b) {
+          const v8k k = *reinterpret_cast<const v8k*>(kb + k_lds<DB>(16 * (n >> 2) + 4 * t + (n & 3), b * 4 + g));
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int p = 0; p < QT; ++p) sum[c] = mfma_k(k, q[c][b][p], sum[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[c][4 * t + r] = sum[c][r];
+      }
+      const int t0 = chunk * 64 + g * 16;
+      const bool edge = chunk * 64 + 63 > first_limit || __any(!there);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float f = ks * to_log2;  // not negative: the largest product has the largest logit
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[c][i] = t0 + i > limit[c] || !there ? -INFINITY : x[c][i] * f;
+          }
+          f = 1.0f;
+        }
+        float top = x[c][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, x[c][i]);
+        top *= f;
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m[c])) {
+          const float now = fmaxf(m[c], top), down = __builtin_amdgcn_exp2f(m[c] - now);
+          m[c] = now;
+          l[c] *= down;
+#pragma unroll
+          for (int j = 0; j < DT; ++j) o[c][j] *= down;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, -m[c]));
+          l[c] += p;
+          x[c][i] = p * vs;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        v8bf p[NC][PT];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          float rest[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) rest[i] = x[c][8 * u + i];
+#pragma unroll
+          for (int k = 0; k < PT; ++k) {
+            if (k + 1 < PT) {  // the leading bits, cut: the next term has the rest
+              v4i w;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                w[i] = (int)__builtin_amdgcn_perm(__builtin_bit_cast(unsigned, rest[2 * i + 1]),
+                                                  __builtin_bit_cast(unsigned, rest[2 * i]), 0x07060302u);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  float& r = rest[2 * i + e];
+                  r -= __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xFFFF0000u);
+                }
+              }
+              p[c][k] = __builtin_bit_cast(v8bf, w);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) p[c][k][i] = (__bf16)rest[i];
+            }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          const v8bf v = *reinterpret_cast<const v8bf*>(vb + v_lds(j * 16 + n, 2 * g + u));
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int k = 0; k < PT; ++k)
+              o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[c][k], o[c][j], 0, 0, 0);
+        }
+      }
+    }
+    if (chunk + 1 < end) store(buf ^ 1);
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    l[c] += __shfl_xor(l[c], 16);
+    l[c] += __shfl_xor(l[c], 32);
+#pragma unroll
+    for (int j = 0; j < DT; ++j) {
+      const float v[4] = {o[c][j][0], o[c][j][1], o[c][j][2], o[c][j][3]};
+      emit<T>(a, s, head, split, col0 + c * 16 + n, j * 16 + g * 4, m[c], l[c], v);
     }
   }
 }
 
 // Joins the splits of each query row: one block per token and query head.
 template <typename T>
-__global__ __launch_bounds__(64) void k_attention_join(AttnArgs a, int kcols) {
+__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a, int kcols) {
+  constexpr int kMany = 256;  // weights kept at a time
+  __shared__ float weight[kMany], red[4], sums[1024];
   const SeqDev s = seq_of(a.b, a.c.page, blockIdx.z);
   const int i = blockIdx.x, hq = blockIdx.y;
   if (!s.ok || i >= s.fresh) return;
@@ -370,18 +693,45 @@ __global__ __launch_bounds__(64) void k_attention_join(AttnArgs a, int kcols) {
   const int used = (total + a.split_chunks - 1) / a.split_chunks;
   const int64_t row = s.first + (int64_t)i, stride = (int64_t)a.b.tokens * a.q_heads;
   const int64_t r = row * a.q_heads + hq;
-  float mx = kNoMax, sum = 0.0f;
-  for (int p = 0; p < used; ++p) mx = fmaxf(mx, a.part_ml[2 * (p * stride + r)]);
-  for (int p = 0; p < used; ++p)
-    sum += __builtin_amdgcn_exp2f(a.part_ml[2 * (p * stride + r)] - mx) * a.part_ml[2 * (p * stride + r) + 1];
-  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-  T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)hq * a.c.dim;
-  for (int d = threadIdx.x; d < a.c.dim; d += 64) {
-    float v = 0.0f;
-    for (int p = 0; p < used; ++p)
-      v += __builtin_amdgcn_exp2f(a.part_ml[2 * (p * stride + r)] - mx) * a.part_o[(p * stride + r) * a.c.dim + d];
-    out[d] = (T)(v * f);
+  const int tid = threadIdx.x, lane = tid & 63;
+  float mx = kNoMax;
+  for (int p = tid; p < used; p += 256) mx = fmaxf(mx, a.part_ml[2 * (p * stride + r)]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+  if (lane == 0) red[tid >> 6] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  // thread: dimensions 4 x .. of the splits y, y + 256 / (dim / 4), ...
+  const int quads = a.c.dim / 4, ways = 256 / quads, x = tid % quads, y = tid / quads;
+  float sum = 0.0f;
+  v4f v = {0, 0, 0, 0};
+  for (int p0 = 0; p0 < used; p0 += kMany) {
+    const int many = min(kMany, used - p0);
+    __syncthreads();
+    if (tid < many) {
+      const int64_t at = (p0 + tid) * stride + r;
+      const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - mx);
+      weight[tid] = w;
+      sum += w * a.part_ml[2 * at + 1];
+    }
+    __syncthreads();
+    if (y < ways)
+      for (int p = y; p < many; p += ways)
+        v += weight[p] * *reinterpret_cast<const v4f*>(a.part_o + ((p0 + p) * stride + r) * a.c.dim + 4 * x);
   }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  __syncthreads();
+  if (lane == 0) red[tid >> 6] = sum;
+  *reinterpret_cast<v4f*>(sums + 4 * tid) = v;
+  __syncthreads();
+  if (tid >= quads) return;
+  sum = red[0] + red[1] + red[2] + red[3];
+  for (int w = 1; w < ways; ++w) v += *reinterpret_cast<const v4f*>(sums + 4 * (w * quads + x));
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)hq * a.c.dim + 4 * x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) out[k] = (T)(v[k] * f);
 }
 
 struct AttnPlan {
@@ -391,18 +741,20 @@ struct AttnPlan {
   int64_t part, bytes;
 };
 
-AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batch& b, int q_heads) {
+constexpr int64_t kBlocksPerCu = 4, kMinChunks = 16;
+
+AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batch& b, int q_heads, int type) {
   AttnPlan p{};
   const int64_t cols = (int64_t)b.max_new * (q_heads / k.heads);
   p.tok = cols <= 16;
-  p.nc = p.tok || k.dim > 128 ? 1 : 2;
+  p.nc = p.tok || k.dim > 128 || type == FXPQ_F32 ? 1 : 2;
   const int64_t tile = (int64_t)p.nc * 16 * (p.tok ? 1 : 4);
   p.col_tiles = (int)((cols + tile - 1) / tile);
   const int64_t blocks = (int64_t)p.col_tiles * b.seqs * k.heads;
   const int64_t chunks = (b.max_len + 63) / 64;
-  const int64_t want = (4 * (int64_t)c.cus + blocks - 1) / blocks;
+  const int64_t want = (kBlocksPerCu * (int64_t)c.cus + blocks - 1) / blocks;
   int64_t per = (chunks + want - 1) / want;
-  if (per < 4) per = 4;
+  if (per < kMinChunks) per = kMinChunks;
   p.split_chunks = (int)per;
   p.splits = (int)((chunks + per - 1) / per);
   if (p.splits > 1) {
@@ -414,6 +766,18 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
   return p;
 }
 
+template <typename T, int KCOLS>
+hipError_t join_splits(const Ctx& c, const AttnArgs& a) {
+  if (a.splits > 1)
+    k_attention_join<T><<<dim3((unsigned)a.b.max_new, (unsigned)a.q_heads, (unsigned)a.b.seqs), dim3(256), 0,
+                          c.stream>>>(a, KCOLS);
+  return hipGetLastError();
+}
+
+inline hipError_t allow_lds(const void* f, int bytes) {
+  return bytes > 65536 ? hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
+
 template <typename T, int DB, int NC, bool TOK>
 hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   // Digits of q and bf16 terms of P by the type that goes in and out: what they
@@ -422,23 +786,30 @@ hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   constexpr int SP = sizeof(T) == 4 ? 3 : __is_same(T, __bf16) ? 1 : 2;
   constexpr int bytes = TOK ? 4 * NC * 16 * (2 + DB * 64 + 4) * 4 : 0;
   auto* f = k_cache_attention<T, DB, NC, SQ, SP, TOK>;
-  if (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-  }
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
+  if (e != hipSuccess) return e;
   f<<<dim3((unsigned)(a.col_tiles * a.splits), (unsigned)a.c.heads, (unsigned)a.b.seqs), dim3(256), bytes,
       c.stream>>>(a);
-  if (a.splits > 1)
-    k_attention_join<T><<<dim3((unsigned)a.b.max_new, (unsigned)a.q_heads, (unsigned)a.b.seqs), dim3(64), 0,
-                          c.stream>>>(a, NC * 16 * (TOK ? 1 : 4));
-  return hipGetLastError();
+  return join_splits<T, NC * 16 * (TOK ? 1 : 4)>(c, a);
+}
+
+template <typename T, int DB>
+hipError_t run_wide(const Ctx& c, const AttnArgs& a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int NC = F32 ? 1 : 2;
+  constexpr int bytes = 2 * (64 * DB * 128 + DB * 64 * 128);
+  auto* f = k_cache_attention_wide<T, DB, NC, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
+  if (e != hipSuccess) return e;
+  f<<<dim3((unsigned)(a.c.heads * a.col_tiles * a.splits), 1u, (unsigned)a.b.seqs), dim3(256), bytes,
+      c.stream>>>(a);
+  return join_splits<T, NC * 64>(c, a);
 }
 
 template <typename T, int DB>
 hipError_t run_dim(const Ctx& c, const AttnArgs& a, const AttnPlan& p) {
   if (p.tok) return run_attention<T, DB, 1, true>(c, a);
-  if constexpr (DB <= 2) return run_attention<T, DB, 2, false>(c, a);
+  if constexpr (DB <= 2) return run_wide<T, DB>(c, a);
   else return run_attention<T, DB, 1, false>(c, a);
 }
 
@@ -446,13 +817,15 @@ hipError_t run_dim(const Ctx& c, const AttnArgs& a, const AttnPlan& p) {
 
 int64_t cache_attention_workspace(const Ctx& c, const fxpq_kv_cache& cache, const fxpq_kv_batch& b,
                                   int q_heads) {
-  return plan_attention(c, cache, b, q_heads).bytes;
+  const int64_t wide = plan_attention(c, cache, b, q_heads, FXPQ_F32).bytes;
+  const int64_t narrow = plan_attention(c, cache, b, q_heads, FXPQ_BF16).bytes;
+  return wide > narrow ? wide : narrow;  // whatever the type of the call
 }
 
 hipError_t launch_cache_attention(const Ctx& c, const fxpq_kv_cache& cache, const fxpq_kv_batch& b,
                                   const void* q, int64_t ldq, int q_heads, float softmax_scale,
                                   int causal, void* out, int64_t ldo, int type, void* ws) {
-  const AttnPlan p = plan_attention(c, cache, b, q_heads);
+  const AttnPlan p = plan_attention(c, cache, b, q_heads, type);
   AttnArgs a{};
   a.c = cache;
   a.b = b;
@@ -466,6 +839,7 @@ hipError_t launch_cache_attention(const Ctx& c, const fxpq_kv_cache& cache, cons
   a.scale = softmax_scale * 1.44269504088896340736f;
   a.col_tiles = p.col_tiles;
   a.splits = p.splits;
+  while ((1 << a.page_log2) < cache.page) ++a.page_log2;
   a.split_chunks = p.split_chunks;
   const int64_t size = real_bytes(type);
   a.vec = (uintptr_t)q % 16 == 0 && (uintptr_t)out % 16 == 0 && ldq * size % 16 == 0 && ldo * size % 16 == 0;
