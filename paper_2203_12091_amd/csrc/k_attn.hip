@@ -41,6 +41,31 @@ struct AttnArgs {
 
 constexpr float kNoMax = -1e30f;  // running maximum before any token
 
+// What a block works on: part (query tile and split) of a sequence and head.
+// Blocks are dealt to the 8 XCDs round-robin by id, so the heads, which have equal
+// work, are the fastest index; where they are 8, a head's keys come through one
+// XCD's L2.  Query tiles of a sequence run together, for the same reason (4 x 1024
+// new tokens over 4000: 303 us, with the sequences in turn 516).  Splits are dealt
+// across the sequences, each sequence's to another XCD: a late split is one that
+// only long sequences have (64 sequences of up to 8192: 164 us with the splits next
+// to each other, 124 so).
+struct BlockAt {
+  int head, seq, part;
+};
+template <bool SPREAD>
+__device__ inline BlockAt block_at(const AttnArgs& a) {
+  const unsigned i = blockIdx.x, rest = i / (unsigned)a.c.heads, seqs = (unsigned)a.b.seqs;
+  if constexpr (SPREAD) {
+    const unsigned part = rest / seqs;
+    return BlockAt{(int)(i % (unsigned)a.c.heads), (int)((rest + part) % seqs), (int)part};
+  }
+  const unsigned parts = (unsigned)(a.col_tiles * a.splits);
+  return BlockAt{(int)(i % (unsigned)a.c.heads), (int)(rest / parts), (int)(rest % parts)};
+}
+inline dim3 attention_grid(const AttnArgs& a) {
+  return dim3((unsigned)a.c.heads * (unsigned)a.b.seqs * (unsigned)(a.col_tiles * a.splits));
+}
+
 // Chunks that the query columns of one tile see: up to the last column's limit.
 __device__ inline int tile_chunks(const AttnArgs& a, const SeqDev& s, int col0, int cols) {
   const int last = min(col0 + cols, s.fresh * a.group) - 1;
@@ -95,13 +120,15 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
   extern __shared__ float smem[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = blockIdx.y, D = a.c.dim, P = a.c.page;
-  const SeqDev s = seq_of(a.b, P, blockIdx.z);
+  const int D = a.c.dim, P = a.c.page;
+  const BlockAt at = block_at<TOK>(a);
+  const int head = at.head;
+  const SeqDev s = seq_of(a.b, P, at.seq);
   if (!s.ok) {
-    if (blockIdx.x == 0 && head == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    if (at.part == 0 && head == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
     return;
   }
-  const int tile = blockIdx.x % a.col_tiles, split = blockIdx.x / a.col_tiles;
+  const int tile = at.part % a.col_tiles, split = at.part / a.col_tiles;
   constexpr int kCols = NC * 16 * (TOK ? 1 : 4);
   const int tile0 = tile * kCols;
   if (tile0 >= s.fresh * a.group) return;
@@ -190,7 +217,7 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
     for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
   }
   const int first_limit = a.causal ? pos0 + col0 / a.group : s.len - 1;
-  const int32_t* table = a.b.table + (int64_t)blockIdx.z * a.b.table_ld;
+  const int32_t* table = a.b.table + (int64_t)at.seq * a.b.table_ld;
   const int last_nth = (s.len - 1) >> a.page_log2;
   const int stride = TOK ? 4 : 1;
 
@@ -222,8 +249,8 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
     const bool there = named >= 0 && named < a.c.pages;
     if (!there && t0 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
     const int page = there ? named : 0;
-    const int64_t at = (int64_t)page * a.c.heads + head;
-    const float ks = there ? a.c.k_scale[at] : 0.0f, vs = there ? a.c.v_scale[at] : 0.0f;
+    const int64_t sc = (int64_t)page * a.c.heads + head;
+    const float ks = there ? a.c.k_scale[sc] : 0.0f, vs = there ? a.c.v_scale[sc] : 0.0f;
     const int8_t* vbase = a.c.v + v_offset(a.c, page, head, (t0 & (P - 1)), 0);
 #pragma unroll
     for (int j = 0; j < DT; ++j)
@@ -427,12 +454,12 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // heads are the fastest index: blocks are dealt to the 8 XCDs round-robin, so one
-  // XCD's L2 holds the keys and values of few heads
-  const int head = blockIdx.x % a.c.heads, part = blockIdx.x / a.c.heads, D = a.c.dim, P = a.c.page;
-  const SeqDev s = seq_of(a.b, P, blockIdx.z);
+  const int D = a.c.dim, P = a.c.page;
+  const BlockAt where = block_at<false>(a);
+  const int head = where.head, part = where.part;
+  const SeqDev s = seq_of(a.b, P, where.seq);
   if (!s.ok) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    if (part == 0 && head == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
     return;
   }
   // the last columns see the most tokens: first
@@ -503,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
     for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
   }
   const int first_limit = a.causal ? pos0 + col0 / a.group : s.len - 1;
-  const int32_t* table = a.b.table + (int64_t)blockIdx.z * a.b.table_ld;
+  const int32_t* table = a.b.table + (int64_t)where.seq * a.b.table_ld;
   const int last_nth = (s.len - 1) >> a.page_log2;
   // page of a group of 16 tokens; 0 (and nothing is seen of it) where it has none
   auto page_of = [&](int t) {
@@ -741,8 +768,13 @@ struct AttnPlan {
   int64_t part, bytes;
 };
 
-constexpr int64_t kBlocksPerCu = 4, kMinChunks = 16;
-
+// Chunks of a split.  With few columns a block's own cost is small, and what matters
+// is that all CUs are busy at the end of a ragged batch: 32 chunks (2048 tokens),
+// fewer down to 8 where that would leave CUs without a block (one token over
+// 131072: 32 chunks 58.9 us, 16 64.1; over 4096: 8 chunks 13.5 us, 16 17.0).  With
+// many columns a split writes and reads back all of them, and is worth it only
+// where the tiles alone do not fill the CUs (2 x 64 new tokens over 20000: 20 chunks
+// 82 us, 8 106; 4 x 1024 over 4000: whole 303, in three 536).
 AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batch& b, int q_heads, int type) {
   AttnPlan p{};
   const int64_t cols = (int64_t)b.max_new * (q_heads / k.heads);
@@ -752,9 +784,11 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
   p.col_tiles = (int)((cols + tile - 1) / tile);
   const int64_t blocks = (int64_t)p.col_tiles * b.seqs * k.heads;
   const int64_t chunks = (b.max_len + 63) / 64;
-  const int64_t want = (kBlocksPerCu * (int64_t)c.cus + blocks - 1) / blocks;
-  int64_t per = (chunks + want - 1) / want;
-  if (per < kMinChunks) per = kMinChunks;
+  // blocks that the chip holds at a time, by the kernels' registers
+  const int64_t slots = (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
+  int64_t per = (blocks * chunks + slots - 1) / slots;
+  if (p.tok) per = per < 8 ? 8 : per > 32 ? 32 : per;
+  else per = blocks >= slots ? chunks : per < 16 ? 16 : per;
   p.split_chunks = (int)per;
   p.splits = (int)((chunks + per - 1) / per);
   if (p.splits > 1) {
@@ -788,8 +822,7 @@ hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   auto* f = k_cache_attention<T, DB, NC, SQ, SP, TOK>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  f<<<dim3((unsigned)(a.col_tiles * a.splits), (unsigned)a.c.heads, (unsigned)a.b.seqs), dim3(256), bytes,
-      c.stream>>>(a);
+  f<<<attention_grid(a), dim3(256), bytes, c.stream>>>(a);
   return join_splits<T, NC * 16 * (TOK ? 1 : 4)>(c, a);
 }
 
@@ -801,8 +834,7 @@ hipError_t run_wide(const Ctx& c, const AttnArgs& a) {
   auto* f = k_cache_attention_wide<T, DB, NC, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  f<<<dim3((unsigned)(a.c.heads * a.col_tiles * a.splits), 1u, (unsigned)a.b.seqs), dim3(256), bytes,
-      c.stream>>>(a);
+  f<<<attention_grid(a), dim3(256), bytes, c.stream>>>(a);
   return join_splits<T, NC * 64>(c, a);
 }
 
@@ -826,6 +858,8 @@ hipError_t launch_cache_attention(const Ctx& c, const fxpq_kv_cache& cache, cons
                                   const void* q, int64_t ldq, int q_heads, float softmax_scale,
                                   int causal, void* out, int64_t ldo, int type, void* ws) {
   const AttnPlan p = plan_attention(c, cache, b, q_heads, type);
+  // 2^32 threads are a launch's limit
+  if ((int64_t)cache.heads * b.seqs * p.col_tiles * p.splits > 0xFFFFFF) return hipErrorInvalidValue;
   AttnArgs a{};
   a.c = cache;
   a.b = b;
