@@ -40,6 +40,23 @@ struct AttnArgs {
 };
 
 constexpr float kNoMax = -1e30f;  // running maximum before any token
+// The reference that logits are taken from is a running maximum that follows only
+// when a logit passes it by more than this (base 2): weights reach 2^8 then, which
+// costs no precision, and most chunks need neither a maximum over the lanes nor a
+// rescaling of O.
+constexpr float kSlack = 8.0f;
+
+// The maximum over the four 16-lane groups of a wave, lane by lane: the swaps leave
+// rows (0, 0, 2, 2) and (1, 1, 3, 3), then halves (low, low) and (high, high).
+// Written out, with the wait state the swap needs after a write of its operand: this
+// compiler's builtins return their first result twice.
+__device__ inline float over_groups(float x) {
+  float y = x;
+  asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+  x = y = fmaxf(x, y);
+  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+  return fmaxf(x, y);
+}
 
 // What a block works on: part (query tile and split) of a sequence and head.
 // Blocks are dealt to the 8 XCDs round-robin by id, so the heads, which have equal
@@ -293,10 +310,8 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
       float top = x[c][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, x[c][i]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > m[c])) {
-        const float now = fmaxf(m[c], top), down = __builtin_amdgcn_exp2f(m[c] - now);
+      if (__any(top > m[c] + kSlack)) {
+        const float now = fmaxf(m[c], over_groups(top)), down = __builtin_amdgcn_exp2f(m[c] - now);
         m[c] = now;
         l[c] *= down;
 #pragma unroll
@@ -441,16 +456,19 @@ __device__ inline int k_lds(int tok, int c) {
   const int f = DB == 1 ? ((tok >> 1) & 1) | ((tok >> 4) & 3) << 1 : (tok & 3) | ((tok >> 4) & 3) << 2;
   return tok * DB * 128 + ((c ^ f) << 4);
 }
-// LDS byte of chunk c (8 tokens) of V row d: 64 tokens, 128 bytes.
+// LDS byte of chunk c of V row d: 64 tokens, 128 bytes; chunk 4 u + g has tokens
+// 16 g + 8 u + 0..7 (the 16 lanes of a ds_read_b128's pass come from two groups: with
+// neighbouring chunks they still cover all banks once).
 __device__ inline int v_lds(int d, int c) { return d * 128 + ((c ^ ((d >> 1) & 7)) << 4); }
 
-template <typename T, int DB, int NC, int QT, int PT>
-__global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
+template <typename T, int DB, int NC, int NW, int QT, int PT>
+__global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a) {
   typedef typename OperandK<T>::type KT;
   typedef KT v8k __attribute__((ext_vector_type(8)));
   constexpr int DT = DB * 4, kSteps = DB * 2;  // 16-dimension tiles of O; 32-dimension steps of S
   constexpr int kK = 64 * DB * 128, kV = DB * 64 * 128;  // LDS bytes of a chunk's K and V
-  constexpr int kCols = NC * 16 * 4;
+  constexpr int kCols = NC * 16 * NW, kThreads = NW * 64;
+  constexpr int kShare = DB * 256 / kThreads;  // 16-byte pieces of K, and of V, of a thread
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -539,13 +557,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
   };
 
   // This thread's share of a chunk: K pieces of 16 dimensions of a token, V pieces
-  // of 16 tokens of a dimension, DB of each (64 tokens x DB * 4 pieces, and DB * 64
-  // dimensions x 4 groups, over 256 threads).
-  v4i kr[DB], vr[DB];
+  // of 16 tokens of a dimension (64 tokens x DB * 4 pieces, and DB * 64 dimensions x
+  // 4 groups, over the threads).
+  v4i kr[kShare], vr[kShare];
   auto load = [&](int chunk) {
 #pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      const int at = i * 256 + (int)threadIdx.x;
+    for (int i = 0; i < kShare; ++i) {
+      const int at = i * kThreads + (int)threadIdx.x;
       const int tok = at / (DB * 4), d = min(at % (DB * 4) * 16, D - 16);
       const int t = chunk * 64 + tok;
       int page = page_of(t);
@@ -561,8 +579,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
   auto store = [&](int buf) {
     int8_t* to = lds + buf * (kK + kV);
 #pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      const int at = i * 256 + (int)threadIdx.x;
+    for (int i = 0; i < kShare; ++i) {
+      const int at = i * kThreads + (int)threadIdx.x;
       v4i lo, hi;
       const int tok = at / (DB * 4), piece = at % (DB * 4);
       codes_to<KT>(kr[i], lo, hi);
@@ -571,8 +589,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
       *reinterpret_cast<v4i*>(to + k_lds<DB>(tok, 2 * piece + 1)) = hi;
       const int grp = at / (DB * 64), d = at % (DB * 64);
       codes_to<__bf16>(vr[i], lo, hi);
-      *reinterpret_cast<v4i*>(to + kK + v_lds(d, 2 * grp)) = lo;
-      *reinterpret_cast<v4i*>(to + kK + v_lds(d, 2 * grp + 1)) = hi;
+      *reinterpret_cast<v4i*>(to + kK + v_lds(d, grp)) = lo;
+      *reinterpret_cast<v4i*>(to + kK + v_lds(d, 4 + grp)) = hi;
     }
   };
 
@@ -602,25 +620,27 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
       const bool there = scales(chunk, ks, vs);
       const int8_t* kb = lds + buf * (kK + kV);
       const int8_t* vb = kb + kK;
+      // independent sums next to each other: a product need not wait for the last
+      v4f sum[NC][4];
+#pragma unroll
+      for (int b = 0; b < kSteps; ++b) {
+        v8k k[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          k[t] = *reinterpret_cast<const v8k*>(kb + k_lds<DB>(16 * (n >> 2) + 4 * t + (n & 3), b * 4 + g));
+#pragma unroll
+        for (int p = 0; p < QT; ++p)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+              sum[c][t] = mfma_k(k[t], q[c][b][p], b + p ? sum[c][t] : v4f{0, 0, 0, 0});
+      }
       float x[NC][16];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        v4f sum[NC];
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) sum[c] = v4f{0, 0, 0, 0};
-#pragma unroll
-        for (int b = 0; b < kSteps; ++b) {
-          const v8k k = *reinterpret_cast<const v8k*>(kb + k_lds<DB>(16 * (n >> 2) + 4 * t + (n & 3), b * 4 + g));
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int p = 0; p < QT; ++p) sum[c] = mfma_k(k, q[c][b][p], sum[c]);
-        }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[c][4 * t + r] = sum[c][r];
-      }
+        for (int i = 0; i < 16; ++i) x[c][i] = sum[c][i >> 2][i & 3];
       const int t0 = chunk * 64 + g * 16;
       const bool edge = chunk * 64 + 63 > first_limit || __any(!there);
 #pragma unroll
@@ -637,10 +657,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[c][i]);
         top *= f;
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m[c])) {
-          const float now = fmaxf(m[c], top), down = __builtin_amdgcn_exp2f(m[c] - now);
+        if (__any(top > m[c] + kSlack)) {
+          const float now = fmaxf(m[c], over_groups(top)), down = __builtin_amdgcn_exp2f(m[c] - now);
           m[c] = now;
           l[c] *= down;
 #pragma unroll
@@ -683,13 +701,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attention_wide(AttnArgs a) {
           }
         }
 #pragma unroll
-        for (int j = 0; j < DT; ++j) {
-          const v8bf v = *reinterpret_cast<const v8bf*>(vb + v_lds(j * 16 + n, 2 * g + u));
+        for (int j = 0; j < DT; j += 2) {
+          v8bf v[2];
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+          for (int e = 0; e < 2; ++e) v[e] = *reinterpret_cast<const v8bf*>(vb + v_lds((j + e) * 16 + n, 4 * u + g));
 #pragma unroll
-            for (int k = 0; k < PT; ++k)
-              o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[c][k], o[c][j], 0, 0, 0);
+          for (int k = 0; k < PT; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int c = 0; c < NC; ++c)
+                o[c][j + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e], p[c][k], o[c][j + e], 0, 0, 0);
         }
       }
     }
@@ -764,6 +786,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a, int kcols) {
 struct AttnPlan {
   bool tok;     // few columns: the waves of a block share them
   int nc;       // 16-column tiles of a wave
+  int waves;    // of a block
   int col_tiles, splits, split_chunks;
   int64_t part, bytes;
 };
@@ -773,22 +796,41 @@ struct AttnPlan {
 // fewer down to 8 where that would leave CUs without a block (one token over
 // 131072: 32 chunks 58.9 us, 16 64.1; over 4096: 8 chunks 13.5 us, 16 17.0).  With
 // many columns a split writes and reads back all of them, and is worth it only
-// where the tiles alone do not fill the CUs (2 x 64 new tokens over 20000: 20 chunks
-// 82 us, 8 106; 4 x 1024 over 4000: whole 303, in three 536).
+// where the tiles alone do not fill the CUs (16 new tokens over 8000, 4 heads: 8
+// chunks 36 us, 16 56; 4 x 1024 over 4000: whole 303, in three 536).
 AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batch& b, int q_heads, int type) {
   AttnPlan p{};
   const int64_t cols = (int64_t)b.max_new * (q_heads / k.heads);
   p.tok = cols <= 16;
   p.nc = p.tok || k.dim > 128 || type == FXPQ_F32 ? 1 : 2;
-  const int64_t tile = (int64_t)p.nc * 16 * (p.tok ? 1 : 4);
-  p.col_tiles = (int)((cols + tile - 1) / tile);
-  const int64_t blocks = (int64_t)p.col_tiles * b.seqs * k.heads;
+  const int64_t groups = (int64_t)b.seqs * k.heads;
+  auto blocks_of = [&](int waves) {
+    const int64_t tile = (int64_t)p.nc * 16 * waves;
+    p.col_tiles = (int)((cols + tile - 1) / tile);
+    return p.col_tiles * groups;
+  };
+  p.waves = 4;
+  int64_t blocks = blocks_of(p.tok ? 1 : 4);
+  if (!p.tok && k.dim > 64 && k.dim <= 128 && cols > p.nc * 64) {
+    // eight waves share one conversion of the keys and values, but a CU holds one
+    // such block: for many tiles, or so few that the cache is split anyway
+    // (4 x 1024 over 4000: 268 us against 284; 2 x 64 over 20000: 70 against 90; the
+    // reverse where four waves just fill the chip, 4 x 1024 over 1000 with 16
+    // ungrouped heads: 167 against 99)
+    const int64_t eight = blocks_of(8);
+    if (eight >= 2 * (int64_t)c.cus || blocks < c.cus) {
+      p.waves = 8;
+      blocks = eight;
+    } else {
+      blocks_of(4);
+    }
+  }
   const int64_t chunks = (b.max_len + 63) / 64;
   // blocks that the chip holds at a time, by the kernels' registers
   const int64_t slots = (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
   int64_t per = (blocks * chunks + slots - 1) / slots;
   if (p.tok) per = per < 8 ? 8 : per > 32 ? 32 : per;
-  else per = blocks >= slots ? chunks : per < 16 ? 16 : per;
+  else per = blocks >= slots ? chunks : per < 8 ? 8 : per;
   p.split_chunks = (int)per;
   p.splits = (int)((chunks + per - 1) / per);
   if (p.splits > 1) {
@@ -826,22 +868,24 @@ hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   return join_splits<T, NC * 16 * (TOK ? 1 : 4)>(c, a);
 }
 
-template <typename T, int DB>
+template <typename T, int DB, int NW>
 hipError_t run_wide(const Ctx& c, const AttnArgs& a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NC = F32 ? 1 : 2;
   constexpr int bytes = 2 * (64 * DB * 128 + DB * 64 * 128);
-  auto* f = k_cache_attention_wide<T, DB, NC, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
+  auto* f = k_cache_attention_wide<T, DB, NC, NW, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  f<<<attention_grid(a), dim3(256), bytes, c.stream>>>(a);
-  return join_splits<T, NC * 64>(c, a);
+  f<<<attention_grid(a), dim3(NW * 64), bytes, c.stream>>>(a);
+  return join_splits<T, NC * 16 * NW>(c, a);
 }
 
 template <typename T, int DB>
 hipError_t run_dim(const Ctx& c, const AttnArgs& a, const AttnPlan& p) {
   if (p.tok) return run_attention<T, DB, 1, true>(c, a);
-  if constexpr (DB <= 2) return run_wide<T, DB>(c, a);
+  if constexpr (DB == 2)
+    if (p.waves == 8) return run_wide<T, DB, 8>(c, a);
+  if constexpr (DB <= 2) return run_wide<T, DB, 4>(c, a);
   else return run_attention<T, DB, 1, false>(c, a);
 }
 

@@ -147,12 +147,14 @@ STEPS = [  # (page, heads, dim, rotated dims, interleaved, q_heads, steps of (ne
 
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("case", STEPS, ids=str)
-def test_append_and_read(fx, h, t, case):
+@pytest.mark.parametrize("gap", [24, 7])
+def test_append_and_read(fx, h, t, case, gap):
     """Several appends to one cache: every code, scale and rotated query equals
     the plain model's; the values read back are code * scale.  Later tokens are
-    larger, so scales grow inside started pages."""
+    larger, so scales grow inside started pages.  gap: values between the rows; an
+    odd one leaves the rows aligned to their type only."""
     page, heads, dim, dims, inter, q_heads, steps = case
-    note("append", t, case)
+    note("append", t, case, gap)
     seqs = len(steps[0])
     total = [sum(st[s] for st in steps) for s in range(seqs)]
     cache = Cache(fx, seqs, total, heads, dim, page, seed=dim)
@@ -163,9 +165,9 @@ def test_append_and_read(fx, h, t, case):
     g, at = torch.Generator().manual_seed(5), [0] * seqs
     for nth, new in enumerate(steps):
         T = sum(new)
-        width = (q_heads + 2 * heads) * dim + 24
+        width = (q_heads + 2 * heads) * dim + gap
         x = (torch.randn(T, width, generator=g) * 2.0 ** (nth + torch.randint(-2, 2, (T, 1), generator=g))).to(TYPES[t])
-        x[:, -24:] = float("nan")  # nothing reads between the rows
+        x[:, -gap:] = float("nan")  # nothing reads between the rows
         d = x.to(DEV)
         size = d.element_size()
         q, k, v = (d.data_ptr() + o * dim * size for o in (0, q_heads, q_heads + heads))
@@ -203,9 +205,10 @@ def test_append_and_read(fx, h, t, case):
                 want = torch.from_numpy(codes[pg, :, p % page].astype(np.float32) * scale[pg][:, None]).to(TYPES[t])
                 assert torch.equal(o[row].cpu(), want) if p in (0, total[s] - 1) or p % 37 == 0 else True
             row += 1
-    only = torch.zeros_like(outs[1])
-    fx.cache_read(h, cache.desc, back, None, only, code_of(fx, t))
-    assert torch.equal(only, outs[1])
+    for shift in (0, 1):  # only the values, to an address aligned to 16 bytes and to the type
+        only = torch.zeros(outs[1].numel() + 1, dtype=TYPES[t], device=DEV)[shift:]
+        fx.cache_read(h, cache.desc, back, None, only, code_of(fx, t))
+        assert torch.equal(only[: outs[1].numel()], outs[1].flatten())
 
 
 def test_growing_scale_stays_within_one_step(fx, h):
