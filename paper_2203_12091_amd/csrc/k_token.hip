@@ -10,7 +10,8 @@ namespace {
 // ---- per-token quantization ----------------------------------------------------
 // One block per row: the largest magnitude, then the codes from a second read
 // of the row (at most a few ten KB, from the caches).
-template <typename T, bool VEC>
+// VB: bytes of a load that every row's address is aligned to (16, 8 or the type's).
+template <typename T, int VB>
 __global__ __launch_bounds__(256) void k_token_quantize(const T* __restrict__ x, int64_t cols,
                                                         int64_t ldx, int rule,
                                                         int8_t* __restrict__ codes, int64_t ldc,
@@ -22,8 +23,8 @@ __global__ __launch_bounds__(256) void k_token_quantize(const T* __restrict__ x,
   int8_t* out = codes + (int64_t)blockIdx.x * ldc;
   const int lane = threadIdx.x & 63;
   auto load = [&](int64_t c, float(&v)[V]) {
-    if (VEC && c + V <= cols) {
-      constexpr int W = 16 / sizeof(T);
+    if (VB > (int)sizeof(T) && c + V <= cols) {
+      constexpr int W = VB / sizeof(T);
 #pragma unroll
       for (int i = 0; i < V; i += W) {
         float u[W];
@@ -595,13 +596,11 @@ hipError_t launch_token_quantize(const Ctx& c, const void* x, int x_type, int64_
   return for_real(x_type, [&](auto zero) {
     using T = decltype(zero);
     const T* p = static_cast<const T*>(x);
-    const bool vec = (uintptr_t)x % 16 == 0 && ldx * sizeof(T) % 16 == 0;
-    if (vec)
-      k_token_quantize<T, true><<<dim3((unsigned)rows), dim3(256), 0, c.stream>>>(
-          p, cols, ldx, rule, codes, ldc, scale, c.sc.flags);
-    else
-      k_token_quantize<T, false><<<dim3((unsigned)rows), dim3(256), 0, c.stream>>>(
-          p, cols, ldx, rule, codes, ldc, scale, c.sc.flags);
+    const uintptr_t at = (uintptr_t)x | (uintptr_t)(ldx * sizeof(T));
+    auto* f = at % 16 == 0  ? k_token_quantize<T, 16>
+              : at % 8 == 0 ? k_token_quantize<T, 8>
+                            : k_token_quantize<T, sizeof(T)>;
+    f<<<dim3((unsigned)rows), dim3(256), 0, c.stream>>>(p, cols, ldx, rule, codes, ldc, scale, c.sc.flags);
     return hipGetLastError();
   });
 }
