@@ -550,7 +550,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
   const int first_limit = a.causal ? pos0 + col0 / a.group : s.len - 1;
   const int32_t* table = a.b.table + (int64_t)where.seq * a.b.table_ld;
   const int last_nth = (s.len - 1) >> a.page_log2;
-  // page of a group of 16 tokens; 0 (and nothing is seen of it) where it has none
+  // page of a token's group of 16; past the sequence's end -1 (nothing is seen of it)
   auto page_of = [&](int t) {
     const int nth = t >> a.page_log2;
     return nth <= last_nth ? table[nth] : -1;
@@ -559,22 +559,36 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
   // This thread's share of a chunk: K pieces of 16 dimensions of a token, V pieces
   // of 16 tokens of a dimension (64 tokens x DB * 4 pieces, and DB * 64 dimensions x
   // 4 groups, over the threads).
+  // A chunk's pages are looked up two chunks ahead and its codes and scales loaded
+  // one ahead, so that neither of the two latencies is waited for.
   v4i kr[kShare], vr[kShare];
-  auto load = [&](int chunk) {
+  int k_page[kShare], v_page[kShare], s_page;  // of the chunk to load next
+  float next_ks = 0.0f, next_vs = 0.0f;        // of this lane's 16 tokens, 0 without a page
+  bool next_there = false;
+  auto lookup = [&](int chunk) {
 #pragma unroll
     for (int i = 0; i < kShare; ++i) {
       const int at = i * kThreads + (int)threadIdx.x;
-      const int tok = at / (DB * 4), d = min(at % (DB * 4) * 16, D - 16);
-      const int t = chunk * 64 + tok;
-      int page = page_of(t);
-      page = page < 0 || page >= a.c.pages ? 0 : page;
-      kr[i] = *reinterpret_cast<const v4i*>(a.c.k + k_offset(a.c, page, head, (t & (P - 1))) + d);
-      const int grp = at / (DB * 64), dv = min(at % (DB * 64), D - 1);
-      const int t0 = chunk * 64 + grp * 16;
-      page = page_of(t0);
-      page = page < 0 || page >= a.c.pages ? 0 : page;
-      vr[i] = *reinterpret_cast<const v4i*>(a.c.v + v_offset(a.c, page, head, (t0 & (P - 1)), dv));
+      k_page[i] = page_of(chunk * 64 + at / (DB * 4));
+      v_page[i] = page_of(chunk * 64 + at / (DB * 64) * 16);
     }
+    s_page = page_of(chunk * 64 + g * 16);
+  };
+  auto load = [&](int chunk) {
+    auto valid = [&](int page) { return page < 0 || page >= a.c.pages ? 0 : page; };
+#pragma unroll
+    for (int i = 0; i < kShare; ++i) {
+      const int at = i * kThreads + (int)threadIdx.x;
+      const int t = chunk * 64 + at / (DB * 4), d = min(at % (DB * 4) * 16, D - 16);
+      kr[i] = *reinterpret_cast<const v4i*>(a.c.k + k_offset(a.c, valid(k_page[i]), head, (t & (P - 1))) + d);
+      const int t0 = chunk * 64 + at / (DB * 64) * 16, dv = min(at % (DB * 64), D - 1);
+      vr[i] = *reinterpret_cast<const v4i*>(a.c.v + v_offset(a.c, valid(v_page[i]), head, (t0 & (P - 1)), dv));
+    }
+    next_there = s_page >= 0 && s_page < a.c.pages;
+    if (!next_there && chunk * 64 + g * 16 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    const int64_t at = (int64_t)valid(s_page) * a.c.heads + head;
+    next_ks = a.c.k_scale[at];
+    next_vs = a.c.v_scale[at];
   };
   auto store = [&](int buf) {
     int8_t* to = lds + buf * (kK + kV);
@@ -594,30 +608,23 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
     }
   };
 
-  // scales of this lane's 16 tokens of a chunk, and whether its page exists
-  auto scales = [&](int chunk, float& ks, float& vs) {
-    const int t0 = chunk * 64 + g * 16;
-    const int named = page_of(t0);
-    const bool there = named >= 0 && named < a.c.pages;
-    if (!there && t0 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
-    const int64_t at = (int64_t)(there ? named : 0) * a.c.heads + head;
-    ks = there ? a.c.k_scale[at] : 0.0f;
-    vs = there ? a.c.v_scale[at] : 0.0f;
-    return there;
-  };
-
   if (begin < end) {
+    lookup(begin);
     load(begin);
+    lookup(begin + 1);
     store(0);
   }
   const float to_log2 = a.scale * sign;
   for (int chunk = begin; chunk < end; ++chunk) {
     const int buf = (chunk - begin) & 1;
     __syncthreads();  // this chunk is in LDS, and the other buffer has been read
-    if (chunk + 1 < end) load(chunk + 1);
+    const bool there = next_there;
+    const float ks = there ? next_ks : 0.0f, vs = there ? next_vs : 0.0f;
+    if (chunk + 1 < end) {
+      load(chunk + 1);
+      lookup(chunk + 2);
+    }
     if (chunk < wave_end) {
-      float ks, vs;
-      const bool there = scales(chunk, ks, vs);
       const int8_t* kb = lds + buf * (kK + kV);
       const int8_t* vb = kb + kK;
       // independent sums next to each other: a product need not wait for the last
@@ -830,7 +837,7 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
   const int64_t slots = (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
   int64_t per = (blocks * chunks + slots - 1) / slots;
   if (p.tok) per = per < 8 ? 8 : per > 32 ? 32 : per;
-  else per = blocks >= slots ? chunks : per < 8 ? 8 : per;
+  else per = blocks >= slots ? chunks : per < 2 * p.waves ? 2 * p.waves : per;
   p.split_chunks = (int)per;
   p.splits = (int)((chunks + per - 1) / per);
   if (p.splits > 1) {
