@@ -238,18 +238,26 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
   const int last_nth = (s.len - 1) >> a.page_log2;
   const int stride = TOK ? 4 : 1;
 
-  // page of a group of 16 tokens, 0 where it has none (then nothing is seen of it)
+  // page of a token's group of 16; past the sequence's end -1 (nothing is seen of it)
   auto page_of = [&](int t) {
     const int nth = t >> a.page_log2;
     return nth <= last_nth ? table[nth] : -1;
   };
+  // Page numbers are looked up two of this wave's chunks ahead, keys and scales
+  // loaded one ahead, values at the chunk's start: no latency is waited for twice.
   const int kg = n >> 2;  // group of the K rows that this lane loads
   v4i kr[4][DB], vr[DT];
-  auto load_k = [&](int chunk) {
-    const int t0 = chunk * 64 + kg * 16;
-    int page = page_of(t0);
-    page = page < 0 || page >= a.c.pages ? 0 : page;
-    const int8_t* base = a.c.k + k_offset(a.c, page, head, (t0 & (P - 1)) + (n & 3));
+  int k_page, s_page;  // of the chunk to load next: of the K rows, of this lane's 16 tokens
+  int next_page = 0;
+  bool next_there = false;
+  float next_ks = 0.0f, next_vs = 0.0f;
+  auto lookup = [&](int chunk) {
+    k_page = page_of(chunk * 64 + kg * 16);
+    s_page = page_of(chunk * 64 + g * 16);
+  };
+  auto load = [&](int chunk) {
+    const int page = k_page < 0 || k_page >= a.c.pages ? 0 : k_page;
+    const int8_t* base = a.c.k + k_offset(a.c, page, head, ((chunk * 64 + kg * 16) & (P - 1)) + (n & 3));
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -257,18 +265,24 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
         const int d = min(b * 64 + g * 16, D - 16);  // past the head: any bytes, q's digits are 0
         kr[t][b] = *reinterpret_cast<const v4i*>(base + t * 4 * D + d);
       }
+    next_there = s_page >= 0 && s_page < a.c.pages;
+    if (!next_there && chunk * 64 + g * 16 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
+    next_page = next_there ? s_page : 0;
+    const int64_t sc = (int64_t)next_page * a.c.heads + head;
+    next_ks = a.c.k_scale[sc];
+    next_vs = a.c.v_scale[sc];
   };
   int chunk = begin + (TOK ? wave : 0);
-  if (chunk < end) load_k(chunk);
+  if (chunk < end) {
+    lookup(chunk);
+    load(chunk);
+    lookup(chunk + stride);
+  }
   for (; chunk < end; chunk += stride) {
     const int t0 = chunk * 64 + g * 16;  // this lane's 16 tokens
-    const int named = page_of(t0);
-    const bool there = named >= 0 && named < a.c.pages;
-    if (!there && t0 < s.len) raise_flag(a.flags, FXPQ_FLAG_RANGE);
-    const int page = there ? named : 0;
-    const int64_t sc = (int64_t)page * a.c.heads + head;
-    const float ks = there ? a.c.k_scale[sc] : 0.0f, vs = there ? a.c.v_scale[sc] : 0.0f;
-    const int8_t* vbase = a.c.v + v_offset(a.c, page, head, (t0 & (P - 1)), 0);
+    const bool there = next_there;
+    const float ks = there ? next_ks : 0.0f, vs = there ? next_vs : 0.0f;
+    const int8_t* vbase = a.c.v + v_offset(a.c, next_page, head, (t0 & (P - 1)), 0);
 #pragma unroll
     for (int j = 0; j < DT; ++j)
       vr[j] = *reinterpret_cast<const v4i*>(vbase + min(j * 16, D - 16) * 16 + n * 16);
@@ -298,7 +312,10 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
         }
       }
     }
-    if (chunk + stride < end) load_k(chunk + stride);
+    if (chunk + stride < end) {
+      load(chunk + stride);
+      lookup(chunk + 2 * stride);
+    }
     const bool edge = chunk * 64 + 63 > first_limit || __any(!there);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
