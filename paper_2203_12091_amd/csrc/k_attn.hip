@@ -851,10 +851,12 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
   }
   const int64_t chunks = (b.max_len + 63) / 64;
   // blocks that the chip holds at a time, by the kernels' registers
-  const int64_t slots = (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
+  // (eight waves: one, and a quarter more for those that end early)
+  const int64_t slots = p.waves == 8 ? (int64_t)c.cus * 5 / 4
+                                     : (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
   int64_t per = (blocks * chunks + slots - 1) / slots;
   if (p.tok) per = per < 8 ? 8 : per > 32 ? 32 : per;
-  else per = blocks >= slots ? chunks : per < 2 * p.waves ? 2 * p.waves : per;
+  else per = blocks >= slots ? chunks : per < 8 ? 8 : per;
   p.split_chunks = (int)per;
   p.splits = (int)((chunks + per - 1) / per);
   if (p.splits > 1) {
