@@ -641,7 +641,8 @@ fxpq_status fxpq_expert_gemm(fxpq_handle h, int64_t rows, int64_t N, int64_t K, 
  *     k        int8 [pages][heads][page][dim]
  *     v        int8 [pages][heads][page / 16][dim][16]   (16 tokens side by side)
  *     k_scale, v_scale   float [pages][heads]
- * k and v are 16-byte aligned.  The memory needs no initialization.
+ * k and v are 16-byte aligned; scales are not negative.  The memory needs no
+ * initialization.
  */
 typedef struct {
   int8_t* k;
@@ -660,6 +661,8 @@ typedef struct {
  * tokens of any sequence.  A sequence whose numbers contradict these bounds
  * (or max_len pages that the table has) is skipped; a page outside the cache
  * is not touched, and its tokens are not seen.  Both raise FXPQ_FLAG_RANGE.
+ * max_len <= 2^30, max_new <= 2^24 (and so that max_new * q_heads / heads stays
+ * below 2^30).
  */
 typedef struct {
   const int32_t* start;  /* [seqs + 1] */

@@ -151,12 +151,13 @@ bool batch_ok(const fxpq_kv_batch* b, const fxpq_kv_cache* c) {
   return b && b->start && b->length && b->table && aligned(b->start, 4) && aligned(b->length, 4) &&
          aligned(b->table, 4) && b->seqs >= 1 && b->seqs <= 65535 && b->table_ld >= 1 && b->tokens >= 0 &&
          b->max_new >= 0 && b->max_new <= b->tokens && (b->max_new > 0 || b->tokens == 0) &&
-         b->max_len >= b->max_new && b->max_len <= INT32_MAX - 256 &&
+         b->max_new <= (1 << 24) && b->max_len >= b->max_new && b->max_len <= (1 << 30) &&
          (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
 }
 
-bool heads_ok(int q_heads, const fxpq_kv_cache* c) {
-  return q_heads >= 1 && q_heads <= kMaxHeads && q_heads % c->heads == 0;
+bool heads_ok(int q_heads, const fxpq_kv_cache* c, const fxpq_kv_batch* b) {
+  return q_heads >= 1 && q_heads <= kMaxHeads && q_heads % c->heads == 0 &&
+         (int64_t)b->max_new * (q_heads / c->heads) < (1 << 30);
 }
 
 }  // namespace
@@ -1024,7 +1025,7 @@ fxpq_status fxpq_cache_attention_workspace(fxpq_handle h, const fxpq_kv_cache* c
                                            int64_t* bytes) {
   if (!bytes) return FXPQ_ERR_INVALID_ARG;
   *bytes = 0;
-  if (!h || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache))
+  if (!h || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache, batch))
     return FXPQ_ERR_INVALID_ARG;
   if (batch->tokens > 0) *bytes = cache_attention_workspace(ctx(h), *cache, *batch, q_heads);
   return FXPQ_OK;
@@ -1035,7 +1036,7 @@ fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
                                  int32_t q_heads, float softmax_scale, int32_t causal, void* out,
                                  int64_t ldo, fxpq_dtype type, void* workspace,
                                  int64_t workspace_bytes) {
-  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache))
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache, batch))
     return FXPQ_ERR_INVALID_ARG;
   const int64_t width = (int64_t)q_heads * cache->dim;
   if (ldq < width || ldo < width || !isfinite(softmax_scale)) return FXPQ_ERR_INVALID_ARG;

@@ -876,10 +876,6 @@ hipError_t join_splits(const Ctx& c, const AttnArgs& a) {
   return hipGetLastError();
 }
 
-inline hipError_t allow_lds(const void* f, int bytes) {
-  return bytes > 65536 ? hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
-}
-
 template <typename T, int DB, int NC, bool TOK>
 hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   // Digits of q and bf16 terms of P by the type that goes in and out: what they
@@ -928,8 +924,7 @@ hipError_t launch_cache_attention(const Ctx& c, const fxpq_kv_cache& cache, cons
                                   const void* q, int64_t ldq, int q_heads, float softmax_scale,
                                   int causal, void* out, int64_t ldo, int type, void* ws) {
   const AttnPlan p = plan_attention(c, cache, b, q_heads, type);
-  // 2^32 threads are a launch's limit
-  if ((int64_t)cache.heads * b.seqs * p.col_tiles * p.splits > 0xFFFFFF) return hipErrorInvalidValue;
+  if ((int64_t)cache.heads * b.seqs * p.col_tiles * p.splits * (p.waves / 4) > kMaxBlocks) return hipErrorInvalidValue;
   AttnArgs a{};
   a.c = cache;
   a.b = b;

@@ -595,6 +595,7 @@ hipError_t launch_cache_append(const Ctx& c, const fxpq_kv_cache& cache, const f
       constexpr int LP = decltype(lanes)::value, U = 256 / LP;
       const bool fit = append_units_fit(a, sizeof(T)), few = !fit || b.max_new <= kFewTokens;
       const int heads = few ? U : U * 16 / cache.page;  // of a block
+      if (((int64_t)cache.heads / heads + 1) * 2 * a.segs + b.max_new > kMaxBlocks) return hipErrorInvalidValue;
       a.head_blocks = (cache.heads + heads - 1) / heads;
       a.kv_blocks = 2 * a.segs * a.head_blocks;
       const int q_tokens = fit ? kQueryTokens : 1, q_blocks = q ? (b.max_new + q_tokens - 1) / q_tokens : 0;
@@ -618,6 +619,7 @@ hipError_t launch_cache_read(const Ctx& c, const fxpq_kv_cache& cache, const fxp
       return for_lanes(cache.dim, [&](auto lanes) {
         constexpr int LP = decltype(lanes)::value, U = 256 / LP;
         const int head_blocks = (cache.heads + U - 1) / U;
+        if ((int64_t)head_blocks * 2 * blocks > kMaxBlocks) return hipErrorInvalidValue;
         k_read_units<T, LP><<<dim3(2u * blocks * (unsigned)head_blocks, (unsigned)b.seqs), dim3(256), 0, c.stream>>>(
             cache, b, static_cast<T*>(k_out), static_cast<T*>(v_out), log2_of(cache.page), head_blocks, c.sc.flags);
         return hipGetLastError();

@@ -527,9 +527,7 @@ hipError_t run_tile(const Ctx& c, const GemmArgs& g, int shares = 1) {
   if (tiles_m * tiles_n * WR * WC * 64 > 0xFFFFFFFF) return hipErrorInvalidValue;
   constexpr int bytes = NS * (BM + BN) * KS;
   auto* f = k_gemm_tile<BM, BN, WR, WC, KS, NS, GROUP, T>;
-  // more than 64 KB of LDS has to be asked for
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f),
-                                     hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
   f<<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(WR * WC * 64), bytes, c.stream>>>(g);
   return hipGetLastError();

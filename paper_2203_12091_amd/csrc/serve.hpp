@@ -69,6 +69,14 @@ __device__ inline unsigned pack4(int a, int b, int c, int d) {
          (unsigned)(d & 0xFF) << 24;
 }
 
+// Blocks of one launch: 2^32 threads are a grid's limit.
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;
+
+// More than 64 KB of LDS has to be asked for.
+inline hipError_t allow_lds(const void* f, int bytes) {
+  return bytes > 65536 ? hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
+
 // ---- launchers -------------------------------------------------------------
 struct GemmArgs {
   int64_t M, N, K;

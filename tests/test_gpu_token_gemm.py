@@ -195,6 +195,21 @@ def test_token_gemm_deepest_sum(fx, h):
     assert (y.cpu() == float(16384 * k)).all()
 
 
+@pytest.mark.parametrize("m", [3, 70])
+def test_nonfinite_token_gives_a_nan_row(fx, h, m):
+    """A token with a NaN or an infinity makes its own output row NaN, no other."""
+    x = torch.randn(m, 64, generator=gen(1))
+    x[1, 5], x[2, 9] = float("inf"), float("nan")
+    codes, scale = torch.empty(m, 64, dtype=torch.int8, device=DEV), torch.empty(m, device=DEV)
+    fx.token_quantize(h, x.to(DEV), fx.F32, m, 64, 64, fx.SCALE_DFX, codes, 64, scale)
+    y, one = torch.zeros(m, 20, device=DEV), torch.ones(20, device=DEV)
+    b = torch.ones(20, 64, dtype=torch.int8, device=DEV)
+    fx.token_gemm(h, m, 20, 64, codes, 64, scale, b, one, None, y, fx.F32, 20)
+    assert fx.sync_status(h) == fx.FLAG_NONFINITE
+    bad = torch.isnan(y.cpu())
+    assert bad[1:3].all() and bad.sum() == 40
+
+
 def test_token_gemm_on_another_stream(fx, h):
     """Inputs made on one stream, the product on the handle's: ordered by an event."""
     side = torch.cuda.Stream()
