@@ -39,12 +39,20 @@ struct AttnArgs {
   unsigned* flags;
 };
 
-constexpr float kNoMax = -1e30f;  // running maximum before any token
+constexpr float kNoMax = -3.40282347e38f;  // running maximum before any token: below every finite logit
 // The reference that logits are taken from is a running maximum that follows only
 // when a logit passes it by more than this (base 2): weights reach 2^8 then, which
 // costs no precision, and most chunks need neither a maximum over the lanes nor a
 // rescaling of O.
 constexpr float kSlack = 8.0f;
+
+// A logit, rounded by itself: a multiply-add with the running maximum would leave
+// the product's rounding error, which exceeds any slack where logits pass 2^31.
+__device__ inline float scaled(float x, float f) {
+#pragma clang fp contract(off)
+  return x * f;
+}
+constexpr float kFar = 0x1p24f;  // references up to this leave an error below 1
 
 // The maximum over the four 16-lane groups of a wave, lane by lane: the swaps leave
 // rows (0, 0, 2, 2) and (1, 1, 3, 3), then halves (low, low) and (high, high).
@@ -308,7 +316,7 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
           else if constexpr (SPLIT_Q == 2) v = (float)(acc[1][r] * 256 + acc[0][r]);
           else if constexpr (SPLIT_Q == 3) v = fmaf((float)(acc[2][r] * 256 + acc[1][r]), 256.0f, (float)acc[0][r]);
           else v = fmaf((float)(acc[3][r] * 256 + acc[2][r]), 65536.0f, (float)(acc[1][r] * 256 + acc[0][r]));
-          x[c][t * 4 + r] = v * f;
+          x[c][t * 4 + r] = scaled(v, f);
         }
       }
     }
@@ -556,11 +564,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
   }
 
   float m[NC], l[NC];
+  bool far[NC];  // the reference is too large for the fused form (same in all lanes)
   v4f o[NC][DT];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m[c] = kNoMax;
     l[c] = 0.0f;
+    far[c] = false;
 #pragma unroll
     for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
   }
@@ -673,7 +683,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
         if (edge) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            x[c][i] = t0 + i > limit[c] || !there ? -INFINITY : x[c][i] * f;
+            x[c][i] = t0 + i > limit[c] || !there ? -INFINITY : scaled(x[c][i], f);
           }
           f = 1.0f;
         }
@@ -687,6 +697,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
           l[c] *= down;
 #pragma unroll
           for (int j = 0; j < DT; ++j) o[c][j] *= down;
+          far[c] = __any(fabsf(now) > kFar);
+        }
+        if (far[c]) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[c][i] = scaled(x[c][i], f);
+          f = 1.0f;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {

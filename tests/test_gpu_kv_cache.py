@@ -418,6 +418,27 @@ def test_attention_extremes(fx, h, new):
     assert fx.sync_status(h) == 0
 
 
+@pytest.mark.parametrize("new", [1, 30])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_attention_of_hugely_negative_logits(fx, h, new, t):
+    """Equal keys give equal logits, here near -2^110: every weight is exactly 1
+    before the division, so what is left is the sum's and the result's rounding."""
+    lens = [3000]
+    cache = Cache(fx, 1, lens, 1, 64, 16)
+    v, vs = fill(cache, lens, 21)[1::2]
+    cache.k.fill_(100)
+    cache.ks.fill_(2.0 ** -6)
+    q = torch.full((new, 4 * 64), -(2.0 ** 104)).to(TYPES[t])
+    got = run_attention(fx, h, cache, [new], lens, q, 4, 1.0, 0, t)
+    assert fx.sync_status(h) == 0
+    pages = cache.table[0]
+    V = (v[pages, 0].astype(np.float64) * vs[pages, 0][:, None, None]).reshape(-1, 64)[: lens[0]]
+    want = V.mean(0)
+    # bf16: P (the page's scale, which may be no power of two) is rounded as well
+    tol = ((lens[0] + 64) * 2.0 ** -23 + (2.0 ** -8 if t == "bf16" else 2.0 ** -22)) * np.abs(V).max() + HALF_ULP[t] * np.abs(want) * 1.01
+    assert (np.abs(got - want) <= tol).all()
+
+
 def test_attention_page_outside_the_cache(fx, h):
     """Its tokens are not seen, and the flag is raised."""
     lens = [100]
