@@ -56,6 +56,8 @@ class Cache:
         """Room for new[i] more tokens of sequence seqs[i]; the batch that describes them."""
         if len(seqs) > self.max_seqs:
             raise ValueError(f"{len(seqs)} sequences: at most {self.max_seqs}")
+        if len(set(seqs)) != len(seqs) or min(new, default=0) < 0:
+            raise ValueError("a sequence is named twice, or is to shrink")
         need = [-(-(self.length.get(s, 0) + n) // self.page) for s, n in zip(seqs, new)]
         more = sum(m - len(self.owned.get(s, ())) for s, m in zip(seqs, need))
         if more > len(self.free) or max(need, default=0) > self.max_pages:
