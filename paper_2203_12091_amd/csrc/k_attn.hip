@@ -895,9 +895,11 @@ hipError_t join_splits(const Ctx& c, const AttnArgs& a) {
 template <typename T, int DB, int NC, bool TOK>
 hipError_t run_attention(const Ctx& c, const AttnArgs& a) {
   // Digits of q and bf16 terms of P by the type that goes in and out: what they
-  // drop stays below that type's own rounding.
+  // drop stays far below that type's own rounding.  (bf16 by one term of P: 116.8
+  // against 117.6 us for 64 tokens over up to 8192, and the whole result's relative
+  // error 0.0021 in the place of 0.0017, which is that of its own rounding.)
   constexpr int SQ = sizeof(T) == 4 ? 4 : 3;
-  constexpr int SP = sizeof(T) == 4 ? 3 : __is_same(T, __bf16) ? 1 : 2;
+  constexpr int SP = sizeof(T) == 4 ? 3 : 2;
   constexpr int bytes = TOK ? 4 * NC * 16 * (2 + DB * 64 + 4) * 4 : 0;
   auto* f = k_cache_attention<T, DB, NC, SQ, SP, TOK>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
@@ -910,6 +912,8 @@ template <typename T, int DB, int NW>
 hipError_t run_wide(const Ctx& c, const AttnArgs& a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NC = F32 ? 1 : 2;
+  // bf16 takes one term of P here, where the matrix products count: an error of the
+  // size of the result's own rounding
   constexpr int bytes = 2 * (64 * DB * 128 + DB * 64 * 128);
   auto* f = k_cache_attention_wide<T, DB, NC, NW, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
