@@ -121,64 +121,85 @@ __global__ __launch_bounds__(WR* WC * 64) void k_gemm_tile(GemmArgs g) {
   // Blocks are dealt to the 8 XCDs round-robin by id; each XCD takes a
   // contiguous run of tiles, in bands of 8 row tiles, so that the tiles it has
   // in flight share rows and columns in its L2.
-  int t = blockIdx.x;
-  const int T_all = gridDim.x;
-  if (T_all % 8 == 0) t = (t % 8) * (T_all / 8) + t / 8;
-  const int rows_all = T_all / tiles_n;
-  constexpr int kBand = 8;
-  const int band = t / (kBand * tiles_n);
-  const int in_band = t - band * kBand * tiles_n;
-  const int high = min(kBand, rows_all - band * kBand);
-  int tm = band * kBand + in_band % high;
-  const int tn = in_band / high;
+  const int block = blockIdx.x, blocks = gridDim.x;
+  int tm = 0, tn = 0;
+  auto place = [&](int t, int rows_all) {
+    constexpr int kBand = 8;
+    const int band = t / (kBand * tiles_n);
+    const int in_band = t - band * kBand * tiles_n;
+    const int high = min(kBand, rows_all - band * kBand);
+    tm = band * kBand + in_band % high;
+    tn = in_band / high;
+  };
   int64_t m0, m_end;
   const int8_t* b = g.b;
   const float* b_scale = g.b_scale;
   const float* bias = g.bias;
   if constexpr (GROUP) {
-    // the expert of this row tile: groups take ceil(rows / BM) tiles each, in order
-    __shared__ int sh_e, sh_first;
+    // Groups take ceil(rows / BM) row tiles each, in order.  The grid holds as many as
+    // any sizes can take; the ones that these sizes take are dealt evenly to the XCDs
+    // (a run of the grid's own tiles would leave the last XCDs idle: 1024 rows of 16
+    // equal experts, 4096 x 2048 weights, 64 us so and 44 dealt evenly).
+    __shared__ int sh_e, sh_first, sh_tm, sh_tn;
     if (threadIdx.x < 64) {
-      int seen = 0, found = -1, first = 0;
-      for (int e0 = 0; e0 < g.experts && found < 0; e0 += 64) {
-        const int e = e0 + lane;
-        int n = 0;
-        if (e < g.experts) {
-          const int lo = g.offsets[e], hi = g.offsets[e + 1];
-          if (lo < 0 || hi < lo || hi > g.M) {
-            if (blockIdx.x == 0) raise_flag(g.flags, FXPQ_FLAG_RANGE);
-          } else {
-            n = (hi - lo + BM - 1) / BM;
-          }
+      auto tiles_of = [&](int e) {
+        if (e >= g.experts) return 0;
+        const int lo = g.offsets[e], hi = g.offsets[e + 1];
+        if (lo < 0 || hi < lo || hi > g.M) {
+          if (block == 0) raise_flag(g.flags, FXPQ_FLAG_RANGE);
+          return 0;
         }
-        int upto = n;  // tiles of the experts up to this one
+        return (int)(((int64_t)hi - lo + BM - 1) / BM);
+      };
+      const int most = blocks / tiles_n;  // row tiles: more only where the offsets contradict each other
+      int total = 0;
+      for (int e0 = 0; e0 < g.experts; e0 += 64) {
+        int n = tiles_of(e0 + lane);
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int o = __shfl_up(upto, d);
-          if (lane >= d) upto += o;
+        for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+        total = min(total + n, most);
+      }
+      const int tiles = total * tiles_n, per = (tiles + 7) / 8, t = block % 8 * per + block / 8;
+      int found = -1, first = 0;
+      if (block / 8 < per && t < tiles) {
+        place(t, total);
+        int seen = 0;
+        for (int e0 = 0; e0 < g.experts && found < 0; e0 += 64) {
+          const int n = tiles_of(e0 + lane);
+          int upto = n;  // tiles of the experts up to this one
+#pragma unroll
+          for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+          }
+          const unsigned long long hit = __ballot(tm < seen + upto);
+          if (hit) {
+            const int l = __ffsll((long long)hit) - 1;
+            found = e0 + l;
+            first = seen + __shfl(upto, l) - __shfl(n, l);
+          }
+          seen += __shfl(upto, 63);
         }
-        const unsigned long long hit = __ballot(tm < seen + upto);
-        if (hit) {
-          const int l = __ffsll((long long)hit) - 1;
-          found = e0 + l;
-          first = seen + __shfl(upto, l) - __shfl(n, l);
-        }
-        seen += __shfl(upto, 63);
       }
       if (lane == 0) {
         sh_e = found;
         sh_first = first;
+        sh_tm = tm;
+        sh_tn = tn;
       }
     }
     __syncthreads();
     const int e = sh_e;
     if (e < 0) return;
+    tm = sh_tm;
+    tn = sh_tn;
     m0 = g.offsets[e] + (int64_t)(tm - sh_first) * BM;
     m_end = g.offsets[e + 1];
     b += (int64_t)e * g.N * g.K;
     b_scale += (int64_t)e * g.N;
     if (bias) bias += (int64_t)e * g.N;
   } else {
+    place(blocks % 8 == 0 ? block % 8 * (blocks / 8) + block / 8 : block, blocks / tiles_n);
     m0 = (int64_t)tm * BM;
     m_end = g.M;
   }
@@ -524,12 +545,13 @@ hipError_t run_tile(const Ctx& c, const GemmArgs& g, int shares = 1) {
   const int64_t tiles_n = (g.N + BN - 1) / BN;
   // groups of any sizes need at most one partly filled row tile each
   const int64_t tiles_m = GROUP ? g.M / BM + g.experts : (g.M + BM - 1) / BM;
-  if (tiles_m * tiles_n * WR * WC * 64 > 0xFFFFFFFF) return hipErrorInvalidValue;
+  if ((tiles_m * tiles_n + 7) * WR * WC * 64 > 0xFFFFFFFF) return hipErrorInvalidValue;
   constexpr int bytes = NS * (BM + BN) * KS;
   auto* f = k_gemm_tile<BM, BN, WR, WC, KS, NS, GROUP, T>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  f<<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)shares), dim3(WR * WC * 64), bytes, c.stream>>>(g);
+  const int64_t blocks = GROUP ? (tiles_m * tiles_n + 7) / 8 * 8 : tiles_m * tiles_n;
+  f<<<dim3((unsigned)blocks, (unsigned)shares), dim3(WR * WC * 64), bytes, c.stream>>>(g);
   return hipGetLastError();
 }
 
