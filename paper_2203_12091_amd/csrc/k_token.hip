@@ -607,7 +607,7 @@ bool few_rows(int64_t M, int64_t N) { return M <= kFewRows && N <= 16 * kCus; }
 // at least 2048 deep (64 x 4096 x 9216: 20.2 us whole, 13.4 in four; 64 x 1000 x
 // 2048: 7.2 whole, 8.4 in two).
 int depth_shares(int64_t M, int64_t N, int64_t K) {
-  if (few_rows(M, N)) return 1;
+  if (M == 0 || few_rows(M, N)) return 1;
   const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
   int64_t shares = kCus / tiles;
   if (shares > K / 2048) shares = K / 2048;

@@ -199,3 +199,18 @@ def test_serving_calls_reject_bad_arguments_without_a_device():
     for m, k, want in ((1, 24, bad), (-1, 16, bad), (1, 131072, fx.ERR_OVERFLOW)):
         assert L.fxpq_token_gemm_workspace(m, 8, k, p(n)) == want and n.value == 0
     assert L.fxpq_token_gemm_workspace(1, 8, 16, None) == bad
+
+
+@pytest.mark.parametrize("n", [1, 4096, 4097, 5000, 2 ** 31 - 1])
+@pytest.mark.parametrize("k", [16, 64, 9216])
+def test_products_of_no_rows_need_no_work_space(n, k):
+    """The query answers for M = 0, which the product accepts, at any width."""
+    import ctypes as C
+    import os
+
+    from paper_2203_12091_amd import fxpq as fx
+    if not os.path.exists(fx.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    need = C.c_int64(-1)
+    assert fx.lib().fxpq_token_gemm_workspace(0, n, k, C.byref(need)) == fx.OK and need.value == 0

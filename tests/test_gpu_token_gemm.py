@@ -336,3 +336,14 @@ def test_products_reject_bad_calls(fx, h):
         with pytest.raises(fx.FxpqError):
             group(**kw)
     assert fx.sync_status(h) == 0
+
+
+def test_products_of_no_rows_of_a_wide_layer(fx, h):
+    """M = 0 is accepted at a width that more than one block column takes, and
+    writes nothing."""
+    b, f = torch.zeros(5000, 64, dtype=torch.int8, device=DEV), torch.zeros(5000, device=DEV)
+    y = torch.full((4, 5000), 9.0, device=DEV)
+    need = fx.token_gemm_workspace(0, 5000, 64)
+    assert need == 0
+    fx.token_gemm(h, 0, 5000, 64, None, 64, None, b, f, None, y, fx.F32, 5000, None, need)
+    assert fx.sync_status(h) == 0 and (y == 9.0).all()
