@@ -29,7 +29,9 @@ def _up16(n):
 
 
 def quantize_rows(h, x, rule=fx.SCALE_MAX):
-    """int8 codes [rows][cols up to a multiple of 16] and a scale for each row."""
+    """int8 codes [rows][cols up to a multiple of 16] and a scale for each row.  From
+    here on the handle works on torch's current stream, where x was made."""
+    fx.set_stream(h, torch.cuda.current_stream(x.device))
     rows, cols = x.shape
     codes = torch.empty(rows, _up16(cols), dtype=torch.int8, device=x.device)
     scale = torch.empty(rows, device=x.device)
@@ -164,8 +166,8 @@ class Layer:
         return (y[place].view(x.shape[0], self.top, -1).float() * weight[..., None]).sum(1).to(self.dtype)
 
     def forward(self, x, cache, batch):
-        """x: the batch's new tokens, [tokens][hidden]."""
-        fx.set_stream(self.h, torch.cuda.current_stream(x.device))
+        """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's
+        current stream (quantize_rows, the first call of each half, says so)."""
         x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
         return x + self.mix(self._norm(x, self.norm[1]))
 

@@ -1,0 +1,68 @@
+"""The decoder layer's host side, without a device: the library is replaced by one
+that records its calls, torch's streams by a name."""
+import types
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+STREAM = "the current stream"
+
+
+class Recorder:
+    """Stands for the library's binding: every call is noted and does nothing; work
+    spaces are wanted by every product."""
+
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def Handle(self, device):
+        return types.SimpleNamespace(value=None, device=device, close=lambda: None)
+
+    def token_gemm_workspace(self, *args):
+        return 4096
+
+    def cache_attention_workspace(self, *args):
+        return 8192
+
+    def kv_cache(self, k, v, k_scale, v_scale, pages, page, heads, dim):
+        return types.SimpleNamespace(pages=pages, page=page, heads=heads, dim=dim)
+
+    def kv_batch(self, start, length, table, seqs, table_ld, tokens, max_new, max_len):
+        return types.SimpleNamespace(seqs=seqs, tokens=tokens, max_new=max_new, max_len=max_len)
+
+    def rotary(self, cos, sin, positions, dims, interleaved=0):
+        return types.SimpleNamespace(positions=positions, dims=dims)
+
+    def __getattr__(self, name):
+        what = getattr(self.real, name)
+        return (lambda *args: self.calls.append((name, args))) if callable(what) else what
+
+    def names(self):
+        return [n for n, _ in self.calls]
+
+
+@pytest.fixture
+def dec(monkeypatch):
+    from paper_2203_12091_amd import decoder
+    monkeypatch.setattr(decoder, "fx", Recorder(decoder.fx))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: STREAM)
+    return decoder
+
+
+def make(dec, **kw):
+    layer = dec.Layer(64, 4, 2, 16, experts=4, top=2, inner=48, dtype=torch.float32, device="cpu", **kw)
+    cache = dec.Cache(pages=8, page=16, heads=2, dim=16, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    return layer, cache
+
+
+def test_quantization_runs_on_the_stream_of_its_values(dec):
+    """What torch computed on its current stream is quantized on that stream: the
+    weights of a new layer, and rows given to the helper."""
+    layer, _ = make(dec)
+    names = dec.fx.names()
+    assert "token_quantize" in names and names.index("set_stream") < names.index("token_quantize")
+    dec.fx.calls.clear()
+    dec.quantize_rows(layer.h, torch.zeros(2, 64))
+    assert dec.fx.names() == ["set_stream", "token_quantize"]
+    assert dec.fx.calls[0][1] == (layer.h, STREAM)

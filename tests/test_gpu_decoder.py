@@ -214,3 +214,24 @@ def test_products_of_no_rows_need_no_work_space(n, k):
         __graft_entry__.build()
     need = C.c_int64(-1)
     assert fx.lib().fxpq_token_gemm_workspace(0, n, k, C.byref(need)) == fx.OK and need.value == 0
+
+
+@pytest.mark.gpu
+def test_layer_of_another_stream(dec):
+    """A layer made and run inside another stream gives what one made and run on the
+    default stream gives."""
+    x = torch.randn(40, 256, device=DEV)
+    layer, cache = make(dec, torch.float32)
+    want = [layer.forward(x, cache, cache.extend([0, 1], [30, 10])), layer.forward(x[:2], cache, cache.extend([0, 1], [1, 1]))]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other, pages = make(dec, torch.float32)
+        got = [other.forward(x, pages, pages.extend([0, 1], [30, 10])), other.forward(x[:2], pages, pages.extend([0, 1], [1, 1]))]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for a, b in zip((layer.qkv, layer.out, layer.up, layer.down), (other.qkv, other.out, other.up, other.down)):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    layer.h.close()
+    other.h.close()
