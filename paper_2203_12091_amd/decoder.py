@@ -99,12 +99,11 @@ class Layer:
         self.norm = [torch.ones(hidden, device=device) for _ in range(2)]
         ang = torch.arange(positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, dim, 2) / dim)
         self.rotary = fx.rotary(ang.cos().float().to(device), ang.sin().float().to(device), positions, dim)
-        self._work = None
 
     def _workspace(self, need):
-        if need and (self._work is None or self._work.numel() < need):
-            self._work = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._work
+        # one for each call: the allocator hands memory on in the order of the current
+        # stream, so calls on different streams never share one that is in use
+        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
 
     def _linear(self, x, weight):
         codes, scale = quantize_rows(self.h, x)

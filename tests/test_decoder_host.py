@@ -66,3 +66,16 @@ def test_quantization_runs_on_the_stream_of_its_values(dec):
     dec.quantize_rows(layer.h, torch.zeros(2, 64))
     assert dec.fx.names() == ["set_stream", "token_quantize"]
     assert dec.fx.calls[0][1] == (layer.h, STREAM)
+
+
+def test_each_call_has_a_work_space_of_its_own(dec):
+    """Calls in flight on two streams must not share one: two products' work spaces,
+    both still held here, are different memory of the size asked for."""
+    layer, _ = make(dec)
+    dec.fx.calls.clear()
+    for _ in range(2):
+        layer._linear(torch.zeros(3, 64), layer.qkv)
+    spaces = [args[-2] for name, args in dec.fx.calls if name == "token_gemm"]
+    assert [s.numel() for s in spaces] == [4096, 4096]
+    assert spaces[0].data_ptr() != spaces[1].data_ptr()
+    assert layer._workspace(0) is None
