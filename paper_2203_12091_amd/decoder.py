@@ -162,7 +162,7 @@ class Layer:
         y = (torch.nn.functional.silu(y[:, : self.inner]) * y[:, self.inner:]).to(self.dtype)
         codes, scale = quantize_rows(self.h, y)
         y = self._grouped(codes, scale, None, offsets, self.down, self.hidden)
-        return (y[place].view(x.shape[0], self.top, -1).float() * weight[..., None]).sum(1).to(self.dtype)
+        return (y[place].view(x.shape[0], self.top, self.hidden).float() * weight[..., None]).sum(1).to(self.dtype)
 
     def forward(self, x, cache, batch):
         """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's

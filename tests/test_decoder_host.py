@@ -79,3 +79,12 @@ def test_each_call_has_a_work_space_of_its_own(dec):
     assert [s.numel() for s in spaces] == [4096, 4096]
     assert spaces[0].data_ptr() != spaces[1].data_ptr()
     assert layer._workspace(0) is None
+
+
+def test_step_without_new_tokens(dec):
+    """Cache.extend accepts one; the layer answers with no rows."""
+    layer, cache = make(dec)
+    for new in ([0, 0], [5, 0]):
+        y = layer.forward(torch.zeros(sum(new), 64), cache, cache.extend([0, 1], new))
+        assert y.shape == (sum(new), 64) and y.dtype == torch.float32
+    assert cache.length == {0: 5, 1: 0}

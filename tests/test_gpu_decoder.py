@@ -235,3 +235,20 @@ def test_layer_of_another_stream(dec):
     assert all(torch.equal(a, b) for a, b in zip(want, got))
     layer.h.close()
     other.h.close()
+
+
+@pytest.mark.gpu
+def test_step_without_tokens_of_a_wide_layer(dec):
+    """No new tokens, in a layer whose projection has 4608 channels, between steps
+    that have some: no rows come back and the cache stays as it was."""
+    from paper_2203_12091_amd import fxpq as fx
+    layer = dec.Layer(64, 64, 4, 64, experts=4, top=2, inner=48, dtype=torch.bfloat16)
+    cache = dec.Cache(pages=4, page=16, heads=4, dim=64, max_pages_per_seq=2, max_seqs=2)
+    x = torch.randn(6, 64, device=DEV).bfloat16()
+    layer.forward(x, cache, cache.extend([0, 1], [4, 2]))
+    kept = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    y = layer.forward(x[:0], cache, cache.extend([0, 1], [0, 0]))
+    assert y.shape == (0, 64) and all(torch.equal(a, b) for a, b in zip(kept, (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+    y = layer.forward(x[:1], cache, cache.extend([0, 1], [0, 1]))
+    assert y.shape == (1, 64) and torch.isfinite(y).all() and fx.sync_status(layer.h) == 0
+    layer.h.close()
