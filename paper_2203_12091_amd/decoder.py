@@ -33,9 +33,12 @@ def quantize_rows(h, x, rule=fx.SCALE_MAX):
     here on the handle works on torch's current stream, where x was made."""
     fx.set_stream(h, torch.cuda.current_stream(x.device))
     rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1 or rows > 1 and x.stride(0) < cols:
+        x = x.contiguous()  # the library takes rows of neighbouring values
     codes = torch.empty(rows, _up16(cols), dtype=torch.int8, device=x.device)
     scale = torch.empty(rows, device=x.device)
-    fx.token_quantize(h, x, TYPES[x.dtype], rows, cols, x.stride(0), rule, codes, codes.shape[1], scale)
+    fx.token_quantize(h, x, TYPES[x.dtype], rows, cols, max(x.stride(0), cols), rule, codes,
+                      codes.shape[1], scale)
     return codes, scale
 
 

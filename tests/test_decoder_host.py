@@ -88,3 +88,17 @@ def test_step_without_new_tokens(dec):
         y = layer.forward(torch.zeros(sum(new), 64), cache, cache.extend([0, 1], new))
         assert y.shape == (sum(new), 64) and y.dtype == torch.float32
     assert cache.length == {0: 5, 1: 0}
+
+
+def test_rows_of_any_strides_are_quantized_as_they_read(dec):
+    """The library takes rows of neighbouring values: what it is given has the
+    tensor's values at the row stride that is named."""
+    base = torch.arange(24 * 12, dtype=torch.float32).view(24, 12)
+    for x in (base, base[:, ::2], base[:, 3:9], base.t(), base[:1].expand(5, 12), base[0].expand(1, 12), base[3:4, 2:5],
+              base[::5], base[:0]):
+        dec.fx.calls.clear()
+        dec.quantize_rows(None, x)
+        _, given, _, rows, cols, ldx, _, codes, ldc, scale = dec.fx.calls[-1][1]
+        assert (rows, cols) == x.shape and ldx >= cols and ldc == codes.shape[1] >= cols and scale.numel() == rows
+        got = torch.as_strided(given, (rows, cols), (ldx, 1)) if rows else given
+        assert torch.equal(got, x)
