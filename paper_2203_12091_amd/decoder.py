@@ -59,13 +59,13 @@ class Cache:
 
     def extend(self, seqs, new):
         """Room for new[i] more tokens of sequence seqs[i]; the batch that describes them."""
-        if len(seqs) > self.max_seqs:
-            raise ValueError(f"{len(seqs)} sequences: at most {self.max_seqs}")
-        if len(set(seqs)) != len(seqs) or min(new, default=0) < 0:
+        if not 0 < len(seqs) <= self.max_seqs or len(new) != len(seqs):
+            raise ValueError(f"{len(seqs)} sequences, {len(new)} counts: one to {self.max_seqs} sequences, a count for each")
+        if len(set(seqs)) != len(seqs) or min(new) < 0:
             raise ValueError("a sequence is named twice, or is to shrink")
         need = [-(-(self.length.get(s, 0) + n) // self.page) for s, n in zip(seqs, new)]
         more = sum(m - len(self.owned.get(s, ())) for s, m in zip(seqs, need))
-        if more > len(self.free) or max(need, default=0) > self.max_pages:
+        if more > len(self.free) or max(need) > self.max_pages:
             raise MemoryError(f"{more} pages wanted, {len(self.free)} free; at most {self.max_pages} a sequence")
         table = torch.zeros(len(seqs), self.max_pages, dtype=torch.int32)
         for i, (s, n, m) in enumerate(zip(seqs, new, need)):

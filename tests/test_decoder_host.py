@@ -102,3 +102,13 @@ def test_rows_of_any_strides_are_quantized_as_they_read(dec):
         assert (rows, cols) == x.shape and ldx >= cols and ldc == codes.shape[1] >= cols and scale.numel() == rows
         got = torch.as_strided(given, (rows, cols), (ldx, 1)) if rows else given
         assert torch.equal(got, x)
+
+
+def test_cache_refuses_lists_that_do_not_match(dec):
+    """A count for each sequence, and one sequence at least: the device reads as many
+    starts and lengths as there are sequences."""
+    _, cache = make(dec)
+    for seqs, new in (([0, 1], [5]), ([0], [5, 6]), ([], [])):
+        with pytest.raises(ValueError):
+            cache.extend(seqs, new)
+    assert cache.length == {} and cache.owned == {} and len(cache.free) == 8
