@@ -170,6 +170,10 @@ class Layer:
     def forward(self, x, cache, batch):
         """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's
         current stream (quantize_rows, the first call of each half, says so)."""
+        if x.shape != (batch.tokens, self.hidden):
+            raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
+        if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
+            raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
         x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
         return x + self.mix(self._norm(x, self.norm[1]))
 

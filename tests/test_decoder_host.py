@@ -112,3 +112,18 @@ def test_cache_refuses_lists_that_do_not_match(dec):
         with pytest.raises(ValueError):
             cache.extend(seqs, new)
     assert cache.length == {} and cache.owned == {} and len(cache.free) == 8
+
+
+def test_layer_refuses_what_does_not_fit_the_batch(dec):
+    """The kernels take the number of rows, heads and dimensions from the batch and
+    the cache: none may go past x or the layer's own.  Nothing is launched."""
+    layer, cache = make(dec)
+    other = dec.Cache(pages=8, page=16, heads=4, dim=16, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    wide = dec.Cache(pages=8, page=16, heads=2, dim=32, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    dec.fx.calls.clear()
+    for x, c in ((torch.zeros(4, 64), cache), (torch.zeros(6, 64), cache), (torch.zeros(5, 48), cache),
+                 (torch.zeros(5), cache), (torch.zeros(5, 64), other), (torch.zeros(5, 64), wide)):
+        with pytest.raises(ValueError):
+            layer.forward(x, c, c.extend([0], [5]))
+        c.release(0)
+    assert dec.fx.calls == []
