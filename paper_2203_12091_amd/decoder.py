@@ -174,6 +174,8 @@ class Layer:
             raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
         if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
             raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
+        if batch.max_len > self.rotary.positions:
+            raise ValueError(f"a sequence of {batch.max_len} tokens: at most {self.rotary.positions}")
         x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
         return x + self.mix(self._norm(x, self.norm[1]))
 

@@ -127,3 +127,14 @@ def test_layer_refuses_what_does_not_fit_the_batch(dec):
             layer.forward(x, c, c.extend([0], [5]))
         c.release(0)
     assert dec.fx.calls == []
+
+
+def test_layer_refuses_sequences_past_its_positions(dec):
+    """The append would skip such a sequence, and the attention run over slots that
+    were never written.  The last position is still fine."""
+    layer, cache = make(dec, positions=20)
+    layer.forward(torch.zeros(24, 64), cache, cache.extend([0, 1], [20, 4]))
+    dec.fx.calls.clear()
+    with pytest.raises(ValueError):
+        layer.forward(torch.zeros(2, 64), cache, cache.extend([0, 1], [1, 1]))
+    assert dec.fx.calls == []
