@@ -76,8 +76,24 @@ class Cache:
         length = [self.length[s] for s in seqs]
         start = torch.tensor([0] + list(new)).cumsum(0).to(torch.int32)
         put = lambda t: t.to(self.device)  # noqa: E731
-        return fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(seqs),
-                           self.max_pages, sum(new), max(new), max(length))
+        batch = fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(seqs),
+                            self.max_pages, sum(new), max(new), max(length))
+        batch.grown = dict(zip(seqs, new))
+        return batch
+
+    def retract(self, batch):
+        """Takes back the newest batch of its sequences, whose tokens were not computed:
+        their lengths, and the pages that only those tokens needed."""
+        for s, n in batch.grown.items():
+            if s not in self.length:
+                continue
+            self.length[s] -= n
+            pages = self.owned[s]
+            while len(pages) > -(-self.length[s] // self.page):
+                self.free.append(pages.pop())
+            if not self.length[s]:
+                self.release(s)
+        batch.grown = {}
 
     def release(self, seq):
         self.free += self.owned.pop(seq, [])
@@ -169,15 +185,20 @@ class Layer:
 
     def forward(self, x, cache, batch):
         """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's
-        current stream (quantize_rows, the first call of each half, says so)."""
-        if x.shape != (batch.tokens, self.hidden):
-            raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
-        if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
-            raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
-        if batch.max_len > self.rotary.positions:
-            raise ValueError(f"a sequence of {batch.max_len} tokens: at most {self.rotary.positions}")
-        x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
-        return x + self.mix(self._norm(x, self.norm[1]))
+        current stream (quantize_rows, the first call of each half, says so).  Where it
+        raises, the cache's lengths and pages are those from before the batch."""
+        try:
+            if x.shape != (batch.tokens, self.hidden):
+                raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
+            if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
+                raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
+            if batch.max_len > self.rotary.positions:
+                raise ValueError(f"a sequence of {batch.max_len} tokens: at most {self.rotary.positions}")
+            x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
+            return x + self.mix(self._norm(x, self.norm[1]))
+        except Exception:
+            cache.retract(batch)
+            raise
 
 
 def main(prompt=512, steps=16, seqs=8):

@@ -138,3 +138,30 @@ def test_layer_refuses_sequences_past_its_positions(dec):
     with pytest.raises(ValueError):
         layer.forward(torch.zeros(2, 64), cache, cache.extend([0, 1], [1, 1]))
     assert dec.fx.calls == []
+
+
+def test_failed_forward_takes_back_the_batch(dec, monkeypatch):
+    """Lengths and pages are what they were before the extend whose tokens did not
+    get through, whether they were refused or a call failed on the way."""
+    layer, cache = make(dec, positions=40)
+    layer.forward(torch.zeros(22, 64), cache, cache.extend([0, 1], [20, 2]))
+
+    def state():
+        return dict(cache.length), {s: list(p) for s, p in cache.owned.items()}, sorted(cache.free)
+
+    before = state()
+    with pytest.raises(ValueError):  # a new sequence, a page more, too many tokens
+        layer.forward(torch.zeros(39, 64), cache, cache.extend([0, 2, 1], [21, 17, 1]))
+    assert state() == before
+
+    def fails(*args):
+        raise dec.fx.real.FxpqError("fxpq_cache_attention", 5)
+
+    monkeypatch.setattr(dec.fx, "cache_attention", fails, raising=False)
+    with pytest.raises(dec.fx.real.FxpqError):
+        layer.forward(torch.zeros(14, 64), cache, cache.extend([1], [14]))
+    assert state() == before
+    batch = cache.extend([1], [3])
+    cache.release(1)
+    cache.retract(batch)  # a sequence that is gone stays gone
+    assert 1 not in cache.length and len(cache.free) == 6
