@@ -37,6 +37,11 @@ __device__ inline float rotate_second(float x1, float x2, float c, float s) {
   return a + b;
 }
 
+// A new token lies past the rotation's positions.
+__device__ inline bool past_positions(const AppendArgs& a, const SeqDev& q) {
+  return a.rot.dims && q.fresh > 0 && q.len > a.rot.positions;
+}
+
 // Dimension d of a row after the rotation of position pos.
 template <typename T>
 __device__ inline float rotated(const T* row, int d, const fxpq_rotary& r, int pos) {
@@ -274,7 +279,7 @@ __global__ __launch_bounds__(256) void k_append_few(AppendArgs a) {
   constexpr int U = 256 / LP;
   const int D = a.c.dim, P = a.c.page;
   const SeqDev q = seq_of(a.b, P, blockIdx.y);
-  if (!q.ok || (a.rot.dims && q.len > a.rot.positions)) {
+  if (!q.ok || past_positions(a, q)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
     return;
   }
@@ -361,7 +366,7 @@ __global__ __launch_bounds__(256) void k_append_few(AppendArgs a) {
 template <typename T>
 __global__ __launch_bounds__(256) void k_rotate_queries(AppendArgs a) {
   const SeqDev q = seq_of(a.b, a.c.page, blockIdx.y);
-  if (!q.ok || (a.rot.dims && q.len > a.rot.positions)) return;
+  if (!q.ok || past_positions(a, q)) return;
   rotate_queries<T>(a, q, (int)blockIdx.x * kQueryTokens);
 }
 
@@ -372,7 +377,7 @@ __global__ __launch_bounds__(256) void k_append_units(AppendArgs a) {
   __shared__ float tops[U];
   const int D = a.c.dim, P = a.c.page;
   const SeqDev q = seq_of(a.b, P, blockIdx.y);
-  if (!q.ok || (a.rot.dims && q.len > a.rot.positions)) {
+  if (!q.ok || past_positions(a, q)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
     return;
   }

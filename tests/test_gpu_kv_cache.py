@@ -509,3 +509,26 @@ def test_cache_calls_reject_bad_arguments(fx, h):
     with pytest.raises(fx.FxpqError):  # the work space is missing
         fx.cache_attention(h, long.desc, b, x, 512, 8, 1.0, 1, x, 512, fx.F32)
     assert fx.sync_status(h) == 0
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [3, 40], ids=str)
+@pytest.mark.parametrize("gap", [8, 1])
+def test_append_beside_a_long_sequence_without_new_tokens(fx, h, t, new, gap):
+    """A sequence that is longer than the rotation has positions, but appends
+    nothing, has no token that needs one: no flag, and its pages stay as they are."""
+    note("append beside", t, new, gap)
+    cos, sin = tables(40, 32)
+    rot = fx.rotary(torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV), 40, 32)
+    cache = Cache(fx, 2, [64, 64], 1, 32, 16)
+    model = Model(cache)
+    x = torch.randn(new, 32 + gap, generator=torch.Generator().manual_seed(13)).to(TYPES[t])
+    d, ld = x.to(DEV), 32 + gap
+    q = torch.zeros(new, ld, dtype=TYPES[t], device=DEV)
+    fx.cache_append(h, cache.desc, cache.batch([0, new], [64, new]), rot, d, ld, d, ld, d, ld, q, ld, 1, code_of(fx, t))
+    assert fx.sync_status(h) == 0
+    rows = x[:, :32].float().view(new, 1, 32).numpy()
+    turned = np.stack([rotate(rows[i], i, cos, sin, 32, 0) for i in range(new)])
+    model.append(1, 0, turned, rows)
+    model.check(cache)
+    assert torch.equal(q[:, :32].cpu(), torch.from_numpy(turned[:, 0]).to(TYPES[t]))
