@@ -995,7 +995,7 @@ fxpq_status fxpq_cache_append(fxpq_handle h, const fxpq_kv_cache* cache,
   const int64_t width = (int64_t)cache->heads * cache->dim;
   if (ldk < width || ldv < width) return FXPQ_ERR_INVALID_ARG;
   if (rot && (rot->dims < 0 || rot->dims % 2 != 0 || rot->dims > cache->dim || rot->positions < 0 ||
-              (rot->dims > 0 && (!rot->cos || !rot->sin))))
+              (rot->dims > 0 && (!rot->cos || !rot->sin || !aligned(rot->cos, 4) || !aligned(rot->sin, 4)))))
     return FXPQ_ERR_INVALID_ARG;
   if (q) {
     if (q_heads < 1 || q_heads > kMaxHeads || !q_out || ldq < (int64_t)q_heads * cache->dim ||

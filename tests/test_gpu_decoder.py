@@ -252,3 +252,24 @@ def test_step_without_tokens_of_a_wide_layer(dec):
     y = layer.forward(x[:1], cache, cache.extend([0, 1], [0, 1]))
     assert y.shape == (1, 64) and torch.isfinite(y).all() and fx.sync_status(layer.h) == 0
     layer.h.close()
+
+
+def test_rotation_tables_are_checked_for_alignment():
+    """cos and sin are floats; checked before any device call (the handle's memory is
+    never looked at: the batch has no tokens)."""
+    import ctypes as C
+    import os
+
+    from paper_2203_12091_amd import fxpq as fx
+    if not os.path.exists(fx.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    at = 1 << 20  # stands for device addresses, none of which is read
+    cache = fx.KvCache(k=at, v=at, k_scale=at, v_scale=at, pages=1, page=16, heads=1, dim=32)
+    batch = fx.KvBatch(start=at, length=at, table=at, seqs=1, table_ld=1, tokens=0, max_new=0, max_len=16)
+    handle = C.create_string_buffer(1 << 16)
+    p = C.byref
+    for shift, want in ((0, fx.OK), (4, fx.OK), (2, fx.ERR_INVALID_ARG), (1, fx.ERR_INVALID_ARG)):
+        for rot in (fx.Rotary(cos=at + shift, sin=at, positions=16, dims=32), fx.Rotary(cos=at, sin=at + shift, positions=16, dims=32)):
+            assert fx.lib().fxpq_cache_append(p(handle), p(cache), p(batch), p(rot), None, 32, None, 32, None, 0, None, 0, 0,
+                                              fx.F32) == want, shift
