@@ -912,10 +912,10 @@ template <typename T, int DB, int NW>
 hipError_t run_wide(const Ctx& c, const AttnArgs& a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NC = F32 ? 1 : 2;
-  // bf16 takes one term of P here, where the matrix products count: an error of the
-  // size of the result's own rounding
+  // terms of P as with few columns, so that a sequence's prompt and its single tokens
+  // have the same accuracy
   constexpr int bytes = 2 * (64 * DB * 128 + DB * 64 * 128);
-  auto* f = k_cache_attention_wide<T, DB, NC, NW, F32 ? 3 : 1, F32 ? 3 : __is_same(T, __bf16) ? 1 : 2>;
+  auto* f = k_cache_attention_wide<T, DB, NC, NW, F32 ? 3 : 1, F32 ? 3 : 2>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
   f<<<attention_grid(a), dim3(NW * 64), bytes, c.stream>>>(a);

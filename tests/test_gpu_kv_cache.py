@@ -532,3 +532,49 @@ def test_append_beside_a_long_sequence_without_new_tokens(fx, h, t, new, gap):
     model.append(1, 0, turned, rows)
     model.check(cache)
     assert torch.equal(q[:, :32].cpu(), torch.from_numpy(turned[:, 0]).to(TYPES[t]))
+
+
+TERMS = [  # (heads, query heads of one, dim, page, new, lengths): few columns, many, many of wide heads
+    (2, 4, 128, 16, [1, 1], [700, 90]),
+    (2, 4, 128, 32, [40, 9], [700, 90]),
+    (1, 1, 64, 16, [70], [500]),
+    (1, 2, 128, 64, [600], [900]),
+    (1, 3, 256, 16, [24], [300]),
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("case", TERMS, ids=str)
+def test_attention_weights_in_more_bits_than_the_result(fx, h, t, case):
+    """The weights' rounding before the second product stays below the result's on
+    every path: two bf16 terms, 2^-16 of a weight, for f16 and bf16, three for f32.
+    The tolerance is the one above with that in the place of 2^-8; an output that
+    cancels to a small part of its values tells one term from two."""
+    heads, group, dim, page, new, lens = case
+    note("attention terms", t, case)
+    cache = Cache(fx, len(new), lens, heads, dim, page, seed=dim)
+    k, v, ks, vs = fill(cache, lens, 31)
+    q_heads, scale, row = heads * group, 0.2 * dim ** -0.5, 0
+    q = torch.randn(sum(new), q_heads * dim, generator=torch.Generator().manual_seed(17)).to(TYPES[t])
+    got = run_attention(fx, h, cache, new, lens, q, q_heads, scale, 1, t)
+    assert fx.sync_status(h) == 0
+    up = 2.0 ** -23 if t == "f32" else 2.0 ** -16
+    for s, n in enumerate(lens):
+        pages = cache.table[s, : -(-n // page)]
+        x = q[row : row + new[s]].double().view(new[s], heads, group, dim).numpy()
+        y = got[row : row + new[s]].astype(np.float64).reshape(new[s], heads, group, dim)
+        row += new[s]
+        seen = np.arange(n)[None, :] < n - new[s] + 1 + np.arange(new[s])[:, None]
+        for hd in range(heads):
+            K = (k[pages, hd] * ks[pages, hd][:, None, None]).reshape(-1, dim)[:n]
+            V = (v[pages, hd] * vs[pages, hd][:, None, None]).reshape(-1, dim)[:n]
+            for gq in range(group):
+                xq = x[:, hd, gq]
+                z = np.where(seen, xq @ K.T * scale, -np.inf)
+                p = np.exp(z - z.max(1, keepdims=True))
+                want = p @ V / p.sum(1, keepdims=True)
+                unit = 2.0 ** (np.floor(np.log2(np.abs(xq).max(1))) - 6) / (2 ** 24 if t == "f32" else 65536)
+                d = scale * unit * np.abs(K).sum(1).max() + 8 * 2.0 ** -24 * np.abs(np.where(seen, z, 0)).max(1)
+                tol = (2 * d + 4 * 2.0 ** -23 + up + (n + 64) * 2.0 ** -24)[:, None] * np.abs(V).max()
+                tol = tol + HALF_ULP[t] * np.abs(want) * 1.01 + 2.0 ** -25 * (t == "f16")
+                assert (np.abs(y[:, hd, gq] - want) <= tol).all(), (s, hd, gq, (np.abs(y[:, hd, gq] - want) / tol).max())
