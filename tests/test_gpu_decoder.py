@@ -273,3 +273,28 @@ def test_rotation_tables_are_checked_for_alignment():
         for rot in (fx.Rotary(cos=at + shift, sin=at, positions=16, dims=32), fx.Rotary(cos=at, sin=at + shift, positions=16, dims=32)):
             assert fx.lib().fxpq_cache_append(p(handle), p(cache), p(batch), p(rot), None, 32, None, 32, None, 0, None, 0, 0,
                                               fx.F32) == want, shift
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_cache_of_one_call_against_several(dec, dtype):
+    """Rows quantized one by one, exact sums, scales of whole pages: prompts that are
+    cut where pages end leave the same codes and scales as in one call.  The norm, a
+    reduction of torch's whose order may depend on the number of rows, is left out."""
+    note("decoder cache", dtype)
+    layer, whole = make(dec, dtype)
+    other, parts = make(dec, dtype)
+    new, cut = [64, 17, 48], [32, 16, 16]
+    rest = [n - c for n, c in zip(new, cut)]
+    x = [torch.randn(n, 256, device=DEV).to(dtype) for n in new]
+    layer.attend(torch.cat(x), whole, whole.extend([0, 1, 2], new))
+    layer.attend(torch.cat([a[:c] for a, c in zip(x, cut)]), parts, parts.extend([0, 1, 2], cut))
+    layer.attend(torch.cat([a[c:] for a, c in zip(x, cut)]), parts, parts.extend([0, 1, 2], rest))
+    torch.cuda.synchronize()
+    for s in range(3):
+        a, b = whole.owned[s], parts.owned[s]
+        assert len(a) == len(b) == -(-new[s] // 16)
+        for one, several in zip((whole.k, whole.v, whole.k_scale, whole.v_scale), (parts.k, parts.v, parts.k_scale, parts.v_scale)):
+            assert torch.equal(one[a], several[b])  # slots past the end are 0 in both
+    layer.h.close()
+    other.h.close()

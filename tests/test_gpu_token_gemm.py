@@ -347,3 +347,69 @@ def test_products_of_no_rows_of_a_wide_layer(fx, h):
     assert need == 0
     fx.token_gemm(h, 0, 5000, 64, None, 64, None, b, f, None, y, fx.F32, 5000, None, need)
     assert fx.sync_status(h) == 0 and (y == 9.0).all()
+
+
+def check_on_device(y, p, want, t):
+    tol = 4 * 2.0 ** -24 * p.abs() + (2 * 2.0 ** -24 + 1.01 * HALF_ULP[t]) * want.abs() + (2.0 ** -25 if t == "f16" else 1e-40)
+    err = (y.double() - want).abs()
+    assert (err <= tol).all(), (err / tol).max()
+
+
+def codes_of(seed, *shape):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randint(-128, 128, shape, generator=g, device=DEV, dtype=torch.int16).to(torch.int8)
+
+
+def scales_of(seed, *shape):
+    return torch.rand(*shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV) * 1e-2
+
+
+@pytest.mark.parametrize("m,n,k", [(130, 1025, 2064), (600, 2100, 272), (513, 4097, 144), (4097, 2101, 272), (4000, 2100, 144)])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("aligned", [True, False], ids=["aligned", "odd"])
+def test_token_gemm_results_of_every_tile(fx, h, m, n, k, t, aligned):
+    """Each tile shape (64 x 64, 128 x 64, 128 x 128, 256 x 256 twice) in each type of
+    result, its rows 16-byte aligned (whole pieces, the last one of an odd N in part)
+    and not (element by element); partly filled tiles on both sides."""
+    note("token_gemm results", m, n, k, t, aligned)
+    a, b, sa, sb = codes_of(1, m, k), codes_of(2, n, k), scales_of(3, m), scales_of(4, n)
+    bias = torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV)
+    ldy = (n + 7) // 8 * 8 if aligned else n + 1 + n % 2
+    y = torch.full((m, ldy), 123.0, dtype=TYPES[t], device=DEV)
+    need = fx.token_gemm_workspace(m, n, k)
+    ws = torch.full((max(need, 16),), 0x5A, dtype=torch.uint8, device=DEV)
+    fx.token_gemm(h, m, n, k, a, k, sa, b, sb, bias, y, code_of(fx, t), ldy, ws, need)
+    assert fx.sync_status(h) == 0
+    p = (a.double() @ b.double().t().contiguous()) * sa.double()[:, None] * sb.double()
+    check_on_device(y[:, :n], p, p + bias.double(), t)
+    assert (y[:, n:] == 123.0).all()
+
+
+@pytest.mark.parametrize("counts,n,k", [([257, 0, 2561, 1182], 2101, 144), ([3000, 1, 255, 744], 2100, 144),
+                                        ([129, 0, 1, 640, 230], 1101, 144), ([385, 3, 0, 511, 1], 2101, 144)],
+                         ids=["256x256 odd", "256x256", "128x64", "128x128"])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("aligned", [True, False], ids=["aligned", "odd"])
+def test_expert_gemm_results_of_every_tile(fx, h, counts, n, k, t, aligned):
+    """Ragged groups, some of one row, none, or one row past a whole tile, in the tiles
+    that large groups take: every row by its own expert's weights, none past the last
+    group."""
+    note("expert_gemm results", counts, n, k, t, aligned)
+    e, rows = len(counts), sum(counts)
+    count = rows // 2
+    a, b = codes_of(1, count, k), codes_of(2, e, n, k)
+    sa, sb = scales_of(3, count), scales_of(4, e, n)
+    bias = torch.randn(e, n, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV)
+    pick = (torch.randperm(rows, generator=gen(6)) % count).to(torch.int32).to(DEV)
+    off = torch.tensor([0] + counts).cumsum(0).to(torch.int32)
+    ldy = (n + 7) // 8 * 8 if aligned else n + 1 + n % 2
+    y = torch.full((rows + 2, ldy), 123.0, dtype=TYPES[t], device=DEV)
+    fx.expert_gemm(h, rows, n, k, e, a, count, k, sa, pick, off.to(DEV), b, sb, bias, y, code_of(fx, t), ldy)
+    assert fx.sync_status(h) == 0
+    for i in range(e):
+        lo, hi = int(off[i]), int(off[i + 1])
+        at = pick[lo:hi].long()
+        p = (a[at].double() @ b[i].double().t().contiguous()) * sa[at].double()[:, None] * sb[i].double()
+        if lo < hi:
+            check_on_device(y[lo:hi, :n], p, p + bias[i].double(), t)
+    assert (y[rows:] == 123.0).all() and (y[:, n:] == 123.0).all()
