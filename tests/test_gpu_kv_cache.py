@@ -578,3 +578,34 @@ def test_attention_weights_in_more_bits_than_the_result(fx, h, t, case):
                 tol = (2 * d + 4 * 2.0 ** -23 + up + (n + 64) * 2.0 ** -24)[:, None] * np.abs(V).max()
                 tol = tol + HALF_ULP[t] * np.abs(want) * 1.01 + 2.0 ** -25 * (t == "f16")
                 assert (np.abs(y[:, hd, gq] - want) <= tol).all(), (s, hd, gq, (np.abs(y[:, hd, gq] - want) / tol).max())
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("page,old,new", [(16, 5, 1), (16, 13, 3), (32, 31, 1), (64, 41, 8), (128, 127, 1), (128, 97, 5)], ids=str)
+@pytest.mark.parametrize("gap", [8, 1])
+def test_scale_growth_in_a_filled_page(fx, h, t, page, old, new, gap):
+    """A few tokens, far larger than the page's old ones in some heads and smaller in
+    others: old codes are requantized where the scale grows and only there, and slots
+    past the new tokens keep their bytes."""
+    note("growth", t, page, old, new, gap)
+    heads, dim = 3, 48
+    cache = Cache(fx, 2, [page, page], heads, dim, page)
+    model = Model(cache)
+    ld = heads * dim + gap
+    g = torch.Generator().manual_seed(page + old)
+    at = 0
+    for n, size in ((old, 1.0), (new, 1.0), (0, 1.0)) if old + new == page else ((old, 1.0), (new, 1.0), (1, 100.0)):
+        x = torch.randn(2 * n, heads, dim, generator=g) * size
+        if at:
+            x = x * torch.tensor([5.0, 0.01, 300.0])[None, :, None]
+        x = x.to(TYPES[t])
+        d = torch.full((2 * n, ld), float("nan"), dtype=TYPES[t])
+        d[:, : heads * dim] = x.flatten(1)
+        d = d.to(DEV)
+        at += n
+        fx.cache_append(h, cache.desc, cache.batch([n, n], [at, at]), None, d, ld, d, ld, None, 0, None, 0, 0, code_of(fx, t))
+        assert fx.sync_status(h) == 0
+        for s in range(2 if n else 0):
+            rows = x[s * n : s * n + n].float().numpy()
+            model.append(s, at - n, rows, rows)
+        model.check(cache)
