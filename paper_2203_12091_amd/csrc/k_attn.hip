@@ -866,9 +866,15 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
     }
   }
   const int64_t chunks = (b.max_len + 63) / 64;
-  // blocks that the chip holds at a time, by the kernels' registers
-  // (eight waves: one, and a quarter more for those that end early)
-  const int64_t slots = p.waves == 8 ? (int64_t)c.cus * 5 / 4
+  // Blocks that the chip holds at a time, by the kernels' registers; one a CU too for
+  // few columns in fp32 of up to 64 dimensions, where two would fit and measure the same
+  // (64 sequences of up to 8192: 72.6 and 72.4 us).  Eight waves: one a CU, and a
+  // quarter more where there are several sequences, whose blocks end early by their
+  // lengths (2 x 64 over up to 20000: 70 us so, 79 without; 4 x 64 in 4 heads 67 and 78;
+  // but 123 and 82 where both are 20000 long, which the host does not know).  One
+  // sequence's blocks end together, and a quarter would run alone (512 over 20000: 400
+  // us so, 271 without; 48 over 100000: 249 and 157).
+  const int64_t slots = p.waves == 8 ? (b.seqs > 1 ? (int64_t)c.cus * 5 / 4 : (int64_t)c.cus)
                                      : (int64_t)c.cus * (k.dim > 128 || (p.tok && type == FXPQ_F32) ? 1 : 2);
   int64_t per = (blocks * chunks + slots - 1) / slots;
   if (p.tok) per = per < 8 ? 8 : per > 32 ? 32 : per;

@@ -609,3 +609,23 @@ def test_scale_growth_in_a_filled_page(fx, h, t, page, old, new, gap):
             rows = x[s * n : s * n + n].float().numpy()
             model.append(s, at - n, rows, rows)
         model.check(cache)
+
+
+@pytest.mark.parametrize("new,length", [(128, 60000), (512, 20000), (48, 100000)])
+def test_blocks_of_one_sequence_end_together(fx, h, new, length):
+    """With one sequence every block of the split cache has equal work: there are no
+    more of them than compute units, else a few would run alone after the others.  The
+    number of splits follows from the work space, whose rows are [splits][tokens][query
+    heads] of dim values and two statistics; a block has 256 query columns (f16, bf16)."""
+    heads, group, dim = 8, 4, 128
+    need = fx.cache_attention_workspace(h, *one_sequence(fx, heads, dim, new, length), heads * group)
+    splits = need // (new * heads * group * (dim + 2) * 4)
+    tiles = -(-new * group // 256)
+    assert 1 < splits and splits * tiles * heads <= torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def one_sequence(fx, heads, dim, new, length):
+    """Descriptors alone: nothing is launched."""
+    t = torch.zeros(16, dtype=torch.int32, device=DEV)
+    cache = fx.kv_cache(t, t, t, t, 1, 16, heads, dim)
+    return cache, fx.kv_batch(t, t, t, 1, 1 << 20, new, new, length)
