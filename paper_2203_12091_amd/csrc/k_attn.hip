@@ -141,6 +141,7 @@ __device__ inline void emit(const AttnArgs& a, const SeqDev& s, int head, int sp
 // columns and deal the chunks among them (few columns), else each has its own.
 template <typename T, int DB, int NC, int SPLIT_Q, int SPLIT_P, bool TOK>
 __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
+  static_assert(SPLIT_Q == 3 || SPLIT_Q == 4, "three digit planes (16-bit types) or four");
   constexpr int DT = DB * 4;  // 16-dimension tiles of O
   extern __shared__ float smem[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
@@ -204,9 +205,9 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
     top = __builtin_bit_cast(float, max(__builtin_bit_cast(int, top), __shfl_xor(__builtin_bit_cast(int, top), 16)));
     top = __builtin_bit_cast(float, max(__builtin_bit_cast(int, top), __shfl_xor(__builtin_bit_cast(int, top), 32)));
     const float step = dfx_scale(fmaxf(finite(top) ? top : 1.0f, kScaleFloor));
-    constexpr float kUp = SPLIT_Q == 1 ? 1.0f : SPLIT_Q == 2 ? 256.0f : SPLIT_Q == 3 ? 65536.0f : 16777216.0f;
+    constexpr float kUp = SPLIT_Q == 3 ? 65536.0f : 16777216.0f;
     // the largest sum of balanced digits: 127 in every place
-    constexpr float kMost = SPLIT_Q == 1 ? 127.0f : SPLIT_Q == 2 ? 32639.0f : SPLIT_Q == 3 ? 8355711.0f : 2139062016.0f;
+    constexpr float kMost = SPLIT_Q == 3 ? 8355711.0f : 2139062016.0f;
     const float inv = pow2_inverse(step) * kUp;
     qscale[c] = finite(top) ? step * (1.0f / kUp) * a.scale : __builtin_nanf("");
 #pragma unroll
@@ -312,9 +313,7 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float v;  // |acc| < 2^22: two planes combine exactly in an int
-          if constexpr (SPLIT_Q == 1) v = (float)acc[0][r];
-          else if constexpr (SPLIT_Q == 2) v = (float)(acc[1][r] * 256 + acc[0][r]);
-          else if constexpr (SPLIT_Q == 3) v = fmaf((float)(acc[2][r] * 256 + acc[1][r]), 256.0f, (float)acc[0][r]);
+          if constexpr (SPLIT_Q == 3) v = fmaf((float)(acc[2][r] * 256 + acc[1][r]), 256.0f, (float)acc[0][r]);
           else v = fmaf((float)(acc[3][r] * 256 + acc[2][r]), 65536.0f, (float)(acc[1][r] * 256 + acc[0][r]));
           x[c][t * 4 + r] = scaled(v, f);
         }
