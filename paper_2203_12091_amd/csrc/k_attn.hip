@@ -70,10 +70,10 @@ __device__ inline float over_groups(float x) {
 // Blocks are dealt to the 8 XCDs round-robin by id, so the heads, which have equal
 // work, are the fastest index; where they are 8, a head's keys come through one
 // XCD's L2.  Query tiles of a sequence run together, for the same reason (4 x 1024
-// new tokens over 4000: 303 us, with the sequences in turn 516).  Splits are dealt
+// new tokens over 4000: 237 us, with the sequences in turn 279).  Splits are dealt
 // across the sequences, each sequence's to another XCD: a late split is one that
-// only long sequences have (64 sequences of up to 8192: 164 us with the splits next
-// to each other, 124 so).
+// only long sequences have (64 sequences of up to 8192: 118.4 us with the splits next
+// to each other, 117.7 so).
 struct BlockAt {
   int head, seq, part;
 };
@@ -138,7 +138,12 @@ __device__ inline void emit(const AttnArgs& a, const SeqDev& s, int head, int sp
 
 // DB: 64-dimension blocks of a head; NC: 16-column query tiles of a wave; SPLIT_Q:
 // digit planes of q; SPLIT_P: bf16 terms of P; TOK: the four waves share the
-// columns and deal the chunks among them (few columns), else each has its own.
+// columns and deal the chunks among them (few columns), else each has its own (many
+// columns of more than 128 dimensions).  Few columns are bound by memory: one token of
+// 64 sequences of up to 8192, 8 heads of 128, 118 us and 4.7 TB/s in bf16, 136 and 4.0
+// in fp32 (287 registers, one wave a SIMD); of 256 dimensions 227 and 4.8.  Many columns
+// of 256 dimensions, 4 x 1024 new tokens over up to 4000: 711 us, one wave a SIMD and
+// every wave converting all codes.
 template <typename T, int DB, int NC, int SPLIT_Q, int SPLIT_P, bool TOK>
 __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
   static_assert(SPLIT_Q == 3 || SPLIT_Q == 4, "three digit planes (16-bit types) or four");
@@ -432,11 +437,14 @@ __global__ __launch_bounds__(256) void k_cache_attention(AttnArgs a) {
 }
 
 // ---- many query columns ----------------------------------------------------------
-// A block of four waves, 16 NC columns each, goes over the cache together: every
+// A block of four or eight waves, 16 NC columns each, goes over the cache together: every
 // thread loads its share of the next 64 tokens' codes while the waves work on the
 // current ones, converts it and leaves it in LDS in the operand types, K as T's own
 // matrix-core type (bf16 for f32), V as bf16 (both hold a code exactly).  q goes in
 // as QT terms of that type (exact for f16 and bf16), P as PT bf16 terms.
+// 4 x 1024 new tokens over up to 4000, 32 query heads of 8 of 128: 237 us in f16, 236
+// in bf16, 379 in fp32.  Bound by the softmax's vector arithmetic, about twelve
+// operations an element, beside the matrix products, at two waves a SIMD.
 template <typename T>
 struct OperandK {
   typedef __bf16 type;
@@ -768,7 +776,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_cache_attention_wide(AttnArgs a)
   }
 }
 
-// Joins the splits of each query row: one block per token and query head.
+// Joins the splits of each query row: one block per token and query head (64 of 32
+// heads of 128: 7 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a, int kcols) {
   constexpr int kMany = 256;  // weights kept at a time
@@ -833,10 +842,10 @@ struct AttnPlan {
 // Chunks of a split.  With few columns a block's own cost is small, and what matters
 // is that all CUs are busy at the end of a ragged batch: 32 chunks (2048 tokens),
 // fewer down to 8 where that would leave CUs without a block (one token over
-// 131072: 32 chunks 58.9 us, 16 64.1; over 4096: 8 chunks 13.5 us, 16 17.0).  With
+// 131072: 32 chunks 58.9 us, 16 63.0; over 4096: 8 chunks 12.7 us, 16 15.8).  With
 // many columns a split writes and reads back all of them, and is worth it only
 // where the tiles alone do not fill the CUs (16 new tokens over 8000, 4 heads: 8
-// chunks 36 us, 16 56; 4 x 1024 over 4000: whole 303, in three 536).
+// chunks 30 us, 16 49; 4 x 1024 over 4000: whole 237, in three 442).
 AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batch& b, int q_heads, int type) {
   AttnPlan p{};
   const int64_t cols = (int64_t)b.max_new * (q_heads / k.heads);
@@ -853,9 +862,9 @@ AttnPlan plan_attention(const Ctx& c, const fxpq_kv_cache& k, const fxpq_kv_batc
   if (!p.tok && k.dim > 64 && k.dim <= 128 && cols > p.nc * 64) {
     // eight waves share one conversion of the keys and values, but a CU holds one
     // such block: for many tiles, or so few that the cache is split anyway
-    // (4 x 1024 over 4000: 268 us against 284; 2 x 64 over 20000: 70 against 90; the
+    // (4 x 1024 over 4000: 237 us against 240; 2 x 64 over 20000: 69 against 88; the
     // reverse where four waves just fill the chip, 4 x 1024 over 1000 with 16
-    // ungrouped heads: 167 against 99)
+    // ungrouped heads: 174 against 86)
     const int64_t eight = blocks_of(8);
     if (eight >= 2 * (int64_t)c.cus || blocks < c.cus) {
       p.waves = 8;

@@ -11,7 +11,8 @@ namespace {
 
 // ---- per-token quantization ----------------------------------------------------
 // One block per row: the largest magnitude, then the codes from a second read
-// of the row (at most a few ten KB, from the caches).
+// of the row (at most a few ten KB, from the caches).  Bound by memory: 8192 rows of
+// 2048 bf16 values 12.5 us, 4.0 TB/s; one row 2 us, a launch.
 // VB: bytes of a load that every row's address is aligned to (16, 8 or the type's).
 template <typename T, int VB, int NT>
 __global__ __launch_bounds__(NT) void k_token_quantize(const T* __restrict__ x, int64_t cols,
@@ -106,6 +107,8 @@ __device__ inline int out_off(int row, int chunk) {
 // Output tile BM tokens x BN channels; WR x WC waves, each (BM / WR) x (BN / WC)
 // in 32 x 32 matrix-core tiles.  Both operands go through an LDS ring of NS
 // stages of KS bytes of depth, filled by global -> LDS loads NS - 1 steps ahead.
+// Large products are bound by the matrix cores, whose clock falls under them: 8192 x
+// 8192 x 4096 (rows, channels, depth) in 230 to 268 us, 2.0 to 2.4 P operations/s.
 // T = int: a block takes the blockIdx.y-th share of the depth and leaves its sums
 // in g.y, [share][M][ldy], for k_gemm_join.
 template <int BM, int BN, int WR, int WC, int KS, int NS, bool GROUP, typename T>
@@ -423,7 +426,7 @@ __global__ __launch_bounds__(WR* WC * 64) void k_gemm_tile(GemmArgs g) {
       T* p = y + to * g.ldy + n;
       if (vec && n + E <= g.N) {
         // the largest tiles make outputs larger than the L2s: past them, so that the
-        // operands stay (8192 x 8192 x 4096: 276 -> 258 us, 16 experts 213 -> 190)
+        // operands stay (8192 x 8192 x 4096: 276 -> 258 us, 16 experts 208 -> 189)
         if constexpr (BM == 256) __builtin_nontemporal_store(__builtin_bit_cast(v4i, v), reinterpret_cast<v4i*>(p));
         else *reinterpret_cast<Reals<T, E>*>(p) = v;
       } else {
@@ -459,7 +462,8 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, const int* part, 
 // One block per 16 output channels; its eight waves deal the depth among them in
 // 128-byte steps and read both operands straight into the matrix cores' registers
 // (lane: channel or row l % 16, 16 bytes of the depth): nothing waits for a
-// barrier before the end, where the eight partial sums are joined.
+// barrier before the end, where the eight partial sums are joined.  Bound by latency:
+// one row of 1000 channels, depth 2048, 4.8 us.
 constexpr int kFewRows = 16;
 
 template <bool GROUP, typename T>
@@ -575,7 +579,10 @@ constexpr int64_t kCus = 256;  // of an MI355X; the work space's size must not n
 
 // Time of a product by its tiles' shape, in us at a depth of 4096 (measured): the
 // 256 x 256 tile has a CU to itself, the others share it with a second block, which
-// costs less than twice the time of one.
+// costs less than twice the time of one.  Shapes are compared at that depth whatever
+// the product's own, which scales all but a block's start and end: 777 x 1533 x 2064
+// (rows, channels, depth) takes 18.0 us by the 128 x 64 tiles that this picks and 17.9
+// by 64 x 64, 300 x 4096 x 4096 18.3 and 17.4 (with the quantization).
 enum Tile { T64, T128x64, T128, T256 };
 double tile_cost(Tile t, double tiles) {
   constexpr double one[] = {11.5, 16, 24, 43}, two[] = {17, 27, 41, 86};
@@ -599,13 +606,18 @@ Tile best_tile(int64_t M, int64_t N, double experts, bool large) {
   return (Tile)best;
 }
 
-// At most 16 rows: 6.5 us against 10.6 by 64 x 64 tiles (1 x 4096 x 4096), as long
-// as no CU gets more than one block (8 x 8192 x 1024: 6.5 against 5.1).
+// At most 16 rows, as long as no CU gets more than one block; wider products go by 64 x
+// 64 tiles, which read a weight once for all rows (rows x channels x depth, with the
+// quantization, this kernel first: 1 x 4096 x 4096 12.1 and 14.3 us, 16 x 1024 x 8192
+// 13.0 and 14.3; 1 x 8192 x 4096 13.7 and 14.3, 16 x 8192 x 4096 15.3 and 14.4, 1 x
+// 14336 x 4096 18.2 and 13.3, 16 x 14336 x 4096 22.3 and 13.9).
 bool few_rows(int64_t M, int64_t N) { return M <= kFewRows && N <= 16 * kCus; }
 
-// Where 64 x 64 tiles leave CUs idle and the depth is long, blocks share it: each
-// at least 2048 deep (64 x 4096 x 9216: 20.2 us whole, 13.4 in four; 64 x 1000 x
-// 2048: 7.2 whole, 8.4 in two).
+// Where 64 x 64 tiles leave CUs idle and the depth is long, blocks share it: one for
+// each 2048 of it at most, in whole slabs, so that the last share may be shorter (rows
+// x channels x depth, with the quantization: 64 x 4096 x 9216 23.6 us whole, 18.7 in
+// two, 16.7 in four; 64 x 4096 x 4112 16.0, 14.7 in two, 14.2 in four; 64 x 2048 x 1008
+// 11.9 whole, 14.0 in two).  No rows, no tiles: M = 0 asks for a work space, too.
 int depth_shares(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || few_rows(M, N)) return 1;
   const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
@@ -623,7 +635,7 @@ hipError_t launch_token_quantize(const Ctx& c, const void* x, int x_type, int64_
     const T* p = static_cast<const T*>(x);
     const uintptr_t at = (uintptr_t)x | (uintptr_t)(ldx * sizeof(T));
     // few rows leave most CUs without one: more threads for each (64 rows of 9216 and
-    // their product 18.3 -> 17.2 us; 8192 rows of 4096 the other way, 276 -> 296)
+    // their product 18.4 -> 17.5 us; 8192 rows of 4096 the other way, 257 -> 277)
     const auto run = [&](auto bytes) {
       constexpr int VB = decltype(bytes)::value;
       if (rows < c.cus && cols > 4096)
@@ -664,9 +676,11 @@ hipError_t launch_expert_gemm(const Ctx& c, const GemmArgs& g, int y_type) {
   return for_real(y_type, [&](auto zero) {
     using T = decltype(zero);
     if (few_rows(g.M, g.N)) return run_few<true, T>(c, g);
-    // 128 rows of 32 experts (4096 x 2048 weights): 58.7 us by 32 x 64 tiles, 65.1 by
-    // 64 x 64, 93 by the kernel for few rows; 1024 rows of 16: 56.6, 56.1 and (128 x
-    // 128) 51.5; 2048 of 16: 128 x 128 57.6, 256 x 256 70.4; 8192 of 16: 136 and 123
+    // By the mean group, 4096 x 2048 weights, with the quantization: 128 rows of 32
+    // experts 59.7 us by 32 x 64 tiles, 62.3 by 64 x 64; 1024 rows of 16 equal experts
+    // 52.4 by 32 x 64, 43.4 by 64 x 64 (the costs' choice), 40.2 by 128 x 128; 2048 of
+    // 16 ragged ones 62.3 by 128 x 128, 71.0 by 256 x 256 (equal ones 47.7 and 47.2);
+    // 4096 of 16 74.7 and 55.0; 16384 of 16 ragged ones 240 and 186
     const int64_t mean = g.M / g.experts;
     if (mean <= 32) return run_tile<32, 64, 1, 2, 128, 4, true, T>(c, g);
     switch (best_tile(g.M, g.N, g.experts, mean >= 192)) {
