@@ -717,7 +717,9 @@ fxpq_status fxpq_cache_read(fxpq_handle h, const fxpq_kv_cache* cache, const fxp
  * query's own.  q: rows of q_heads * dim reals (row stride ldq); query head i
  * uses key / value head i / (q_heads / heads), q_heads % heads == 0.  out: the
  * same shape, row stride ldo.  A query that sees no token gets 0, one that
- * holds a NaN or an infinity gets NaN.  workspace as for fxpq_token_gemm.
+ * holds a NaN or an infinity gets NaN.  Weights are divided by their sum last:
+ * 2^8 * tokens * max |v| has to stay below 2^128.  workspace as for
+ * fxpq_token_gemm.
  */
 fxpq_status fxpq_cache_attention_workspace(fxpq_handle h, const fxpq_kv_cache* cache,
                                            const fxpq_kv_batch* batch, int32_t q_heads,
