@@ -186,7 +186,9 @@ class Layer:
     def forward(self, x, cache, batch):
         """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's
         current stream (quantize_rows, the first call of each half, says so).  Where it
-        raises, the cache's lengths and pages are those from before the batch."""
+        raises, the cache's lengths and pages are those from before the batch.  It does
+        not wait for the device: what raises a flag there (a NaN or an infinity in x) is
+        for the caller to ask for, with fx.sync_status(layer.h)."""
         try:
             if x.shape != (batch.tokens, self.hidden):
                 raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
