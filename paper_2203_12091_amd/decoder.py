@@ -84,7 +84,7 @@ class Cache:
     def retract(self, batch):
         """Takes back the newest batch of its sequences, whose tokens were not computed:
         their lengths, and the pages that only those tokens needed."""
-        for s, n in batch.grown.items():
+        for s, n in getattr(batch, "grown", {}).items():  # a batch made by hand took nothing
             if s not in self.length:
                 continue
             self.length[s] -= n

@@ -165,3 +165,12 @@ def test_failed_forward_takes_back_the_batch(dec, monkeypatch):
     cache.release(1)
     cache.retract(batch)  # a sequence that is gone stays gone
     assert 1 not in cache.length and len(cache.free) == 6
+
+
+def test_failed_forward_of_a_batch_made_by_hand(dec):
+    """A batch that no extend made has nothing to take back: the error is its own."""
+    layer, cache = make(dec)
+    batch = dec.fx.kv_batch(None, None, None, 1, 4, 5, 5, 5)
+    with pytest.raises(ValueError):
+        layer.forward(torch.zeros(4, 64), cache, batch)
+    assert cache.length == {} and len(cache.free) == 8
