@@ -1,0 +1,419 @@
+"""The latent attention operators as measurable cases.
+
+  append     rotate each token's shared key and the rotary part of its query heads,
+             append its latent vector and that key to the paged 8-bit latent cache
+             (a scale for each token and part), read the new tokens' values back
+  read       every token of the sequences out of the pages: rows of codes with their
+             scales, as the 8-bit product takes them, and the rotary keys
+  latent     absorbed attention: the query heads of a token over one shared latent
+             vector and rotary key a token, which are keys and values at once
+  expanded   attention of a prompt over keys and values of each head, made of the
+             latents, and the shared rotary key; causal
+
+``run`` computes them in their plain form (elementary torch operations in 32
+bits) or, where ``own`` is set, through the framework's entry points.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+FLOOR = 2.0 ** -100  # magnitudes below this count as this when a scale is chosen
+
+
+def listed():
+    return [
+        # one decoding step of 64 sequences
+        dict(name="append_64x1", kind="append", seqs=64, new=1, ctx=4096, page=16, heads=16, nope=64, latent=512, rope=64, interleaved=True, rule="max", type="bf16"),
+        # prompts of up to 2048 tokens, some continuing an earlier context; power-of-two scales
+        dict(name="append_8x2048", kind="append", seqs=8, new=2048, ctx=1000, page=64, heads=32, nope=128, latent=512, rope=64, interleaved=False, rule="dfx", type="f16"),
+        # a short odd context, full-precision values
+        dict(name="read_3x777", kind="read", seqs=3, ctx=777, page=32, latent=256, rope=32, type="f32"),
+        # a batch of contexts about to be expanded for a prompt
+        dict(name="read_16x8192", kind="read", seqs=16, ctx=8192, page=64, latent=512, rope=64, type="bf16"),
+        # one short conversation: latency
+        dict(name="latent_1x1_300", kind="latent", seqs=1, new=1, ctx=300, page=16, heads=16, latent=512, rope=64, type="bf16"),
+        # a few drafted tokens a sequence, an odd number of heads, full-precision values
+        dict(name="latent_5x7_3001", kind="latent", seqs=5, new=7, ctx=3001, page=32, heads=12, latent=256, rope=32, type="f32"),
+        # a full serving batch, lengths from a few tokens to 8192: bound by memory
+        dict(name="latent_64x1_8192", kind="latent", seqs=64, new=1, ctx=8192, page=64, heads=16, latent=512, rope=64, type="bf16"),
+        # the same path with many heads a token: bound by the matrix cores
+        dict(name="latent_32x1_4096_h128", kind="latent", seqs=32, new=1, ctx=4096, page=64, heads=128, latent=512, rope=64, type="bf16"),
+        # one very long context: the cache is split among the compute units
+        dict(name="latent_1x1_131072", kind="latent", seqs=1, new=1, ctx=131072, page=128, heads=32, latent=512, rope=64, type="f16"),
+        # a short prompt of odd length: latency
+        dict(name="expanded_2x77", kind="expanded", seqs=2, new=77, ctx=50, heads=16, nope=64, rope=32, vdim=64, type="f32"),
+        # prompts appended in chunks: causal inside the chunk, everything before it visible
+        dict(name="expanded_4x1024_4000", kind="expanded", seqs=4, new=1024, ctx=4000, heads=32, nope=128, rope=64, vdim=128, type="bf16"),
+        # a long prompt from nothing
+        dict(name="expanded_1x8192", kind="expanded", seqs=1, new=8192, ctx=0, heads=16, nope=128, rope=64, vdim=128, type="f16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    top = {c["kind"]: max(_cost(x) for x in listed() if x["kind"] == c["kind"]) for c in listed()}
+    kind = rng.choice(["append", "read", "latent", "latent", "expanded"])
+    while True:
+        c = dict(kind=kind, seqs=_log(rng, 1, 64), new=rng.choice([1, 1, _log(rng, 2, 2048)]), ctx=_log(rng, 16, 131072),
+                 type=rng.choice(["bf16", "bf16", "f16", "f32"]), rope=rng.choice([32, 64, 64]))
+        if kind == "expanded":
+            c |= dict(new=_log(rng, 2, 8192), ctx=rng.choice([0, _log(rng, 16, 8192)]), heads=_log(rng, 1, 64),
+                      nope=rng.choice([64, 128]), vdim=rng.choice([64, 128]))
+        else:
+            c |= dict(page=rng.choice([16, 32, 64, 128]), latent=rng.choice([256, 512, 512]))
+        if kind in ("append", "latent"):
+            c["heads"] = _log(rng, 1, 128)
+        if kind == "append":
+            c |= dict(ctx=min(c["ctx"], 8192), nope=rng.choice([64, 128]), interleaved=rng.random() < 0.5, rule=rng.choice(["max", "dfx"]))
+        if kind == "read":
+            del c["new"]
+        if _cost(c) <= top[kind]:
+            return c
+
+
+def _cost(c):
+    """What bounds a draw: the time a plain form would take, roughly (padded sizes included)."""
+    if c["kind"] == "append":
+        return c["seqs"] * c["new"] * (c["heads"] * (c["nope"] + 3.0 * c["rope"]) + 8.0 * c["latent"]) + 0.1 * c["seqs"] * (c["ctx"] + c["new"])
+    if c["kind"] == "read":
+        return 1.0 * c["seqs"] * c["ctx"] * (c["latent"] + c["rope"])
+    if c["kind"] == "latent":
+        return c["seqs"] * (c["ctx"] + c["new"]) * (60.0 * (c["latent"] + c["rope"]) + 1.0 * c["new"] * c["heads"] * (c["latent"] + 40))
+    return 1.0 * c["seqs"] * (c["ctx"] + c["new"]) * c["new"] * c["heads"] * (c["nope"] + c["rope"] + c["vdim"] + 80)
+
+
+def _sizes(c):
+    """New tokens and lengths of the sequences, which the seed does not change: a ragged
+    batch, the first sequence has the largest sizes, the others spread below them."""
+    s, most = c["seqs"], c.get("new", 0)
+    new = [most if i % 3 == 0 else min(most, max(1, most * (2 * i + 1) // (2 * s + 1))) for i in range(s)]
+    return new, [n + (c["ctx"] if i == 0 else max(1 - min(n, 1), c["ctx"] * (i * 37 % (s + 1)) // (s + 1))) for i, n in enumerate(new)]
+
+
+def _seen(new, length):
+    return sum(n * x - n * (n - 1) // 2 for n, x in zip(new, length))
+
+
+def work(c):
+    b = 4 if c["type"] == "f32" else 2
+    new, length = _sizes(c)
+    t, held = sum(new), sum(length)
+    if c["kind"] == "append":
+        # read latents, keys and the queries' rotary parts; write those, the codes and scales; read and write the values
+        w = c["latent"] + c["rope"]
+        return {"bytes": t * (w * b + 2 * c["heads"] * c["rope"] * b + 2 * (w + 8) + w * b), "flops": 3 * t * c["rope"] * (c["heads"] + 1)}
+    if c["kind"] == "read":
+        return {"bytes": held * (2 * c["latent"] + 4 + c["rope"] + 8 + c["rope"] * b), "flops": held * c["rope"]}
+    if c["kind"] == "latent":
+        return {"bytes": held * (c["latent"] + c["rope"] + 8) + t * c["heads"] * (2 * c["latent"] + c["rope"]) * b,
+                "flops": 2 * _seen(new, length) * c["heads"] * (2 * c["latent"] + c["rope"])}
+    d = c["nope"] + c["rope"]
+    return {"bytes": b * (held * (c["heads"] * (c["nope"] + c["vdim"]) + c["rope"]) + t * c["heads"] * (d + c["vdim"])),
+            "flops": 2 * _seen(new, length) * c["heads"] * (d + c["vdim"])}
+
+
+class _State(dict):
+    __getattr__ = dict.__getitem__
+
+
+def prepare(case, seed):
+    c = _State(case)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    dt = TYPES[c.type]
+    randn = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    new, length = _sizes(c)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    t, held = sum(new), sum(length)
+    s = _State(case=c, dt=dt, tokens=t, held=held, most_new=max(new), most_len=max(length), length=ints(length),
+               start=ints([0] + new).cumsum(0).to(torch.int32), kv_start=ints([0] + length).cumsum(0).to(torch.int32))
+    if c.kind == "expanded":
+        # one product's output: each head's key and value side by side, as the latents give them
+        s.kv = randn(held, c.heads * (c.nope + c.vdim)).to(dt)
+        s.key = randn(held, c.rope).to(dt)
+        s.q = (1.5 * randn(t, c.heads * (c.nope + c.rope))).to(dt)
+        s |= dict(table=torch.zeros(c.seqs, 1, dtype=torch.int32, device=DEV), width=1)
+    else:
+        s |= _cache(c, g, length)
+    if c.kind == "append":
+        # one fused projection's output, latent and shared key side by side; normalised latents
+        # with some channels larger than the rest; whole queries, whose rotary part ends a head
+        s.ckr = (randn(t, c.latent + c.rope) * torch.exp(0.5 * randn(1, c.latent + c.rope))).to(dt)
+        s.q = randn(t, c.heads * (c.nope + c.rope)).to(dt)
+        ang = torch.arange(max(length), device=DEV, dtype=torch.float64)[:, None] * 10000.0 ** (
+            -torch.arange(0, c.rope, 2, device=DEV, dtype=torch.float64) / c.rope)
+        s.cos, s.sin = ang.cos().float(), ang.sin().float()
+    elif c.kind == "latent":
+        # queries that passed through the key's weights: some latent channels larger than the rest
+        s.q = (randn(t, c.heads, c.latent) * torch.exp(0.5 * randn(1, 1, c.latent))).to(dt)
+        s.qr = (1.5 * randn(t, c.heads, c.rope)).to(dt)
+    if own:
+        _handles(s)
+    return s
+
+
+def _cache(c, g, length):
+    """A paged latent cache that holds the contexts, its pages in no order."""
+    need = [-(-x // c.page) for x in length]
+    pages, width = sum(need), max(need)
+    order = torch.randperm(pages, generator=g, device=DEV).to(torch.int32)
+    table = torch.zeros(c.seqs, width, dtype=torch.int32, device=DEV)
+    at = 0
+    for i, n in enumerate(need):
+        table[i, :n] = order[at : at + n]
+        at += n
+    codes = torch.randn(pages, c.page, c.latent + c.rope, generator=g, device=DEV, dtype=torch.float16)
+    scale = lambda a: a / 127 * torch.exp(0.2 * torch.randn(pages, c.page, generator=g, device=DEV))  # noqa: E731
+    return dict(codes=(codes * 37).round().clamp(-127, 127).to(torch.int8), scale=scale(3.0), rope_scale=scale(4.0), table=table,
+                pages=pages, width=width)
+
+
+def _handles(s):
+    """What a user's program keeps beside its data: the handle, descriptors, results and work space."""
+    from paper_2203_12091_amd import fxpq as fx
+    global _handle
+    if _handle is None:
+        _handle = fx.Handle(0)
+    c, empty = s.case, lambda *sh, dt=s.dt: torch.empty(sh, dtype=dt, device=DEV)
+    s.fx, s.h, s.t = fx, _handle, {"f32": fx.F32, "f16": fx.F16, "bf16": fx.BF16}[c.type]
+    s.batch = fx.kv_batch(s.start, s.length, s.table, c.seqs, s.width, s.tokens, s.most_new, s.most_len)
+    if c.kind == "expanded":
+        d, v = c.nope + c.rope, c.nope + c.vdim
+        values = s.kv.data_ptr() + c.nope * s.kv.element_size()
+        s.desc = fx.expanded_kv(s.kv, c.heads * v, v, s.key, c.rope, values, c.heads * v, v, s.kv_start, s.held, c.heads, c.nope, c.rope, c.vdim)
+        s.out = empty(s.tokens, c.heads * c.vdim)
+        return
+    s.cache = fx.latent_cache(s.codes, s.scale, s.rope_scale, s.pages, c.page, c.latent, c.rope)
+    if c.kind == "append":
+        s.rotary = fx.rotary(s.cos, s.sin, s.cos.shape[0], c.rope, c.interleaved)
+        s |= dict(q_out=empty(s.tokens, c.heads, c.rope), latents=empty(s.tokens, c.latent), keys=empty(s.tokens, c.rope))
+    elif c.kind == "read":
+        s |= dict(rows=empty(s.held, c.latent, dt=torch.int8), steps=empty(s.held, dt=torch.float32), keys=empty(s.held, c.rope))
+    else:
+        s.out = empty(s.tokens, c.heads, c.latent)
+        s.ws_bytes = fx.latent_attention_workspace(s.h, s.cache, s.batch, c.heads)
+        s.ws = empty(max(s.ws_bytes, 16), dt=torch.uint8)
+
+
+_handle = None
+
+
+def run(s):
+    c = s.case
+    if own:
+        return _OWN[c.kind](s, c, s.fx)
+    return _PLAIN[c.kind](s, c)
+
+
+# ---- through the framework ----------------------------------------------------
+
+def _own_append(s, c, fx):
+    size, d, w = s.q.element_size(), c.nope + c.rope, c.latent + c.rope
+    rule = fx.SCALE_DFX if c.rule == "dfx" else fx.SCALE_MAX
+    fx.latent_append(s.h, s.cache, s.batch, s.rotary, rule, s.ckr, w, s.ckr.data_ptr() + c.latent * size, w,
+                     s.q.data_ptr() + c.nope * size, c.heads * d, d, s.q_out, c.heads * c.rope, c.rope, c.heads, s.t)
+    fx.latent_read(s.h, s.cache, s.batch, None, s.tokens, None, 0, None, s.latents, c.latent, s.keys, c.rope, s.t)
+    return s.q_out, s.latents, s.keys
+
+
+def _own_read(s, c, fx):
+    fx.latent_read(s.h, s.cache, s.batch, s.kv_start, s.held, s.rows, c.latent, s.steps, None, 0, s.keys, c.rope, s.t)
+    return s.rows, s.steps, s.keys
+
+
+def _own_latent(s, c, fx):
+    fx.latent_attention(s.h, s.cache, s.batch, s.q, c.heads * c.latent, c.latent, s.qr, c.heads * c.rope, c.rope, c.heads,
+                        _softmax_scale(c), 1, s.out, c.heads * c.latent, c.latent, s.t, s.ws, s.ws_bytes)
+    return s.out
+
+
+def _own_expanded(s, c, fx):
+    fx.expanded_attention(s.h, s.desc, s.batch, s.q, c.heads * (c.nope + c.rope), _softmax_scale(c), 1, s.out, c.heads * c.vdim, s.t)
+    return s.out
+
+
+_OWN = {"append": _own_append, "read": _own_read, "latent": _own_latent, "expanded": _own_expanded}
+
+
+# ---- plain forms ----------------------------------------------------------------
+
+def _softmax_scale(c):
+    # absorbed queries score as the heads they came from do: heads a quarter as wide as the latent
+    return (c.get("nope", c.get("latent", 0) // 4) + c.rope) ** -0.5
+
+
+def _quantize(x, rule):
+    """Codes (as fp32 integers) and the scale of each row."""
+    a = x.abs().amax(-1, keepdim=True).clamp_min(FLOOR)
+    if rule == "max":
+        return (x * (torch.full_like(a, 127.0) / a)).round(), a / 127.0
+    m, e = torch.frexp(a)
+    scale = torch.ldexp(torch.ones_like(a), e - 7 + (m * 128.0 >= 127.5).to(e.dtype))
+    return (x / scale).round(), scale
+
+
+def _rows(start, many, value):
+    """For rows 0 .. many - 1: the sequence each belongs to and its place behind start."""
+    i = torch.arange(many, device=DEV)
+    seq = torch.searchsorted(start, i.to(start.dtype), right=True) - 1
+    return seq, i - start[seq] + value[seq]
+
+
+def _rotate(x, cos, sin, interleaved):
+    """In 64 bits: a rounded product next to the border of two codes would pick the other one."""
+    x, cos, sin = x.double(), cos.double(), sin.double()
+    h = x.shape[-1] // 2
+    x1, x2 = (x[..., 0::2], x[..., 1::2]) if interleaved else (x[..., :h], x[..., h:])
+    y1, y2 = x1 * cos - x2 * sin, x2 * cos + x1 * sin
+    return (torch.stack([y1, y2], -1).flatten(-2) if interleaved else torch.cat([y1, y2], -1)).float()
+
+
+def _plain_append(s, c):
+    n = s.start[1:] - s.start[:-1]
+    seq, pos = _rows(s.start, s.tokens, s.length - n)
+    cos, sin = s.cos[pos], s.sin[pos]
+    q = s.q.view(s.tokens, c.heads, c.nope + c.rope)[..., c.nope :]
+    q = _rotate(q, cos[:, None], sin[:, None], c.interleaved)
+    latent, ls = _quantize(s.ckr[:, : c.latent].float(), c.rule)
+    key, ks = _quantize(_rotate(s.ckr[:, c.latent :], cos, sin, c.interleaved), c.rule)
+    page, slot = s.table[seq, pos // c.page].long(), pos % c.page
+    s.codes[page, slot] = torch.cat([latent, key], -1).to(torch.int8)
+    s.scale[page, slot], s.rope_scale[page, slot] = ls[:, 0], ks[:, 0]
+    held = s.codes[page, slot].float()
+    return (q.to(s.dt), (held[:, : c.latent] * s.scale[page, slot][:, None]).to(s.dt),
+            (held[:, c.latent :] * s.rope_scale[page, slot][:, None]).to(s.dt))
+
+
+def _plain_read(s, c):
+    seq, pos = _rows(s.kv_start, s.held, torch.zeros_like(s.length))
+    page, slot = s.table[seq, pos // c.page].long(), pos % c.page
+    held = s.codes[page, slot]
+    return held[:, : c.latent].contiguous(), s.scale[page, slot], (held[:, c.latent :].float() * s.rope_scale[page, slot][:, None]).to(s.dt)
+
+
+def _plain_latent(s, c):
+    S, H, N = c.seqs, c.heads, s.most_new
+    n = s.start[1:] - s.start[:-1]
+    page = s.table.long()
+    latent = (s.codes[page][..., : c.latent].float() * s.scale[page][..., None]).reshape(S, -1, c.latent)
+    key = (s.codes[page][..., c.latent :].float() * s.rope_scale[page][..., None]).reshape(S, -1, c.rope)
+    i = torch.arange(N, device=DEV)
+    src = (s.start[:-1, None] + torch.minimum(i, n[:, None] - 1)).clamp_min(0)
+    q, qr = s.q[src].float().reshape(S, N * H, c.latent), s.qr[src].float().reshape(S, N * H, c.rope)
+    x = q @ latent.transpose(1, 2).contiguous() + qr @ key.transpose(1, 2).contiguous()
+    x = (x * _softmax_scale(c)).view(S, N, H, -1)
+    see = torch.arange(x.shape[-1], device=DEV) <= ((s.length - n)[:, None] + i)[:, :, None]
+    x = x.masked_fill(~see[:, :, None], float("-inf"))
+    p = torch.exp(x - x.amax(-1, keepdim=True))
+    # pages past a sequence's end hold other sequences' rows: their weight is zero
+    o = ((p / p.sum(-1, keepdim=True)).view(S, N * H, -1) @ latent).view(S, N, H, c.latent)
+    seq, at = _rows(s.start, s.tokens, torch.zeros_like(s.length))
+    return o[seq, at].to(s.dt)
+
+
+def _plain_expanded(s, c):
+    S, H, N, L = c.seqs, c.heads, s.most_new, s.most_len
+    n = s.start[1:] - s.start[:-1]
+    i, j = torch.arange(N, device=DEV), torch.arange(L, device=DEV)
+    src = (s.start[:-1, None] + torch.minimum(i, n[:, None] - 1)).clamp_min(0)
+    at = s.kv_start[:-1, None] + torch.minimum(j, s.length[:, None] - 1)
+    kv = s.kv[at].float().view(S, L, H, c.nope + c.vdim).transpose(1, 2)
+    key = s.key[at].float()[:, None].expand(S, H, L, c.rope)
+    k = torch.cat([kv[..., : c.nope], key], -1).transpose(2, 3).contiguous()
+    q = s.q[src].float().view(S, N, H, c.nope + c.rope).transpose(1, 2).contiguous()
+    x = (q @ k) * _softmax_scale(c)
+    see = j <= ((s.length - n)[:, None] + i)[:, :, None]
+    x = x.masked_fill(~see[:, None], float("-inf"))
+    p = torch.exp(x - x.amax(-1, keepdim=True))
+    o = (p / p.sum(-1, keepdim=True)) @ kv[..., c.nope :].contiguous()
+    seq, place = _rows(s.start, s.tokens, torch.zeros_like(s.length))
+    return o.transpose(1, 2)[seq, place].reshape(s.tokens, H * c.vdim).to(s.dt)
+
+
+_PLAIN = {"append": _plain_append, "read": _plain_read, "latent": _plain_latent, "expanded": _plain_expanded}
+
+
+# ---- definitions in 64 bits ----------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return _EXACT[s.case.kind](s, s.case)
+
+
+def _exact_values(x, rule):
+    """What the codes of each row stand for."""
+    top = x.abs().max(dim=-1).values.clamp(min=FLOOR)
+    if rule == "max":
+        step = top / 127
+    else:
+        step = torch.exp2(torch.floor(torch.log2(top)) - 6)
+        step = torch.where(torch.round(top / step) > 127, 2 * step, step)
+    return torch.round(x / step[:, None]) * step[:, None]
+
+
+def _exact_append(s, c):
+    start, length, W = s.start.tolist(), s.length.tolist(), c.latent
+    queries, keys = [], []
+    for i in range(c.seqs):
+        a, b = start[i], start[i + 1]
+        p0 = length[i] - (b - a)
+        turn = torch.complex(s.cos[p0 : length[i]].double(), s.sin[p0 : length[i]].double())[:, None]
+        x = s.q[a:b].double().view(b - a, c.heads, -1)[:, :, c.nope :]
+        x = torch.cat([x, s.ckr[a:b, None, W:].double()], 1)
+        pair = x.reshape(b - a, -1, c.rope // 2, 2) if c.interleaved else x.reshape(b - a, -1, 2, c.rope // 2).transpose(2, 3)
+        y = torch.view_as_real(torch.view_as_complex(pair.contiguous()) * turn)
+        y = (y if c.interleaved else y.transpose(2, 3)).reshape(b - a, -1, c.rope)
+        queries.append(y[:, :-1])
+        keys.append(_exact_values(y[:, -1], c.rule))
+    return torch.cat(queries), _exact_values(s.ckr[:, :W].double(), c.rule), torch.cat(keys)
+
+
+def _held(s, c, i):
+    """Codes, latent scales and rotary scales of sequence i in the order of its tokens."""
+    n = int(s.length[i])
+    page = s.table[i, : -(-n // c.page)].long()
+    return s.codes[page].flatten(0, 1)[:n], s.scale[page].flatten()[:n], s.rope_scale[page].flatten()[:n]
+
+
+def _exact_read(s, c):
+    got = [_held(s, c, i) for i in range(c.seqs)]
+    return (torch.cat([x[:, : c.latent] for x, _, _ in got]), torch.cat([y.double() for _, y, _ in got]),
+            torch.cat([x[:, c.latent :].double() * z.double()[:, None] for x, _, z in got]))
+
+
+def _exact_latent(s, c):
+    start, length, out = s.start.tolist(), s.length.tolist(), []
+    for i in range(c.seqs):
+        codes, ls, ks = _held(s, c, i)
+        v = codes[:, : c.latent].double() * ls.double()[:, None]
+        k = torch.cat([v, codes[:, c.latent :].double() * ks.double()[:, None]], 1).t().contiguous()
+        for a in range(start[i], start[i + 1]):
+            seen = length[i] - (start[i + 1] - 1 - a)
+            q = torch.cat([s.q[a], s.qr[a]], -1).double()
+            out.append(torch.softmax(torch.matmul(q, k[:, :seen]) * _softmax_scale(c), -1) @ v[:seen])
+    return torch.stack(out)
+
+
+def _exact_expanded(s, c):
+    start, rows = s.start.tolist(), s.kv_start.tolist()
+    out = torch.zeros(s.tokens, c.heads, c.vdim, dtype=torch.float64, device=DEV)
+    q = s.q.view(s.tokens, c.heads, -1)
+    kv = s.kv.view(s.held, c.heads, -1)
+    for i in range(c.seqs):
+        a, b, n = start[i], start[i + 1], rows[i + 1] - rows[i]
+        for h in range(c.heads):
+            k = torch.cat([kv[rows[i] : rows[i + 1], h, : c.nope], s.key[rows[i] : rows[i + 1]]], -1).double()
+            x = torch.matmul(q[a:b, h].double(), k.t().contiguous()) * _softmax_scale(c)
+            x += torch.full_like(x, -math.inf).triu(n - (b - a) + 1)
+            out[a:b, h] = torch.matmul(torch.softmax(x, -1), kv[rows[i] : rows[i + 1], h, c.nope :].double())
+    return out.flatten(1)
+
+
+_EXACT = {"append": _exact_append, "read": _exact_read, "latent": _exact_latent, "expanded": _exact_expanded}
