@@ -193,9 +193,9 @@ def _handles(s):
     s.cache = fx.latent_cache(s.codes, s.scale, s.rope_scale, s.pages, c.page, c.latent, c.rope)
     if c.kind == "append":
         s.rotary = fx.rotary(s.cos, s.sin, s.cos.shape[0], c.rope, c.interleaved)
-        s |= dict(q_out=empty(s.tokens, c.heads, c.rope), latents=empty(s.tokens, c.latent), keys=empty(s.tokens, c.rope))
+        s |= dict(q_out=empty(s.tokens, c.heads, c.rope), latents=empty(s.tokens, c.latent), keys_out=empty(s.tokens, c.rope))
     elif c.kind == "read":
-        s |= dict(rows=empty(s.held, c.latent, dt=torch.int8), steps=empty(s.held, dt=torch.float32), keys=empty(s.held, c.rope))
+        s |= dict(rows=empty(s.held, c.latent, dt=torch.int8), steps=empty(s.held, dt=torch.float32), keys_out=empty(s.held, c.rope))
     else:
         s.out = empty(s.tokens, c.heads, c.latent)
         s.ws_bytes = fx.latent_attention_workspace(s.h, s.cache, s.batch, c.heads)
@@ -219,13 +219,13 @@ def _own_append(s, c, fx):
     rule = fx.SCALE_DFX if c.rule == "dfx" else fx.SCALE_MAX
     fx.latent_append(s.h, s.cache, s.batch, s.rotary, rule, s.ckr, w, s.ckr.data_ptr() + c.latent * size, w,
                      s.q.data_ptr() + c.nope * size, c.heads * d, d, s.q_out, c.heads * c.rope, c.rope, c.heads, s.t)
-    fx.latent_read(s.h, s.cache, s.batch, None, s.tokens, None, 0, None, s.latents, c.latent, s.keys, c.rope, s.t)
-    return s.q_out, s.latents, s.keys
+    fx.latent_read(s.h, s.cache, s.batch, None, s.tokens, None, 0, None, s.latents, c.latent, s.keys_out, c.rope, s.t)
+    return s.q_out, s.latents, s.keys_out
 
 
 def _own_read(s, c, fx):
-    fx.latent_read(s.h, s.cache, s.batch, s.kv_start, s.held, s.rows, c.latent, s.steps, None, 0, s.keys, c.rope, s.t)
-    return s.rows, s.steps, s.keys
+    fx.latent_read(s.h, s.cache, s.batch, s.kv_start, s.held, s.rows, c.latent, s.steps, None, 0, s.keys_out, c.rope, s.t)
+    return s.rows, s.steps, s.keys_out
 
 
 def _own_latent(s, c, fx):
