@@ -730,6 +730,121 @@ fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
                                  int64_t ldo, fxpq_dtype type, void* workspace,
                                  int64_t workspace_bytes);
 
+/* ---- latent attention ------------------------------------------------------ */
+
+/*
+ * Attention whose keys and values come from one latent vector a token, shared by
+ * all heads, beside one rotated key that all heads share too.  Head h's key of
+ * token j is (K_h c_j, r_j), its value V_h c_j.  Two forms give the same result:
+ *   expanded  keys and values of each head are made of the latents by a product
+ *             (fxpq_latent_read hands its operand over) and fxpq_expanded_attention
+ *             runs over them: fewest operations, for prompts;
+ *   absorbed  K_h moves into the query (K_h^T q) and V_h behind the attention, and
+ *             fxpq_latent_attention runs over the latents themselves, which are keys
+ *             and values at once: fewest bytes, for single tokens.
+ * A paged cache of latents in 8-bit codes, a row and two scales a token:
+ *     codes       int8 [pages][page][latent + rope]   the latent's codes, then the
+ *                 shared key's; 16-byte aligned
+ *     scale       float [pages][page]   of the latent: value = code * scale
+ *     rope_scale  float [pages][page]   of the shared key
+ * scales 16-byte aligned, finite and not negative.  latent is 256 or 512, rope 16,
+ * 32, 48 or 64, page as for fxpq_kv_cache.  The memory needs no initialization.
+ */
+typedef struct {
+  int8_t* codes;
+  float* scale;
+  float* rope_scale;
+  int32_t pages, page, latent, rope;
+} fxpq_latent_cache;
+
+/*
+ * Appends the new tokens' latents (rows of `latent` reals, row stride ldc) and
+ * shared keys (rows of `rope` reals, row stride ldr), the key rotated first (rot
+ * nullable: no rotation; else rot->dims == rope), and writes the rotated rotary
+ * part of each query head: `rope` reals at q + token * ldq + head * hdq go to
+ * q_out + token * ldqo + head * hdqo (the same place or one that does not overlap;
+ * q NULL: no queries).  Scales by `rule` (fxpq_scale_rule) and codes are those of
+ * fxpq_token_quantize for the latent's row and for the key's; the rotation is
+ * computed in fp64 and rounded once.  A NaN or an infinity is stored as 0, takes no
+ * part in the scale and raises FXPQ_FLAG_NONFINITE; a token past rot->positions
+ * raises FXPQ_FLAG_RANGE and its sequence is skipped.
+ */
+fxpq_status fxpq_latent_append(fxpq_handle h, const fxpq_latent_cache* cache,
+                               const fxpq_kv_batch* batch, const fxpq_rotary* rot, int32_t rule,
+                               const void* c, int64_t ldc, const void* r, int64_t ldr, const void* q,
+                               int64_t ldq, int64_t hdq, void* q_out, int64_t ldqo, int64_t hdqo,
+                               int32_t q_heads, fxpq_dtype type);
+
+/*
+ * Reads tokens out of the pages.  kv_start (device int32[seqs + 1]): all tokens of
+ * the sequences, token t of sequence s to row kv_start[s] + t, and kv_start[s + 1] -
+ * kv_start[s] has to be length[s], rows below kv_tokens; a sequence for which that
+ * does not hold is skipped and raises FXPQ_FLAG_RANGE.  kv_start NULL: the call's
+ * new tokens only, to their own rows.  Any of the outputs may be NULL:
+ *     codes   int8, row stride ld_codes (a multiple of 16, 16-byte aligned), and
+ *     scale   float, one a row: the latents as fxpq_token_gemm takes them
+ *     latent  reals, row stride ld_latent: code * scale
+ *     key     reals, row stride ld_key: the shared key
+ * A token whose page is outside the cache is read as zeros (FXPQ_FLAG_RANGE).
+ */
+fxpq_status fxpq_latent_read(fxpq_handle h, const fxpq_latent_cache* cache,
+                             const fxpq_kv_batch* batch, const int32_t* kv_start, int32_t kv_tokens,
+                             int8_t* codes, int64_t ld_codes, float* scale, void* latent,
+                             int64_t ld_latent, void* key, int64_t ld_key, fxpq_dtype type);
+
+/*
+ * Absorbed attention of the new tokens' queries over the cache (which holds the
+ * new tokens already):
+ *     o = sum_j softmax_j(softmax_scale * (q . c_j + q_rope . r_j)) c_j
+ * over all tokens of the sequence, or with causal != 0 over those up to the
+ * query's own.  q: `latent` reals of each token and head at token * ldq + head *
+ * hdq, q_rope: `rope` reals at token * ldqr + head * hdqr, out: `latent` reals at
+ * token * ldo + head * hdo (strides in any order; out's rows must not overlap).
+ * A query that sees no token gets 0, one that holds a NaN or an infinity NaN.
+ * workspace as for fxpq_token_gemm.
+ */
+fxpq_status fxpq_latent_attention_workspace(fxpq_handle h, const fxpq_latent_cache* cache,
+                                            const fxpq_kv_batch* batch, int32_t q_heads,
+                                            int64_t* bytes);
+fxpq_status fxpq_latent_attention(fxpq_handle h, const fxpq_latent_cache* cache,
+                                  const fxpq_kv_batch* batch, const void* q, int64_t ldq, int64_t hdq,
+                                  const void* q_rope, int64_t ldqr, int64_t hdqr, int32_t q_heads,
+                                  float softmax_scale, int32_t causal, void* out, int64_t ldo,
+                                  int64_t hdo, fxpq_dtype type, void* workspace,
+                                  int64_t workspace_bytes);
+
+/*
+ * Keys and values of each head in rows of tokens: sequence s has rows start[s] ..
+ * start[s + 1] - 1 (device int32[seqs + 1], as kv_start above), `tokens` rows in
+ * all.  Head h's key: `nope` reals at k + row * ldk + h * hdk beside the shared
+ * `rope` reals at key + row * ld_key; its value: `vdim` reals at v + row * ldv + h *
+ * hdv.  nope and vdim are 64 or 128, rope 32 or 64.
+ */
+typedef struct {
+  const void* k;
+  const void* key;
+  const void* v;
+  int64_t ldk, hdk, ld_key, ldv, hdv;
+  const int32_t* start;
+  int32_t tokens, heads, nope, rope, vdim, pad0;
+} fxpq_expanded_kv;
+
+/*
+ * Expanded attention of the new tokens' queries over such keys and values:
+ *     o_h = sum_j softmax_j(softmax_scale * (q_h[: nope] . k_jh + q_h[nope :] . key_j)) v_jh
+ * over all rows of the sequence, or with causal != 0 over those up to the query's
+ * own (the new tokens are the sequence's last rows).  q: rows of heads * (nope +
+ * rope) reals, row stride ldq; out: rows of heads * vdim reals, row stride ldo.  A
+ * query that sees no token gets 0; keys and values that a query does not see have no
+ * part in its result, whatever they hold.  Of the batch start, length, seqs, tokens,
+ * max_new and max_len are used (table is not, and may be NULL).  A sequence whose
+ * numbers contradict the bounds or kv->start is skipped and raises FXPQ_FLAG_RANGE.
+ */
+fxpq_status fxpq_expanded_attention(fxpq_handle h, const fxpq_expanded_kv* kv,
+                                    const fxpq_kv_batch* batch, const void* q, int64_t ldq,
+                                    float softmax_scale, int32_t causal, void* out, int64_t ldo,
+                                    fxpq_dtype type);
+
 /* ---- measurement --------------------------------------------------------- */
 
 /* Kernels the handle can time with HIP events on its stream. */

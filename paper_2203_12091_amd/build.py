@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfxpq.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["fxpq_api.hip", "k_stream.hip", "k_flsearch.hip", "k_conv.hip", "k_pred.hip",
-           "k_teacher.hip", "k_wide.hip", "k_token.hip", "k_cache.hip", "k_attn.hip"]
+           "k_teacher.hip", "k_wide.hip", "k_token.hip", "k_cache.hip", "k_attn.hip",
+           "k_latent.hip", "k_latent_attn.hip", "k_expanded.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include")]

@@ -155,6 +155,36 @@ bool batch_ok(const fxpq_kv_batch* b, const fxpq_kv_cache* c) {
          (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
 }
 
+// The batch's numbers, for pages of `page` tokens.
+bool batch_sizes_ok(const fxpq_kv_batch* b) {
+  return b && b->start && b->length && aligned(b->start, 4) && aligned(b->length, 4) && b->seqs >= 1 &&
+         b->seqs <= 65535 && b->tokens >= 0 && b->max_new >= 0 && b->max_new <= b->tokens &&
+         (b->max_new > 0 || b->tokens == 0) && b->max_new <= (1 << 24) && b->max_len >= b->max_new &&
+         b->max_len <= (1 << 30);
+}
+
+bool latent_ok(const fxpq_latent_cache* c) {
+  return c && c->codes && c->scale && c->rope_scale && aligned(c->codes, 16) && aligned(c->scale, 16) &&
+         aligned(c->rope_scale, 16) && c->pages >= 1 &&
+         (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) &&
+         (c->latent == 256 || c->latent == 512) && c->rope >= 16 && c->rope <= 64 && c->rope % 16 == 0;
+}
+
+bool latent_batch_ok(const fxpq_kv_batch* b, const fxpq_latent_cache* c) {
+  return batch_sizes_ok(b) && b->table && aligned(b->table, 4) && b->table_ld >= 1 &&
+         (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
+}
+
+// Rows of `width` at token * ld + head * hd that do not overlap.
+bool apart(int64_t tokens, int64_t heads, int64_t width, int64_t ld, int64_t hd) {
+  return ld >= width && hd >= width && ld <= (INT64_C(1) << 40) && hd <= (INT64_C(1) << 40) &&
+         (ld >= (heads - 1) * hd + width || hd >= (tokens - 1) * ld + width);
+}
+
+bool latent_heads_ok(int heads, const fxpq_kv_batch* b) {
+  return heads >= 1 && heads <= kMaxHeads && (int64_t)b->max_new * heads < (1 << 30);
+}
+
 bool heads_ok(int q_heads, const fxpq_kv_cache* c, const fxpq_kv_batch* b) {
   return q_heads >= 1 && q_heads <= kMaxHeads && q_heads % c->heads == 0 &&
          (int64_t)b->max_new * (q_heads / c->heads) < (1 << 30);
@@ -1049,6 +1079,136 @@ fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
   DeviceGuard g(h->device);
   return hip_status(launch_cache_attention(ctx(h), *cache, *batch, q, ldq, q_heads, softmax_scale, causal,
                                            out, ldo, type, workspace));
+}
+
+fxpq_status fxpq_latent_append(fxpq_handle h, const fxpq_latent_cache* cache,
+                               const fxpq_kv_batch* batch, const fxpq_rotary* rot, int32_t rule,
+                               const void* c, int64_t ldc, const void* r, int64_t ldr, const void* q,
+                               int64_t ldq, int64_t hdq, void* q_out, int64_t ldqo, int64_t hdqo,
+                               int32_t q_heads, fxpq_dtype type) {
+  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (rule != FXPQ_SCALE_MAX && rule != FXPQ_SCALE_DFX) return FXPQ_ERR_INVALID_ARG;
+  if (ldc < cache->latent || ldr < cache->rope) return FXPQ_ERR_INVALID_ARG;
+  if (rot && (rot->dims != cache->rope || rot->positions < 0 || !rot->cos || !rot->sin ||
+              !aligned(rot->cos, 4) || !aligned(rot->sin, 4)))
+    return FXPQ_ERR_INVALID_ARG;
+  const int size = real_bytes(type);
+  if (q) {
+    if (q_heads < 1 || q_heads > kMaxHeads || !q_out || !aligned(q, size) || !aligned(q_out, size) ||
+        ldq < cache->rope || hdq < cache->rope || !apart(batch->tokens, q_heads, cache->rope, ldqo, hdqo) ||
+        (q == q_out && (ldq != ldqo || hdq != hdqo)))
+      return FXPQ_ERR_INVALID_ARG;
+  }
+  if (batch->tokens == 0) return FXPQ_OK;
+  if (!c || !r || !aligned(c, size) || !aligned(r, size)) return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  LatentAppendArgs a{};
+  a.c = *cache;
+  a.b = *batch;
+  if (rot) a.rot = *rot;
+  a.rule = rule;
+  a.latent = c;
+  a.key = r;
+  a.q = q;
+  a.q_out = q_out;
+  a.ldc = ldc;
+  a.ldr = ldr;
+  a.ldq = ldq;
+  a.hdq = hdq;
+  a.ldqo = ldqo;
+  a.hdqo = hdqo;
+  a.heads = q ? q_heads : 0;
+  a.flags = h->sc.flags;
+  return hip_status(launch_latent_append(ctx(h), a, type));
+}
+
+fxpq_status fxpq_latent_read(fxpq_handle h, const fxpq_latent_cache* cache,
+                             const fxpq_kv_batch* batch, const int32_t* kv_start, int32_t kv_tokens,
+                             int8_t* codes, int64_t ld_codes, float* scale, void* latent,
+                             int64_t ld_latent, void* key, int64_t ld_key, fxpq_dtype type) {
+  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (kv_start ? kv_tokens < 0 || !aligned(kv_start, 4) : kv_tokens != batch->tokens) return FXPQ_ERR_INVALID_ARG;
+  if ((codes && (!aligned(codes, 16) || ld_codes < cache->latent || ld_codes % 16 != 0)) ||
+      (latent && ld_latent < cache->latent) || (key && ld_key < cache->rope))
+    return FXPQ_ERR_INVALID_ARG;
+  if (!aligned(scale, 4) || !aligned(latent, real_bytes(type)) || !aligned(key, real_bytes(type)))
+    return FXPQ_ERR_INVALID_ARG;
+  if (kv_tokens == 0 || (!codes && !scale && !latent && !key)) return FXPQ_OK;
+  DeviceGuard g(h->device);
+  LatentReadArgs a{*cache, *batch, kv_start, kv_tokens, codes, scale, latent, key, ld_codes, ld_latent, ld_key,
+                   h->sc.flags};
+  return hip_status(launch_latent_read(ctx(h), a, type));
+}
+
+fxpq_status fxpq_latent_attention_workspace(fxpq_handle h, const fxpq_latent_cache* cache,
+                                            const fxpq_kv_batch* batch, int32_t q_heads,
+                                            int64_t* bytes) {
+  if (!bytes) return FXPQ_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (!h || !latent_ok(cache) || !latent_batch_ok(batch, cache) || !latent_heads_ok(q_heads, batch))
+    return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens > 0) *bytes = latent_attention_workspace(ctx(h), *cache, *batch, q_heads);
+  return FXPQ_OK;
+}
+
+fxpq_status fxpq_latent_attention(fxpq_handle h, const fxpq_latent_cache* cache,
+                                  const fxpq_kv_batch* batch, const void* q, int64_t ldq, int64_t hdq,
+                                  const void* q_rope, int64_t ldqr, int64_t hdqr, int32_t q_heads,
+                                  float softmax_scale, int32_t causal, void* out, int64_t ldo,
+                                  int64_t hdo, fxpq_dtype type, void* workspace,
+                                  int64_t workspace_bytes) {
+  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache) ||
+      !latent_heads_ok(q_heads, batch) || !isfinite(softmax_scale))
+    return FXPQ_ERR_INVALID_ARG;
+  if (ldq < cache->latent || hdq < cache->latent || ldqr < cache->rope || hdqr < cache->rope ||
+      !apart(batch->tokens, q_heads, cache->latent, ldo, hdo))
+    return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens == 0) return FXPQ_OK;
+  const int size = real_bytes(type);
+  if (!q || !q_rope || !out || !aligned(q, size) || !aligned(q_rope, size) || !aligned(out, size))
+    return FXPQ_ERR_INVALID_ARG;
+  const int64_t need = latent_attention_workspace(ctx(h), *cache, *batch, q_heads);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  LatentArgs a{};
+  a.c = *cache;
+  a.b = *batch;
+  a.q = q;
+  a.qr = q_rope;
+  a.out = out;
+  a.ldq = ldq;
+  a.hdq = hdq;
+  a.ldqr = ldqr;
+  a.hdqr = hdqr;
+  a.ldo = ldo;
+  a.hdo = hdo;
+  a.heads = q_heads;
+  a.causal = causal ? 1 : 0;
+  a.scale = softmax_scale;
+  return hip_status(launch_latent_attention(ctx(h), a, type, workspace));
+}
+
+fxpq_status fxpq_expanded_attention(fxpq_handle h, const fxpq_expanded_kv* kv,
+                                    const fxpq_kv_batch* batch, const void* q, int64_t ldq,
+                                    float softmax_scale, int32_t causal, void* out, int64_t ldo,
+                                    fxpq_dtype type) {
+  if (!h || !is_real(type) || !kv || !batch_sizes_ok(batch) || !isfinite(softmax_scale)) return FXPQ_ERR_INVALID_ARG;
+  if ((kv->nope != 64 && kv->nope != 128) || (kv->vdim != 64 && kv->vdim != 128) ||
+      (kv->rope != 32 && kv->rope != 64) || kv->heads < 1 || kv->heads > kMaxHeads || kv->tokens < 0)
+    return FXPQ_ERR_INVALID_ARG;
+  if (kv->ldk < kv->nope || kv->hdk < kv->nope || kv->ldv < kv->vdim || kv->hdv < kv->vdim ||
+      kv->ld_key < kv->rope || ldq < (int64_t)kv->heads * (kv->nope + kv->rope) ||
+      ldo < (int64_t)kv->heads * kv->vdim)
+    return FXPQ_ERR_INVALID_ARG;
+  if (batch->tokens == 0) return FXPQ_OK;
+  const int size = real_bytes(type);
+  if (!q || !out || !kv->k || !kv->key || !kv->v || !kv->start || !aligned(kv->start, 4) || !aligned(q, size) ||
+      !aligned(out, size) || !aligned(kv->k, size) || !aligned(kv->key, size) || !aligned(kv->v, size))
+    return FXPQ_ERR_INVALID_ARG;
+  DeviceGuard g(h->device);
+  ExpandedArgs a{*kv, *batch, q, out, ldq, ldo, causal ? 1 : 0, softmax_scale};
+  return hip_status(launch_expanded_attention(ctx(h), a, type));
 }
 
 fxpq_status fxpq_timer_start(fxpq_handle h, fxpq_timer_kind kind) {

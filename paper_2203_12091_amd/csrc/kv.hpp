@@ -14,14 +14,19 @@ struct SeqDev {
   bool ok;
 };
 
-__device__ inline SeqDev seq_of(const fxpq_kv_batch& b, int page, int s) {
+__device__ inline SeqDev seq_of(const fxpq_kv_batch& b, int s) {
   SeqDev q;
   q.first = b.start[s];
   const int end = b.start[s + 1];
   q.len = b.length[s];
   q.fresh = end - q.first;
   q.ok = q.first >= 0 && end >= q.first && end <= b.tokens && q.fresh <= b.max_new && q.len >= q.fresh &&
-         q.len <= b.max_len && (q.len + page - 1) / page <= b.table_ld;
+         q.len <= b.max_len;
+  return q;
+}
+__device__ inline SeqDev seq_of(const fxpq_kv_batch& b, int page, int s) {
+  SeqDev q = seq_of(b, s);
+  q.ok = q.ok && (q.len + page - 1) / page <= b.table_ld;
   return q;
 }
 
@@ -32,6 +37,11 @@ __device__ inline int64_t k_offset(const fxpq_kv_cache& c, int page, int head, i
 }
 __device__ inline int64_t v_offset(const fxpq_kv_cache& c, int page, int head, int slot, int d) {
   return (((int64_t)page * c.heads + head) * c.page + (slot & ~15)) * c.dim + d * 16 + (slot & 15);
+}
+
+// First byte of token slot `slot` of a page of latents.
+__device__ inline int64_t latent_offset(const fxpq_latent_cache& c, int page, int slot) {
+  return ((int64_t)page * c.page + slot) * (c.latent + c.rope);
 }
 
 }  // namespace fxpq

@@ -112,4 +112,55 @@ hipError_t launch_cache_attention(const Ctx& c, const fxpq_kv_cache& cache, cons
                                   const void* q, int64_t ldq, int q_heads, float softmax_scale,
                                   int causal, void* out, int64_t ldo, int type, void* ws);
 
+// Absorbed attention's arguments: row = new token * heads + head of a sequence.
+struct LatentArgs {
+  fxpq_latent_cache c;
+  fxpq_kv_batch b;
+  const void* q;
+  const void* qr;
+  void* out;
+  int64_t ldq, hdq, ldqr, hdqr, ldo, hdo;
+  int heads, causal;
+  float scale;
+};
+struct ExpandedArgs {
+  fxpq_expanded_kv kv;
+  fxpq_kv_batch b;
+  const void* q;
+  void* out;
+  int64_t ldq, ldo;
+  int causal;
+  float scale;
+};
+struct LatentAppendArgs {
+  fxpq_latent_cache c;
+  fxpq_kv_batch b;
+  fxpq_rotary rot;  // dims 0: no rotation
+  int rule;
+  const void* latent;
+  const void* key;
+  const void* q;
+  void* q_out;
+  int64_t ldc, ldr, ldq, hdq, ldqo, hdqo;
+  int heads;
+  unsigned* flags;
+};
+struct LatentReadArgs {
+  fxpq_latent_cache c;
+  fxpq_kv_batch b;
+  const int32_t* kv_start;
+  int kv_tokens;
+  int8_t* codes;
+  float* scale;
+  void* latent;
+  void* key;
+  int64_t ld_codes, ld_latent, ld_key;
+  unsigned* flags;
+};
+hipError_t launch_latent_append(const Ctx& c, LatentAppendArgs a, int type);
+hipError_t launch_latent_read(const Ctx& c, LatentReadArgs a, int type);
+int64_t latent_attention_workspace(const Ctx& c, const fxpq_latent_cache& cache, const fxpq_kv_batch& b, int heads);
+hipError_t launch_latent_attention(const Ctx& c, const LatentArgs& a, int type, void* ws);
+hipError_t launch_expanded_attention(const Ctx& c, const ExpandedArgs& a, int type);
+
 }  // namespace fxpq

@@ -31,6 +31,8 @@ EXPORTS = [
     "fxpq_token_quantize", "fxpq_token_gemm_workspace", "fxpq_token_gemm", "fxpq_expert_gemm",
     "fxpq_cache_append", "fxpq_cache_read", "fxpq_cache_attention_workspace",
     "fxpq_cache_attention",
+    "fxpq_latent_append", "fxpq_latent_read", "fxpq_latent_attention_workspace",
+    "fxpq_latent_attention", "fxpq_expanded_attention",
 ]
 TIMER_OFF, TIMER_FLS_WINDOW, TIMER_QCONV, TIMER_REQUANT, TIMER_CBLOCK_PASS, TIMER_CBLOCK_PRED = range(6)
 TILING_AUTO, TILING_GEMM, TILING_HALO = range(3)
@@ -74,6 +76,17 @@ class KvBatch(C.Structure):
 class Rotary(C.Structure):
     _fields_ = ([(f, C.c_void_p) for f in ("cos", "sin")]
                 + [(f, C.c_int32) for f in ("positions", "dims", "interleaved", "pad0")])
+
+
+class LatentCache(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("codes", "scale", "rope_scale")]
+                + [(f, C.c_int32) for f in ("pages", "page", "latent", "rope")])
+
+
+class ExpandedKv(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("k", "key", "v")]
+                + [(f, C.c_int64) for f in ("ldk", "hdk", "ld_key", "ldv", "hdv")] + [("start", C.c_void_p)]
+                + [(f, C.c_int32) for f in ("tokens", "heads", "nope", "rope", "vdim", "pad0")])
 
 
 class FxpqError(RuntimeError):
@@ -142,6 +155,12 @@ def lib():
             "fxpq_cache_read": [p, p, p, p, p, C.c_int],
             "fxpq_cache_attention_workspace": [p, p, p, i32, p],
             "fxpq_cache_attention": [p, p, p, p, i64, i32, C.c_float, i32, p, i64, C.c_int, p, i64],
+            "fxpq_latent_append": [p, p, p, p, i32, p, i64, p, i64, p, i64, i64, p, i64, i64, i32, C.c_int],
+            "fxpq_latent_read": [p, p, p, p, i32, p, i64, p, p, i64, p, i64, C.c_int],
+            "fxpq_latent_attention_workspace": [p, p, p, i32, p],
+            "fxpq_latent_attention": [p, p, p, p, i64, i64, p, i64, i64, i32, C.c_float, i32, p, i64, i64,
+                                      C.c_int, p, i64],
+            "fxpq_expanded_attention": [p, p, p, p, i64, C.c_float, i32, p, i64, C.c_int],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -404,6 +423,35 @@ def cache_attention(h, cache, batch, q, ldq, q_heads, scale, causal, out, ldo, x
           scale, int(causal), ptr(out), ldo, x_type, ptr(workspace), ws_bytes)
 
 
+def latent_append(h, cache, batch, rot, rule, c, ldc, r, ldr, q, ldq, hdq, q_out, ldqo, hdqo, q_heads, x_type):
+    _call("fxpq_latent_append", h.value, C.byref(cache), C.byref(batch),
+          C.byref(rot) if rot is not None else None, rule, ptr(c), ldc, ptr(r), ldr, ptr(q), ldq, hdq,
+          ptr(q_out), ldqo, hdqo, q_heads, x_type)
+
+
+def latent_read(h, cache, batch, kv_start, kv_tokens, codes, ld_codes, scale, latent, ld_latent, key, ld_key, x_type):
+    _call("fxpq_latent_read", h.value, C.byref(cache), C.byref(batch), ptr(kv_start), kv_tokens, ptr(codes),
+          ld_codes, ptr(scale), ptr(latent), ld_latent, ptr(key), ld_key, x_type)
+
+
+def latent_attention_workspace(h, cache, batch, q_heads):
+    b = C.c_int64(0)
+    _call("fxpq_latent_attention_workspace", h.value, C.byref(cache), C.byref(batch), q_heads,
+          C.byref(b))
+    return b.value
+
+
+def latent_attention(h, cache, batch, q, ldq, hdq, q_rope, ldqr, hdqr, q_heads, scale, causal, out, ldo, hdo,
+                     x_type, workspace=None, ws_bytes=0):
+    _call("fxpq_latent_attention", h.value, C.byref(cache), C.byref(batch), ptr(q), ldq, hdq, ptr(q_rope),
+          ldqr, hdqr, q_heads, scale, int(causal), ptr(out), ldo, hdo, x_type, ptr(workspace), ws_bytes)
+
+
+def expanded_attention(h, kv, batch, q, ldq, scale, causal, out, ldo, x_type):
+    _call("fxpq_expanded_attention", h.value, C.byref(kv), C.byref(batch), ptr(q), ldq, scale, int(causal),
+          ptr(out), ldo, x_type)
+
+
 def timer_start(h, kind):
     _call("fxpq_timer_start", h.value, kind)
 
@@ -470,3 +518,14 @@ def kv_batch(start, length, table, seqs, table_ld, tokens, max_new, max_len):
 def rotary(cos, sin, positions, dims, interleaved=0):
     return _keep(Rotary(cos=ptr(cos), sin=ptr(sin), positions=positions, dims=dims,
                         interleaved=int(interleaved)), cos, sin)
+
+
+def latent_cache(codes, scale, rope_scale, pages, page, latent, rope):
+    return _keep(LatentCache(codes=ptr(codes), scale=ptr(scale), rope_scale=ptr(rope_scale), pages=pages,
+                             page=page, latent=latent, rope=rope), codes, scale, rope_scale)
+
+
+def expanded_kv(k, ldk, hdk, key, ld_key, v, ldv, hdv, start, tokens, heads, nope, rope, vdim):
+    return _keep(ExpandedKv(k=ptr(k), ldk=ldk, hdk=hdk, key=ptr(key), ld_key=ld_key, v=ptr(v), ldv=ldv,
+                            hdv=hdv, start=ptr(start), tokens=tokens, heads=heads, nope=nope, rope=rope,
+                            vdim=vdim), k, key, v, start)
