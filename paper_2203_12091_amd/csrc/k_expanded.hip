@@ -249,7 +249,9 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
       for (int i = 1; i < N; ++i) top = fmaxf(top, x[c][i]);
       top *= f;
       if (__any(top > m[c] + kSlack)) {
-        const float now = fmaxf(m[c], over_groups(top)), down = __builtin_amdgcn_exp2f(m[c] - now);
+        // row by row: what one row sees has no part in its neighbours' rounding
+        const float row_top = over_groups(top), now = row_top > m[c] + kSlack ? row_top : m[c];
+        const float down = __builtin_amdgcn_exp2f(m[c] - now);
         m[c] = now;
         l[c] *= down;
 #pragma unroll

@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256, RT == 1 && sizeof(T) == 2 ? 2 : 1) void k_late
         const float y = fmaxf(fmaxf(tops[at], tops[kRows + at]), fmaxf(tops[2 * kRows + at], tops[3 * kRows + at]));
         // what came before weighs `ratio` of what it did against the new R
         const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
-        const float now = fmaxf(before, y), down = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
+        const float now = y > before + kSlack ? y : before, down = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
         m[r] = now;
         l[r] *= down;
         const float f = down * ratio;
