@@ -2,13 +2,16 @@
 // rotary key that all heads share.
 //
 // A block of four waves takes 64 NC query rows of one head over the keys, kTok at a
-// time, which it stages in LDS: a key's nope and rotary parts side by side, values
-// transposed, dimension by dimension, their tokens next to each other.  Wave by wave
-// S = K Q^T with 16 NC rows of q in registers, then O^T = V^T P^T.  LDS row 16 t + i of
-// the keys is token 4 TT (i / 4) + 4 t + i % 4 (TT: 16-row tiles of a chunk), so that the
-// lane that holds S for a query row has the 4 TT neighbouring tokens that its operand of the
-// second product needs: P goes from the first product's result into it without leaving
-// the lane.
+// time: two LDS buffers, filled straight from memory while the other one is worked on.
+// Wave by wave S = K Q^T with 16 NC rows of q in registers, then O^T = V^T P^T.  A lane
+// holds S for one query row and tokens 4 g .. 4 g + 3 of each 16-token tile; two tiles of
+// them are its operand of the second product as they are, so P never leaves the lane.
+// V's operand is its transpose: the hardware's transposed LDS read hands a lane four
+// tokens of one dimension (f32 reads them one by one).
+//
+// LDS holds panels of 128 bytes a token: keys' nope part, rotary part, values.  Within a
+// panel's row the 16-byte pieces are swapped by the token's number, by the address that
+// each lane loads from, so that reads of 16 rows cover all banks.
 //
 // f16 and bf16 multiply as they are, P rounded to the same type (bf16: 2^-9 a weight, which
 // leaves the whole result's error at 1.3 times that of its own rounding; f16 with weights
@@ -17,6 +20,7 @@
 #include <type_traits>
 
 #include "kv.hpp"
+#include "ring.hpp"
 #include "values.hpp"
 
 namespace fxpq {
@@ -46,7 +50,7 @@ constexpr float kFar = 0x1p24f;  // references up to this leave an error below 1
 
 struct ExpandedRun {
   ExpandedArgs a;
-  int row_tiles, vec, vec_out;
+  int row_tiles, vec, vec_out;  // vec: rows are 16-byte aligned and near enough for 32-bit offsets
   unsigned* flags;
 };
 
@@ -62,30 +66,87 @@ __device__ inline float over_groups(float x) {
 template <typename T>
 __device__ inline bool real_finite(T x) { return finite((float)x); }
 
-// D: dimensions of a query and key (nope + rope); VD: of a value; NC: 16-row tiles of a wave.
+// Panels of 128 bytes of a token's row, and a piece's place in its row.
+template <typename T>
+struct Panels {
+  static constexpr int kDims = 128 / (int)sizeof(T);
+  static constexpr int of(int dims) { return (dims + kDims - 1) / kDims; }
+  static constexpr int kBytes = Operand<T>::kTok * 128;
+};
+__device__ inline int key_swap(int tok) { return (tok >> 1) & 7; }
+template <typename T>
+__device__ inline int value_swap(int tok) {
+  return sizeof(T) == 4 ? ((tok >> 2) & 1) << 2 : ((tok >> 1) & 3) << 1;
+}
+
+// A thread's piece of each panel, real by real.
+template <typename T>
+__device__ inline void copy_pieces(const int8_t* from, int panels, int8_t* to) {
+  constexpr int kPiece = 16 / (int)sizeof(T);
+#pragma unroll 1
+  for (int q = 0; q < panels; ++q) {
+    const T* src = reinterpret_cast<const T*>(from + q * 128);
+    Reals<T, kPiece> x;
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) x.v[k] = src[k];
+    *reinterpret_cast<Reals<T, kPiece>*>(to + q * Panels<T>::kBytes) = x;
+  }
+}
+
+// Eight tokens of one dimension: tokens 4 g + 0..3 of the 16-token tiles 2 u and 2 u + 1,
+// dimension 16 j + n.
+template <typename T>
+__device__ inline typename Operand<T>::v8 value_operand(const int8_t* vl, int u, int j, int g, int n) {
+  typename Operand<T>::v8 v;
+  if constexpr (sizeof(T) == 4) {
+    const int piece = (j & 1) * 4 + (n >> 2);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int tok = 32 * u + 16 * (k >> 2) + 4 * g + (k & 3);
+      v[k] = *reinterpret_cast<const float*>(vl + (j >> 1) * Panels<T>::kBytes + tok * 128 +
+                                             ((piece ^ value_swap<T>(tok)) << 4) + (n & 3) * 4);
+    }
+  } else {
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s* lds_v4s;
+    v4s part[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // lane n points at token n / 4 of the four, dimensions 4 (n % 4) .. + 3
+      const int tok = 32 * u + 16 * k + 4 * g + (n >> 2), piece = (j & 3) * 2 + ((n >> 1) & 1);
+      const int8_t* at = vl + (j >> 2) * Panels<T>::kBytes + tok * 128 + ((piece ^ value_swap<T>(tok)) << 4) + (n & 1) * 8;
+      part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uint32_t)(uintptr_t)at);
+    }
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    v = __builtin_bit_cast(typename Operand<T>::v8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  return v;
+}
+
+// D: dimensions of a query and key (nope + rope: up to 128 64 + 32 or 64, else 128 + 32 or 64); VD: of a value; NC: 16-row tiles of a wave.
 template <typename T, int D, int VD, int NC>
-__global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
+__global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun p) {
   typedef typename Operand<T>::v8 v8;
   constexpr int kTok = Operand<T>::kTok, TT = kTok / 16, S = sizeof(T);
   constexpr int kSteps = D / 32, DT = VD / 16;
   constexpr int kRows = NC * 64;
-  constexpr int kKRow = D * S + 16, kVRow = kTok * S + 16;  // LDS bytes of a key, of a value dimension; the pads spread the banks
-  constexpr int kPiece = 16 / S;                            // reals of a 16-byte piece
-  constexpr int kKPieces = kTok * D / kPiece / 256;         // a thread's share of a chunk's keys
-  constexpr int kVCols = VD / 32;                           // value dimensions of a thread, for 8 tokens at 256 / 32 groups
+  constexpr int kPiece = 16 / S;  // reals of a 16-byte piece
+  typedef Panels<T> Pan;
+  constexpr int KP = Pan::of(D), VP = Pan::of(VD), kStage = (KP + VP) * Pan::kBytes;
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
-  int8_t* kl = lds;
-  int8_t* vl = lds + kTok * kKRow;
-  volatile unsigned* wild = reinterpret_cast<volatile unsigned*>(vl + VD * kVRow);  // [2]: tokens of a chunk with a NaN or an infinity in a value
-  const ExpandedArgs& a = p.a;
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned heads = (unsigned)a.kv.heads, rest = blockIdx.x / heads;
+  // copies of the arguments: the loads below are opaque to the compiler
+  const int64_t ldk = p.a.kv.ldk, ldr = p.a.kv.ld_key, ldv = p.a.kv.ldv;
+  const bool vec = p.vec;
+  const float scale = p.a.scale;
+  const int causal = p.a.causal;
+  const unsigned heads = (unsigned)p.a.kv.heads, rest = blockIdx.x / heads;
   const int head = (int)(blockIdx.x % heads), seq = (int)(rest / (unsigned)p.row_tiles);
   const int tile = p.row_tiles - 1 - (int)(rest % (unsigned)p.row_tiles);  // the last rows see the most tokens: first
-  const SeqDev s = seq_of(a.b, seq);
-  const int from = a.kv.start[seq], to = a.kv.start[seq + 1];
-  if (!s.ok || from < 0 || to < from || to - from != s.len || to > a.kv.tokens) {
+  const SeqDev s = block_seq(seq_of(p.a.b, seq));
+  const int from = __builtin_amdgcn_readfirstlane(p.a.kv.start[seq]), to = __builtin_amdgcn_readfirstlane(p.a.kv.start[seq + 1]);
+  if (!s.ok || from < 0 || to < from || to - from != s.len || to > p.a.kv.tokens) {
     if (tile == 0 && head == 0 && threadIdx.x == 0) raise_flag(p.flags, FXPQ_FLAG_RANGE);
     return;
   }
@@ -93,23 +154,64 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
   if (row0 >= s.fresh) return;
   const int pos0 = s.len - s.fresh;
   const int last = min(row0 + kRows, s.fresh) - 1;
-  const int end = ((a.causal ? pos0 + last : s.len - 1) + kTok) / kTok;
+  const int end = ((causal ? pos0 + last : s.len - 1) + kTok) / kTok;
   const int wrow = row0 + wave * NC * 16;
   const int wlast = min(wrow + NC * 16, s.fresh) - 1;
-  const int wave_end = wlast < wrow ? 0 : ((a.causal ? pos0 + wlast : s.len - 1) + kTok) / kTok;
-  const float sign = a.scale < 0.0f ? -1.0f : 1.0f, f_log2 = a.scale * sign * 1.44269504088896340736f;
+  const int wave_end = wlast < wrow ? 0 : ((causal ? pos0 + wlast : s.len - 1) + kTok) / kTok;
 
+  // A chunk's pieces: thread tid loads piece tid % 8 of rows tid / 8 and 32 on, panel by panel.
+  constexpr int nope_panels = (D > 128 ? 128 : 64) / Pan::kDims, kRope = D > 128 ? D - 128 : D - 64;
+  const int8_t* keys = reinterpret_cast<const int8_t*>(static_cast<const T*>(p.a.kv.k) + from * ldk + head * p.a.kv.hdk);
+  const int8_t* shared = reinterpret_cast<const int8_t*>(static_cast<const T*>(p.a.kv.key) + from * ldr);
+  const int8_t* values = reinterpret_cast<const int8_t*>(static_cast<const T*>(p.a.kv.v) + from * ldv + head * p.a.kv.hdv);
+  const int trow = (int)threadIdx.x >> 3;
+  const int kpiece = ((int)threadIdx.x & 7) ^ key_swap(trow), vpiece = ((int)threadIdx.x & 7) ^ value_swap<T>(trow);
+  // a rotary part of half a panel: its first half twice
+  const int rpiece = kRope * S < 128 ? kpiece & 3 : kpiece;
+  auto load = [&](int chunk, int buf) __attribute__((always_inline)) {
+    int8_t* to_lds = lds + buf * kStage + wave * 1024;
+    const int64_t row_at = (int64_t)chunk * kTok;
+    // past the sequence's end its last row, which nobody looks at there
+    const int most = s.len - 1 - chunk * kTok;
+#pragma unroll
+    for (int half = 0; half < kTok / 32; ++half) {
+      const int r = min(trow + 32 * half, most);
+      if (vec) {
+        const uint32_t ko = (uint32_t)r * (uint32_t)(ldk * S) + kpiece * 16;
+        const uint32_t ro = (uint32_t)r * (uint32_t)(ldr * S) + rpiece * 16;
+        const uint32_t vo = (uint32_t)r * (uint32_t)(ldv * S) + vpiece * 16;
+#pragma unroll
+        for (int q = 0; q < KP; ++q) {
+          int8_t* l = to_lds + q * Pan::kBytes + half * 4096;
+          if (q < nope_panels) dma16(keys + row_at * ldk * S + q * 128, ko, l);
+          else dma16(shared + row_at * ldr * S + (q - nope_panels) * 128, ro, l);
+        }
+#pragma unroll
+        for (int q = 0; q < VP; ++q)
+          dma16(values + row_at * ldv * S + q * 128, vo, to_lds + (KP + q) * Pan::kBytes + half * 4096);
+      } else {
+        const int64_t row = row_at + r;
+        copy_pieces<T>(keys + (row * ldk * S + kpiece * 16), nope_panels, to_lds + half * 4096 + lane * 16);
+        copy_pieces<T>(shared + (row * ldr * S + rpiece * 16), KP - nope_panels,
+                       to_lds + nope_panels * Pan::kBytes + half * 4096 + lane * 16);
+        copy_pieces<T>(values + (row * ldv * S + vpiece * 16), VP, to_lds + KP * Pan::kBytes + half * 4096 + lane * 16);
+      }
+    }
+  };
+  load(0, 0);
+
+  const float sign = scale < 0.0f ? -1.0f : 1.0f, f_log2 = scale * sign * 1.44269504088896340736f;
   v8 q[NC][kSteps];  // lane: row n of tile c, dimensions 32 b + 8 g + 0..7
   int limit[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int row = wrow + c * 16 + n;
-    limit[c] = a.causal ? pos0 + row : s.len - 1;
-    const T* at = static_cast<const T*>(a.q) + (s.first + (int64_t)min(row, s.fresh - 1)) * a.ldq + (int64_t)head * D + 8 * g;
+    limit[c] = causal ? pos0 + row : s.len - 1;
+    const T* at = static_cast<const T*>(p.a.q) + (s.first + (int64_t)min(row, s.fresh - 1)) * p.a.ldq + (int64_t)head * D + 8 * g;
 #pragma unroll
     for (int b = 0; b < kSteps; ++b) {
       float x[8];
-      if (p.vec) {
+      if (vec) {
 #pragma unroll
         for (int k = 0; k < 8; k += kPiece) {
           float u[kPiece];
@@ -136,102 +238,41 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
 #pragma unroll
     for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
   }
-  const int first_limit = a.causal ? pos0 + wrow : s.len - 1;
-  const int block_limit = a.causal ? pos0 + row0 : s.len - 1;
+  const int first_limit = causal ? pos0 + wrow : s.len - 1;
+  constexpr float kLift = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
 
-  // This thread's share of a chunk: pieces of keys, and kVCols dimensions of tokens
-  // (kTok / 8) groups of 8 (f32: 4 groups, of twice the dimensions).
-  constexpr int kVGroups = kTok / 8, kVThreads = 256 / kVGroups, kCols = VD / kVThreads;
-  static_assert(kCols * kVThreads == VD && kKPieces * 256 * kPiece == kTok * D, "whole shares");
-  typedef Reals<T, kPiece> Piece;
-  typedef Reals<T, kCols> Cols;
-  Piece kr[kKPieces];
-  Cols vr[8];
-  const T* keys = static_cast<const T*>(a.kv.k) + (int64_t)head * a.kv.hdk;
-  const T* shared = static_cast<const T*>(a.kv.key);
-  const T* values = static_cast<const T*>(a.kv.v) + (int64_t)head * a.kv.hdv;
-  const int vg = threadIdx.x / kVThreads, vc = threadIdx.x % kVThreads * kCols;
-  auto load = [&](int chunk) {
-    // past the sequence's end its last row, which nobody looks at there
-#pragma unroll
-    for (int i = 0; i < kKPieces; ++i) {
-      const int at = i * 256 + (int)threadIdx.x, tok = at / (D / kPiece), d = at % (D / kPiece) * kPiece;
-      const int64_t row = from + (int64_t)min(chunk * kTok + tok, s.len - 1);
-      const T* src = d < a.kv.nope ? keys + row * a.kv.ldk + d : shared + row * a.kv.ld_key + (d - a.kv.nope);
-      if (p.vec) {
-        kr[i] = *reinterpret_cast<const Piece*>(src);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kPiece; ++k) kr[i].v[k] = src[k];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t row = from + (int64_t)min(chunk * kTok + vg * 8 + j, s.len - 1);
-      const T* src = values + row * a.kv.ldv + vc;
-      if (p.vec) {
-        vr[j] = *reinterpret_cast<const Cols*>(src);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k) vr[j].v[k] = src[k];
-      }
-    }
-  };
-  auto store = [&](int chunk) {
-#pragma unroll
-    for (int i = 0; i < kKPieces; ++i) {
-      const int at = i * 256 + (int)threadIdx.x, tok = at / (D / kPiece), piece = at % (D / kPiece);
-      const int r = tok & 3, t = tok / 4 % TT, i4 = tok / (4 * TT);
-      *reinterpret_cast<Piece*>(kl + (16 * t + 4 * i4 + r) * kKRow + piece * 16) = kr[i];
-    }
-    // where some rows do not see some tokens, a value that is not finite must not meet
-    // their weight of 0: it is kept out of the product and added to the rows that see it
-    if (chunk * kTok + kTok - 1 > block_limit) {
-      unsigned bad = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int k = 0; k < kCols; ++k)
-          if (!real_finite(vr[j].v[k])) {
-            bad |= 1u << j;
-            vr[j].v[k] = (T)0.0f;
-          }
-      if (bad) {
-        const int at = vg * 8;
-        atomicOr(const_cast<unsigned*>(&wild[at / 32]), bad << (at % 32));
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kCols; ++k) {
-      v8 x;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = vr[j].v[k];
-      *reinterpret_cast<v8*>(vl + (vc + k) * kVRow + vg * 8 * S) = x;
-    }
-  };
-
-  load(0);
   for (int chunk = 0; chunk < end; ++chunk) {
-    __syncthreads();  // the chunk before has been read
-    if (threadIdx.x < 2) wild[threadIdx.x] = 0;
-    if (chunk * kTok + kTok - 1 > block_limit) __syncthreads();
-    store(chunk);
-    __syncthreads();
-    if (chunk + 1 < end) load(chunk + 1);
+    __builtin_amdgcn_s_waitcnt(0);  // this chunk is in LDS
+    ring_barrier();                 // everybody's part of it, and the other buffer has been read
+    const int8_t* kl = lds + (chunk & 1) * kStage;
+    const int8_t* vl = kl + KP * Pan::kBytes;
+    if (chunk + 1 < end) load(chunk + 1, (chunk + 1) & 1);
     if (chunk >= wave_end) continue;
     v4f sum[NC][TT];
 #pragma unroll
     for (int b = 0; b < kSteps; ++b) {
       v8 k[TT];
 #pragma unroll
-      for (int t = 0; t < TT; ++t) k[t] = *reinterpret_cast<const v8*>(kl + (16 * t + n) * kKRow + (32 * b + 8 * g) * S);
+      for (int t = 0; t < TT; ++t) {
+        const int8_t* row = kl + (b * 32 / Pan::kDims) * Pan::kBytes + (16 * t + n) * 128;
+        if constexpr (S == 2) {
+          k[t] = *reinterpret_cast<const v8*>(row + (((b & 1) * 4 + g) ^ key_swap(n)) * 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const v4f part = *reinterpret_cast<const v4f*>(row + ((2 * g + e) ^ key_swap(n)) * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[t][4 * e + i] = part[i];
+          }
+        }
+      }
 #pragma unroll
       for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int c = 0; c < NC; ++c) sum[c][t] = mfma8(k[t], q[c][b], b ? sum[c][t] : v4f{0, 0, 0, 0});
     }
-    constexpr int N = 4 * TT;  // this lane's tokens: N g + 0 .. N - 1 of the chunk
-    const int t0 = chunk * kTok + N * g;
+    constexpr int N = 4 * TT;  // this lane's tokens: 16 (i / 4) + 4 g + i % 4 of the chunk
+    const int t0 = chunk * kTok + 4 * g;
     const bool edge = chunk * kTok + kTok - 1 > first_limit;
     float x[NC][N];
 #pragma unroll
@@ -241,7 +282,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
       for (int i = 0; i < N; ++i) x[c][i] = sum[c][i >> 2][i & 3];
       if (edge) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[c][i] = t0 + i > limit[c] ? -INFINITY : scaled(x[c][i], f);
+        for (int i = 0; i < N; ++i) x[c][i] = t0 + 16 * (i >> 2) + (i & 3) > limit[c] ? -INFINITY : scaled(x[c][i], f);
         f = 1.0f;
       }
       float top = x[c][0];
@@ -260,47 +301,70 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
       }
       if (far[c]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[c][i] = scaled(x[c][i], f);
-        f = 1.0f;
+        for (int i = 0; i < N; ++i) x[c][i] = scaled(x[c][i], f) - m[c];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[c][i] = __builtin_amdgcn_exp2f(x[c][i] + kLift);
+      } else {
+        const float ref = kLift - m[c];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[c][i] = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, ref));
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float w = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, -m[c]));
-        if constexpr (std::is_same<T, _Float16>::value) w *= 64.0f;
-        l[c] += w;
-        x[c][i] = w;
-      }
+      for (int i = 0; i < N; ++i) l[c] += x[c][i];
     }
+    v8 w[NC][N / 8];
 #pragma unroll
-    for (int u = 0; u < N / 8; ++u) {
-      v8 w[NC];
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int i = 0; i < N; ++i) w[c][i >> 3][i & 7] = (T)x[c][i];
+    // Where some rows do not see some tokens, a value that is not finite must not meet
+    // their weight of 0: it is kept out of the product and added to the rows that see it.
+    bool wild = false;
+    if (edge) {
+#pragma unroll 1
+      for (int i = lane; i < VP * kTok * 8; i += 64) {
+        const Reals<T, kPiece> y = *reinterpret_cast<const Reals<T, kPiece>*>(vl + i * 16);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[c][i] = (T)x[c][8 * u + i];
-#pragma unroll
-      for (int j = 0; j < DT; ++j) {
-        const v8 v = *reinterpret_cast<const v8*>(vl + (16 * j + n) * kVRow + (N * g + 8 * u) * S);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, w[c], o[c][j]);
+        for (int k = 0; k < kPiece; ++k) wild |= !finite((float)y.v[k]);
       }
+      wild = __any(wild);
     }
-    if (chunk * kTok + kTok - 1 > block_limit) {
-      unsigned bits[2] = {wild[0], wild[1]};
-      while (bits[0] | bits[1]) {
-        const int t = bits[0] ? __builtin_ctz(bits[0]) : 32 + __builtin_ctz(bits[1]);
-        bits[t / 32] &= ~(1u << (t % 32));
+    if (!wild) {
+#pragma unroll
+      for (int u = 0; u < N / 8; ++u)
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          const v8 v = value_operand<T>(vl, u, j, g, n);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, w[c][u], o[c][j]);
+        }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < N / 8; ++u)
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          v8 v = value_operand<T>(vl, u, j, g, n);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = finite((float)v[k]) ? v[k] : (T)0.0f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, u ? w[c][N / 8 - 1] : w[c][0], o[c][j]);
+        }
+#pragma unroll 1
+      for (int t = 0; t < kTok; ++t) {
         const int at = chunk * kTok + t;
-        const T* row = values + (from + (int64_t)min(at, s.len - 1)) * a.kv.ldv;
+        if (at >= s.len) break;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int j = 0; j < DT; ++j)
 #pragma unroll
-          for (int j = 0; j < DT; ++j)
+          for (int i = 0; i < 4; ++i) {
+            const int d = 16 * j + 4 * g + i;
+            const float v = (float)*reinterpret_cast<const T*>(
+                vl + d / Pan::kDims * Pan::kBytes + t * 128 +
+                ((d % Pan::kDims / kPiece ^ value_swap<T>(t)) << 4) + d % kPiece * S);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float v = (float)row[16 * j + 4 * g + i];
-              if (at <= limit[c] && at < s.len && !finite(v)) o[c][j][i] += v;
-            }
+            for (int c = 0; c < NC; ++c)
+              if (at <= limit[c] && !finite(v)) o[c][j][i] += v;
+          }
       }
     }
   }
@@ -311,7 +375,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
     const int row = wrow + c * 16 + n;
     if (row >= s.fresh) continue;
     const float f = l[c] == 0.0f ? 0.0f : 1.0f / l[c];
-    T* at = static_cast<T*>(a.out) + (s.first + (int64_t)row) * a.ldo + (int64_t)head * VD + 4 * g;
+    T* at = static_cast<T*>(p.a.out) + (s.first + (int64_t)row) * p.a.ldo + (int64_t)head * VD + 4 * g;
 #pragma unroll
     for (int j = 0; j < DT; ++j) {
       const float y[4] = {o[c][j][0] * f, o[c][j][1] * f, o[c][j][2] * f, o[c][j][3] * f};
@@ -327,8 +391,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(ExpandedRun p) {
 
 template <typename T, int D, int VD, int NC>
 hipError_t run(const Ctx& c, const ExpandedRun& p) {
-  constexpr int kTok = Operand<T>::kTok, S = sizeof(T);
-  constexpr int bytes = kTok * (D * S + 16) + VD * (kTok * S + 16) + 16;
+  constexpr int bytes = 2 * (Panels<T>::of(D) + Panels<T>::of(VD)) * Panels<T>::kBytes;
   auto* f = k_expanded_attention<T, D, VD, NC>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
@@ -367,6 +430,9 @@ hipError_t launch_expanded_attention(const Ctx& c, const ExpandedArgs& a, int ty
   };
   p.vec = fits(a.kv.k, a.kv.ldk, a.kv.hdk) && fits(a.kv.v, a.kv.ldv, a.kv.hdv) && fits(a.kv.key, a.kv.ld_key, 0) &&
           fits(a.q, a.ldq, 0);
+  // 64 rows have to lie within 32-bit offsets of each other
+  constexpr int64_t kNear = int64_t(1) << 24;
+  p.vec = p.vec && a.kv.ldk < kNear && a.kv.ldv < kNear && a.kv.ld_key < kNear;
   p.vec_out = fits(a.out, a.ldo, 0);
   p.flags = c.sc.flags;
   return for_real(type, [&](auto zero) {

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, RT == 1 && sizeof(T) == 2 ? 2 : 1) void k_late
   const int tile = p.row_tiles - 1 - (int)(oct % (unsigned)p.row_tiles);  // the last rows see the most tokens
   const int split = (int)(pair / (unsigned)a.b.seqs), seq = (int)((pair + split) % (unsigned)a.b.seqs);
   const int P = a.c.page;
-  const SeqDev s = seq_of(a.b, P, seq);
+  const SeqDev s = block_seq(seq_of(a.b, P, seq));
   if (!s.ok) {
     if (split == 0 && tile == 0 && threadIdx.x == 0) raise_flag(p.flags, FXPQ_FLAG_RANGE);
     return;

@@ -30,6 +30,12 @@ __device__ inline SeqDev seq_of(const fxpq_kv_batch& b, int page, int s) {
   return q;
 }
 
+// The same for a block that works on one sequence: in scalar registers.
+__device__ inline SeqDev block_seq(SeqDev q) {
+  return SeqDev{__builtin_amdgcn_readfirstlane(q.first), __builtin_amdgcn_readfirstlane(q.fresh),
+                __builtin_amdgcn_readfirstlane(q.len), (bool)__builtin_amdgcn_readfirstlane((int)q.ok)};
+}
+
 // First byte of token slot `slot` of a page and head: K rows are whole, V rows
 // come in 16-token blocks of [dim][16].
 __device__ inline int64_t k_offset(const fxpq_kv_cache& c, int page, int head, int slot) {

@@ -27,6 +27,12 @@ __device__ inline void dma16(const int8_t* g, int8_t* lds) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "{m0}"(l) : "memory");
 }
 
+// The same from a wave-uniform address and a byte offset of each lane.
+__device__ inline void dma16(const void* base, uint32_t offset, int8_t* lds) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(l) : "memory");
+}
+
 // Workgroup barrier without the memory fence __syncthreads() adds: that fence
 // would wait for every outstanding LDS-ring load.  The empty asm statements
 // keep the compiler from moving memory accesses across it.
