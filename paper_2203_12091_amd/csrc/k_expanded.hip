@@ -93,31 +93,37 @@ __device__ inline void copy_pieces(const int8_t* from, int panels, int8_t* to) {
   }
 }
 
-// Eight tokens of one dimension: tokens 4 g + 0..3 of the 16-token tiles 2 u and 2 u + 1,
-// dimension 16 j + n.
+typedef __attribute__((address_space(3))) const int8_t* LdsAt;
+__device__ inline LdsAt lds_at(const int8_t* p) { return (LdsAt)(uint32_t)(uintptr_t)p; }
+template <typename V>
+__device__ inline V lds_read(LdsAt p) { return *(__attribute__((address_space(3))) const V*)p; }
+
+// A lane's first byte of values, for dimensions 16 j .. of panels' quarters j % 4 (f32:
+// halves j % 2); the rest of an operand's address is a constant.
 template <typename T>
-__device__ inline typename Operand<T>::v8 value_operand(const int8_t* vl, int u, int j, int g, int n) {
+__device__ inline int value_at(int j, int g, int n) {
+  if constexpr (sizeof(T) == 4) return 4 * g * 128 + ((((j & 1) * 4 + (n >> 2)) ^ value_swap<T>(4 * g)) << 4) + (n & 3) * 4;
+  // lane n points at token n / 4 of four, dimensions 4 (n % 4) .. + 3
+  const int tok = 4 * g + (n >> 2), piece = (j & 3) * 2 + ((n >> 1) & 1);
+  return tok * 128 + ((piece ^ value_swap<T>(tok)) << 4) + (n & 1) * 8;
+}
+// Eight tokens of one dimension: tokens 4 g + 0..3 of the 16-token tiles 2 u and 2 u + 1,
+// dimension 16 j + n, from `at` = value_at of j.
+template <typename T>
+__device__ inline typename Operand<T>::v8 value_operand(LdsAt at, int u, int j) {
   typename Operand<T>::v8 v;
   if constexpr (sizeof(T) == 4) {
-    const int piece = (j & 1) * 4 + (n >> 2);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int tok = 32 * u + 16 * (k >> 2) + 4 * g + (k & 3);
-      v[k] = *reinterpret_cast<const float*>(vl + (j >> 1) * Panels<T>::kBytes + tok * 128 +
-                                             ((piece ^ value_swap<T>(tok)) << 4) + (n & 3) * 4);
-    }
+    for (int k = 0; k < 8; ++k)
+      v[k] = lds_read<float>(at + (j >> 1) * Panels<T>::kBytes + (32 * u + 16 * (k >> 2) + (k & 3)) * 128);
   } else {
     typedef short v4s __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) v4s* lds_v4s;
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) v4s* Quad;
     v4s part[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      // lane n points at token n / 4 of the four, dimensions 4 (n % 4) .. + 3
-      const int tok = 32 * u + 16 * k + 4 * g + (n >> 2), piece = (j & 3) * 2 + ((n >> 1) & 1);
-      const int8_t* at = vl + (j >> 2) * Panels<T>::kBytes + tok * 128 + ((piece ^ value_swap<T>(tok)) << 4) + (n & 1) * 8;
-      part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uint32_t)(uintptr_t)at);
-    }
-    typedef short v8s __attribute__((ext_vector_type(8)));
+    for (int k = 0; k < 2; ++k)
+      part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Quad)(at + (j >> 2) * Panels<T>::kBytes + (32 * u + 16 * k) * 128));
     v = __builtin_bit_cast(typename Operand<T>::v8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
   return v;
@@ -228,39 +234,49 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
     }
   }
   float m[NC], l[NC];
-  bool far[NC];
+  bool far = false;  // a reference is too large for the fused form
   v4f o[NC][DT];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m[c] = kNoMax;
     l[c] = 0.0f;
-    far[c] = false;
 #pragma unroll
     for (int j = 0; j < DT; ++j) o[c][j] = v4f{0, 0, 0, 0};
   }
   const int first_limit = causal ? pos0 + wrow : s.len - 1;
   constexpr float kLift = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
 
-  for (int chunk = 0; chunk < end; ++chunk) {
+  const LdsAt first = lds_at(lds);
+  constexpr int kValueBases = S == 4 ? 2 : 4;
+  int kat[2], vat[kValueBases];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) kat[e] = n * 128 + ((S == 4 ? 2 * g + e : 4 * e + g) ^ key_swap(n)) * 16;
+#pragma unroll
+  for (int j = 0; j < kValueBases; ++j) vat[j] = KP * Pan::kBytes + value_at<T>(j, g, n);
+
+  // One chunk; edge: some of the wave's rows do not see some of its tokens.
+  auto step = [&](int chunk, auto at_edge) __attribute__((always_inline)) {
+    constexpr bool edge = decltype(at_edge)::value;
     __builtin_amdgcn_s_waitcnt(0);  // this chunk is in LDS
     ring_barrier();                 // everybody's part of it, and the other buffer has been read
-    const int8_t* kl = lds + (chunk & 1) * kStage;
-    const int8_t* vl = kl + KP * Pan::kBytes;
+    const LdsAt stage = first + (chunk & 1) * kStage;
     if (chunk + 1 < end) load(chunk + 1, (chunk + 1) & 1);
-    if (chunk >= wave_end) continue;
+    if (edge && chunk >= wave_end) return;
     v4f sum[NC][TT];
+    const LdsAt kb[2] = {stage + kat[0], stage + kat[1]};
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int b = 0; b < kSteps; ++b) {
       v8 k[TT];
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        const int8_t* row = kl + (b * 32 / Pan::kDims) * Pan::kBytes + (16 * t + n) * 128;
+        const int at = b * 32 / Pan::kDims * Pan::kBytes + 16 * t * 128;
         if constexpr (S == 2) {
-          k[t] = *reinterpret_cast<const v8*>(row + (((b & 1) * 4 + g) ^ key_swap(n)) * 16);
+          k[t] = lds_read<v8>(kb[b & 1] + at);
         } else {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const v4f part = *reinterpret_cast<const v4f*>(row + ((2 * g + e) ^ key_swap(n)) * 16);
+            const v4f part = lds_read<v4f>(kb[e] + at);
 #pragma unroll
             for (int i = 0; i < 4; ++i) k[t][4 * e + i] = part[i];
           }
@@ -271,56 +287,73 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
 #pragma unroll
         for (int c = 0; c < NC; ++c) sum[c][t] = mfma8(k[t], q[c][b], b ? sum[c][t] : v4f{0, 0, 0, 0});
     }
+    __builtin_amdgcn_s_setprio(0);
     constexpr int N = 4 * TT;  // this lane's tokens: 16 (i / 4) + 4 g + i % 4 of the chunk
     const int t0 = chunk * kTok + 4 * g;
-    const bool edge = chunk * kTok + kTok - 1 > first_limit;
-    float x[NC][N];
+    float x[NC][N], f = f_log2;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float f = f_log2;
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int i = 0; i < N; ++i) x[c][i] = sum[c][i >> 2][i & 3];
-      if (edge) {
+    if constexpr (edge) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < N; ++i) x[c][i] = t0 + 16 * (i >> 2) + (i & 3) > limit[c] ? -INFINITY : scaled(x[c][i], f);
-        f = 1.0f;
-      }
-      float top = x[c][0];
+      f = 1.0f;
+    }
+    float top[NC];
+    bool over = false;
 #pragma unroll
-      for (int i = 1; i < N; ++i) top = fmaxf(top, x[c][i]);
-      top *= f;
-      if (__any(top > m[c] + kSlack)) {
+    for (int c = 0; c < NC; ++c) {
+      top[c] = x[c][0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) top[c] = fmaxf(top[c], x[c][i]);
+      top[c] *= f;
+      over |= top[c] > m[c] + kSlack;
+    }
+    if (__any(over)) {
+      far = false;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
         // row by row: what one row sees has no part in its neighbours' rounding
-        const float row_top = over_groups(top), now = row_top > m[c] + kSlack ? row_top : m[c];
+        const float row_top = over_groups(top[c]), now = row_top > m[c] + kSlack ? row_top : m[c];
         const float down = __builtin_amdgcn_exp2f(m[c] - now);
         m[c] = now;
         l[c] *= down;
 #pragma unroll
         for (int j = 0; j < DT; ++j) o[c][j] *= down;
-        far[c] = __any(fabsf(now) > kFar);
+        far |= now > kFar || (now < -kFar && now != kNoMax);
       }
-      if (far[c]) {
+      far = __any(far);
+    }
+    float ref[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) ref[c] = kLift - m[c];
+    if (far) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[c][i] = scaled(x[c][i], f) - m[c];
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[c][i] = __builtin_amdgcn_exp2f(x[c][i] + kLift);
-      } else {
-        const float ref = kLift - m[c];
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[c][i] = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, ref));
+        ref[c] = kLift;
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) l[c] += x[c][i];
+      f = 1.0f;
     }
     v8 w[NC][N / 8];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[c][i >> 3][i & 7] = (T)x[c][i];
+      for (int i = 0; i < N; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, ref[c]));
+        l[c] += e;
+        w[c][i >> 3][i & 7] = (T)e;
+      }
+    const LdsAt vb = stage;
     // Where some rows do not see some tokens, a value that is not finite must not meet
     // their weight of 0: it is kept out of the product and added to the rows that see it.
     bool wild = false;
-    if (edge) {
+    const int8_t* vl = lds + (chunk & 1) * kStage + KP * Pan::kBytes;
+    if constexpr (edge) {
 #pragma unroll 1
       for (int i = lane; i < VP * kTok * 8; i += 64) {
         const Reals<T, kPiece> y = *reinterpret_cast<const Reals<T, kPiece>*>(vl + i * 16);
@@ -330,20 +363,22 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       wild = __any(wild);
     }
     if (!wild) {
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < N / 8; ++u)
 #pragma unroll
         for (int j = 0; j < DT; ++j) {
-          const v8 v = value_operand<T>(vl, u, j, g, n);
+          const v8 v = value_operand<T>(vb + vat[j % kValueBases], u, j);
 #pragma unroll
           for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, w[c][u], o[c][j]);
         }
+      __builtin_amdgcn_s_setprio(0);
     } else {
 #pragma unroll 1
       for (int u = 0; u < N / 8; ++u)
 #pragma unroll
         for (int j = 0; j < DT; ++j) {
-          v8 v = value_operand<T>(vl, u, j, g, n);
+          v8 v = value_operand<T>(vb + vat[j % kValueBases], u, j);
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[k] = finite((float)v[k]) ? v[k] : (T)0.0f;
 #pragma unroll
@@ -367,7 +402,13 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
           }
       }
     }
-  }
+  };
+  // the chunks that all of the wave's rows see whole come first
+  const int whole = wave_end ? min((first_limit + 1) / kTok, end) : 0;
+#pragma unroll 1
+  for (int chunk = 0; chunk < whole; ++chunk) step(chunk, std::false_type());
+#pragma unroll 1
+  for (int chunk = whole; chunk < end; ++chunk) step(chunk, std::true_type());
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     l[c] += __shfl_xor(l[c], 16);
