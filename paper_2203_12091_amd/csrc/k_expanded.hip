@@ -46,6 +46,8 @@ __device__ inline v4f mfma8(Operand<float>::v8 a, Operand<float>::v8 b, v4f c) {
 
 constexpr float kNoMax = -3.40282347e38f;
 constexpr float kSlack = 8.0f;   // a reference follows when a logit passes it by more than this (base 2)
+// kinds of instructions in a prescribed order
+constexpr int kMfma = 0x8, kDsRead = 0x100;
 constexpr float kFar = 0x1p24f;  // references up to this leave an error below 1
 
 struct ExpandedRun {
@@ -287,6 +289,15 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
 #pragma unroll
         for (int c = 0; c < NC; ++c) sum[c][t] = mfma8(k[t], q[c][b], b ? sum[c][t] : v4f{0, 0, 0, 0});
     }
+    if constexpr (S == 2) {
+      // the next step's operands are read before this one's products
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 2 * TT, 0);
+#pragma unroll
+      for (int b = 0; b < kSteps; ++b) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, TT * NC, 0);
+        if (b + 2 < kSteps) __builtin_amdgcn_sched_group_barrier(kDsRead, TT, 0);
+      }
+    }
     __builtin_amdgcn_s_setprio(0);
     constexpr int N = 4 * TT;  // this lane's tokens: 16 (i / 4) + 4 g + i % 4 of the chunk
     const int t0 = chunk * kTok + 4 * g;
@@ -340,15 +351,21 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       f = 1.0f;
     }
     v8 w[NC][N / 8];
+    auto weigh = [&](int u, int i) __attribute__((always_inline)) {  // token i of the 8 of operand u
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(x[c][i], f, ref[c]));
+      for (int c = 0; c < NC; ++c) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[c][8 * u + i], f, ref[c]));
         l[c] += e;
-        w[c][i >> 3][i & 7] = (T)e;
+        w[c][u][i] = (T)e;
       }
+    };
     const LdsAt vb = stage;
+    constexpr int kAhead = 4;  // operands read ahead
+    v8 v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) v[j] = value_operand<T>(vb + vat[j % kValueBases], j / DT, j % DT);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) weigh(0, i);
     // Where some rows do not see some tokens, a value that is not finite must not meet
     // their weight of 0: it is kept out of the product and added to the rows that see it.
     bool wild = false;
@@ -363,26 +380,31 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       wild = __any(wild);
     }
     if (!wild) {
-      __builtin_amdgcn_s_setprio(1);
+      // the second half's weights between the first half's products, in this order
 #pragma unroll
-      for (int u = 0; u < N / 8; ++u)
+      for (int k = 0; k < N / 8 * DT; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < DT; ++j) {
-          const v8 v = value_operand<T>(vb + vat[j % kValueBases], u, j);
+        for (int c = 0; c < NC; ++c) o[c][k % DT] = mfma8(v[k % kAhead], w[c][k / DT], o[c][k % DT]);
+        const int ahead = k + kAhead;
+        if (ahead < N / 8 * DT) v[k % kAhead] = value_operand<T>(vb + vat[ahead % kValueBases], ahead / DT, ahead % DT);
+        if (N > 8 && k < DT)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, w[c][u], o[c][j]);
-        }
-      __builtin_amdgcn_s_setprio(0);
+          for (int i = 0; i < 8 / DT; ++i) weigh(1, k * (8 / DT) + i);
+      }
     } else {
+      if (N > 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) weigh(N / 8 - 1, i);
 #pragma unroll 1
       for (int u = 0; u < N / 8; ++u)
 #pragma unroll
         for (int j = 0; j < DT; ++j) {
-          v8 v = value_operand<T>(vb + vat[j % kValueBases], u, j);
+          v8 y = value_operand<T>(vb + vat[j % kValueBases], u, j);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = finite((float)v[k]) ? v[k] : (T)0.0f;
+          for (int k = 0; k < 8; ++k) y[k] = finite((float)y[k]) ? y[k] : (T)0.0f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(v, u ? w[c][N / 8 - 1] : w[c][0], o[c][j]);
+          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(y, u ? w[c][N / 8 - 1] : w[c][0], o[c][j]);
         }
 #pragma unroll 1
       for (int t = 0; t < kTok; ++t) {
