@@ -19,6 +19,7 @@
 // when a row passes it by more than kSlack, so P_t is below 2^(kSlack + kLift) and most
 // chunks need neither a maximum across the waves nor a second barrier.
 #include "kv.hpp"
+#include "ring.hpp"
 #include "values.hpp"
 
 namespace fxpq {
@@ -28,19 +29,31 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
+// How the work is split.  shared: each sequence's chunks are cut into equal parts of at
+// most `share` chunks, and the share is the smallest for which no group of row_tiles
+// blocks has more than `rounds` parts, whatever the sequences' lengths; parts of a
+// sequence are joined afterwards.  Otherwise a block takes a row tile of a sequence whole.
 struct LatentRun {
   LatentArgs a;
-  int row_tiles, splits, split_chunks, page_log2, vec;
-  float* part_o;   // [splits][tokens][heads][latent]
-  float* part_ml;  // [splits][tokens][heads][2]: reference and sum
+  int row_tiles, shared, groups, rounds, page_log2, vec;
+  float* part_o;   // [groups * rounds][row_tiles][rows of a tile][latent]
+  float* part_ml;  // [groups * rounds][row_tiles][rows of a tile][2]: reference and sum
+  int* line;       // [seqs] each sequence's first part; [seqs]: the share
   unsigned* flags;
 };
+// Chunks of each of a sequence's parts, of which there are ceil(chunks / share).
+__device__ inline int part_chunks(int chunks, int share) {
+  const int parts = (chunks + share - 1) / share;
+  return parts == 0 ? 1 : (chunks + parts - 1) / parts;
+}
+constexpr int kMostSeqs = 256;  // of a call that is shared
 
 constexpr float kNoMax = -3.40282347e38f;  // reference before any token
 constexpr float kSlack = 8.0f;
 // P is written as f16: 2^kLift at the reference, so that weights down to 2^-20 of the
 // largest keep all 11 bits and smaller ones lose at most 2^-31 of it.
 constexpr float kLift = 64.0f;
+constexpr int kLeastShare = 2;  // chunks
 constexpr float kLeastLog = -50.0f;  // of s_t / R, where it only moves the reference
 
 __device__ inline void lds_barrier() {
@@ -52,12 +65,14 @@ __device__ inline void lds_barrier() {
 
 // Byte u = code + 128 below the exponent of 1024 is 1024 + u, and 1024 + u - 1152 the
 // code, exactly.
-__device__ inline unsigned halves(unsigned biased) {
+__device__ inline unsigned unbiased(unsigned biased) {
   const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
   return __builtin_bit_cast(unsigned, __builtin_bit_cast(v2h, biased) - off);
 }
-// 16 codes as two operands of 8.
+// 16 codes as two operands of 8; BIASED: 1152 more than each code.
+template <bool BIASED>
 __device__ inline void codes_to_halves(v4i w, v8h& lo, v8h& hi) {
+  const auto halves = [](unsigned biased) { return BIASED ? biased : unbiased(biased); };
   v4i r[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -70,7 +85,7 @@ __device__ inline void codes_to_halves(v4i w, v8h& lo, v8h& hi) {
 }
 // Byte `at` of two tokens' words as a pair of halves.
 __device__ inline int pair_of(unsigned first, unsigned second, int at) {
-  return (int)halves(__builtin_amdgcn_perm(second, first, 0x0C040C00u + (unsigned)at * 0x00010001u) ^ 0x64806480u);
+  return (int)unbiased(__builtin_amdgcn_perm(second, first, 0x0C040C00u + (unsigned)at * 0x00010001u) ^ 0x64806480u);
 }
 
 __device__ inline v4f mfma(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -89,475 +104,703 @@ __device__ inline float over_groups(float x) {
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
+// A group of 16 tokens of a chunk in LDS: rows of LB * 4 + 4 pieces of 16 bytes.  A latent's
+// piece c of token t sits at c ^ (t / 4), so that reads of one piece of 16 tokens cover all
+// banks; the shared key's pieces follow in order.
 template <int LB, int RT, int QT>
 struct LatentLds {
-  static constexpr int kRow = LB * 64 + 16;  // bytes of a token: the pad spreads the banks
-  static constexpr int kCodes = 64 * kRow;
-  static constexpr int kPRow = 144;  // bytes of a row of P: 64 halves and a pad
+  static constexpr int kPieces = LB * 4 + 4, kRow = kPieces * 16;
+  static constexpr int kLoads = kPieces * 16 / 64;  // 1 KB loads of a group
+  static constexpr int kGroup = 16 * kRow, kSlot = 4 * kGroup;
+  // one tile of a wide latent: two slots, so that two blocks fit a CU
+  static constexpr int kSlots = LB == 8 && RT * QT == 1 ? 2 : 3;
+  static constexpr int kScales = kSlots * kSlot;              // [slots][4 groups][64] floats
+  static constexpr int kPRow = 144;                           // bytes of a row of P: 64 halves and a pad
   static constexpr int kP = RT * 16 * kPRow;
-  static constexpr int kStats = 2 * kCodes + 2 * QT * kP;
-  static constexpr int kBytes = kStats + 4 * RT * 16 * 4 + 64;
+  static constexpr int kWeights = kScales + kSlots * 4 * 256;  // [2][QT] P
+  static constexpr int kStats = kWeights + 2 * QT * kP;
+  static constexpr int kLine = kStats + 4 * RT * 16 * 4 + 64;  // [kMostSeqs] first parts
+  static constexpr int kBytes = kLine + (kMostSeqs + 1) * 4;
+  // q as f16 lies in the slots behind the first until the waves have taken it
+  static constexpr int kQRow = (LB * 64 + 64) * 2, kQ = RT * 16 * kQRow;
+  static_assert(QT * kQ <= (kSlots - 1) * kSlot, "q fits");
 };
 
-template <typename T, int LB, int RT>
-__global__ __launch_bounds__(256, RT == 1 && sizeof(T) == 2 ? 2 : 1) void k_latent_attention(LatentRun p) {
+// LB: 64-dimension pieces of the latent; RT: 16-row tiles of a block; W: waves.  Four waves:
+// each has one group of 16 tokens in the first product and a quarter of the latent's
+// dimensions in the second.  Eight: two share a group of tokens and have half of the rows
+// each, and an eighth of the dimensions.
+template <typename T, int LB, int RT, int W>
+__global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 : 1) void k_latent_attention(const LatentRun p) {
   constexpr int QT = sizeof(T) == 4 ? 2 : 1;  // f16 terms of q and of P
   constexpr int KB = LB + 1;                  // 64-byte pieces of a token: the latent's, the key's
-  constexpr int kRows = RT * 16;
+  constexpr int kRows = RT * 16, D = LB * 64, kThreads = W * 64;
+  constexpr int H = W / 4, QR = RT / H;  // row tiles of a wave in the first product
+  constexpr int CB = LB / H;             // 16-dimension tiles of a wave in the second
+  // 16-bit q meets 1152 + code, not the code: one operation fewer for each pair of codes.
+  // What the 1152 adds, 1152 sum q, is where the sums start from, below zero; their fp32
+  // rounding then counts against it, 2^-24 of about 30 times the products themselves.
+  constexpr bool kBiased = QT == 1;
   typedef LatentLds<LB, RT, QT> L;
+  // loads of a wave: with eight, the first four waves have the first half of each group
+  constexpr int kHalf = (L::kLoads + H - 1) / H, kWaveLoads = W == 8 ? kHalf : L::kLoads + 1;
+  static_assert(W == 4 || L::kLoads - kHalf + 1 == kHalf, "both halves wait for as many loads");
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
   float* tops = reinterpret_cast<float*>(lds + L::kStats);          // [4][kRows]
   float* scales = tops + 4 * kRows;                                 // [4]
   volatile int* raised = reinterpret_cast<volatile int*>(scales + 4);  // [2]: chunk + 1 of the last that passed its reference
-  const LatentArgs& a = p.a;
+  int* line = reinterpret_cast<int*>(lds + L::kLine);
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // Row tiles of one part of a cache are 8 ids apart: on one XCD, whose L2 they share.
-  const unsigned oct = blockIdx.x / 8, pairs = (unsigned)a.b.seqs * (unsigned)p.splits;
-  const unsigned pair = oct / (unsigned)p.row_tiles * 8 + blockIdx.x % 8;
-  if (pair >= pairs) return;
-  const int tile = p.row_tiles - 1 - (int)(oct % (unsigned)p.row_tiles);  // the last rows see the most tokens
-  const int split = (int)(pair / (unsigned)a.b.seqs), seq = (int)((pair + split) % (unsigned)a.b.seqs);
-  const int P = a.c.page;
-  const SeqDev s = block_seq(seq_of(a.b, P, seq));
-  if (!s.ok) {
-    if (split == 0 && tile == 0 && threadIdx.x == 0) raise_flag(p.flags, FXPQ_FLAG_RANGE);
-    return;
-  }
-  const int row0 = tile * kRows, rows = s.fresh * a.heads;
-  if (row0 >= rows) return;
-  const int total = rows_chunks(p, s, row0, kRows);
-  const int begin = split * p.split_chunks, end = min(begin + p.split_chunks, total);
-  if (p.splits > 1 && begin >= end) return;
-  const int pos0 = s.len - s.fresh;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tg = wave & 3, half = W == 8 ? wave >> 2 : 0;
+  const int heads = p.a.heads, causal = p.a.causal, rope = p.a.c.rope, pages = p.a.c.pages, page_log2 = p.page_log2;
+  const int P = 1 << page_log2, seqs = p.a.b.seqs;
+  const int8_t* codes = p.a.c.codes;
+  const float* latent_scale = p.a.c.scale;
+  const float* key_scale = p.a.c.rope_scale;
+  unsigned* flags = p.flags;
+  const float to_log2 = p.a.scale * 1.44269504088896340736f;
 
-  v8h q[QT][RT][2 * KB];  // lane: row n of tile r, dimensions 64 b + 16 g + 8 h + 0..7 at 2 b + h
-  float qn[RT];
-  int limit[RT];
+  // Row tiles of one part of a cache are 8 ids apart: on one XCD, whose L2 they share.
+  const unsigned oct = blockIdx.x / 8;
+  const int group = (int)(oct / (unsigned)p.row_tiles * 8 + blockIdx.x % 8);
+  const int tile = p.row_tiles - 1 - (int)(oct % (unsigned)p.row_tiles);  // the last rows see the most tokens
+  if (group >= p.groups) return;
+
+  // This lane's 16 bytes of each load of a group, whose tokens lie one after another in
+  // their page.
+  constexpr int kMine = W == 8 ? kHalf : L::kLoads;
+  uint32_t from[kMine];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = row0 + r * 16 + n, i = row / a.heads, head = row % a.heads;
-    const bool real = row < rows;
-    limit[r] = a.causal ? pos0 + i : s.len - 1;
-    const int64_t at = s.first + (int64_t)(real ? i : 0);
-    const T* ql = static_cast<const T*>(a.q) + at * a.ldq + head * a.hdq + 16 * g;
-    const T* qr = static_cast<const T*>(a.qr) + at * a.ldqr + head * a.hdqr + 16 * g;
-    float x[KB][16];
-    unsigned top = 0;
+  for (int i = 0; i < kMine; ++i) {
+    const int at = (i + half * kHalf) * 64 + lane, t = (at / L::kPieces) & 15, c = at % L::kPieces;
+    const int piece = c < LB * 4 ? c ^ (t >> 2) : c - LB * 4 < rope / 16 ? c : LB * 4;
+    from[i] = (uint32_t)(t * (D + rope) + piece * 16);
+  }
+
+  // every wave finds the share and its sequences' first parts by itself: four sequences a lane
+  int part = group, parts = p.groups, share = 1;
+  int4* known = reinterpret_cast<int4*>(lds + L::kSlot);  // what was read, until q comes there
+  bool fresh_known = p.shared;
+  if (p.shared) {
+    constexpr int kOwn = kMostSeqs / 64;
+    int count[kOwn], all = 0;
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      const bool some = real && (b < LB || 16 * g < a.c.rope);
-      const T* from = b < LB ? ql + 64 * b : qr;
-#pragma unroll
-      for (int k = 0; k < 16; ++k) x[b][k] = 0.0f;
-      if (some) {
-        if (p.vec) {
-          constexpr int W = 16 / sizeof(T);
-#pragma unroll
-          for (int k = 0; k < 16; k += W) {
-            float u[W];
-            load_reals<T, W>(from + k, u);
-#pragma unroll
-            for (int j = 0; j < W; ++j) x[b][k + j] = u[j];
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) x[b][k] = (float)from[k];
-        }
+    for (int e = 0; e < kOwn; ++e) {
+      const int i = lane + 64 * e;
+      count[e] = 0;
+      if (64 * e < seqs && i < seqs) {
+        const SeqDev d = seq_of(p.a.b, P, i);
+        if (!d.ok && blockIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+        count[e] = d.ok ? rows_chunks(p, d, 0, d.fresh * heads) : 0;
+        known[i] = int4{d.first, d.fresh, d.len, count[e]};
       }
-#pragma unroll
-      for (int k = 0; k < 16; ++k) top = max(top, __builtin_bit_cast(unsigned, x[b][k]) & 0x7FFFFFFFu);
+      all += count[e];
     }
-    top = max(top, (unsigned)__shfl_xor((int)top, 16));
-    top = max(top, (unsigned)__shfl_xor((int)top, 32));
-    const bool fine = top < 0x7F800000u;
-    const float step = __builtin_bit_cast(
-        float, (unsigned)__builtin_bit_cast(int, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
-    const float up = pow2_inverse(step) * 0x1p13f;
-    qn[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
+    auto over_wave = [](int v) {
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+      for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+      return __builtin_amdgcn_readfirstlane(v);
+    };
+    all = over_wave(all);
+    share = max((all + p.groups * p.rounds - 1) / (p.groups * p.rounds), kLeastShare);
+    for (;;) {
+      int mine = 0;
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        float rest = fine ? x[b][k] * up : 0.0f;
+      for (int e = 0; e < kOwn; ++e) mine += (count[e] + share - 1) / share;
+      parts = over_wave(mine);
+      if (parts <= p.groups * p.rounds) break;  // at the latest where no sequence has two
+      share += 1 + share / 16;
+    }
+    int before = 0;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+      const int mine = (count[e] + share - 1) / share;
+      int sum = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+      }
+      const int i = lane + 64 * e;
+      if (i < seqs) {
+        line[i] = before + sum - mine;
+        if (blockIdx.x == 0 && wave == 0) p.line[i] = before + sum - mine;
+      }
+      before += __shfl(sum, 63);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.line[seqs] = share;
+    __syncthreads();
+  }
+
+  for (; part < parts; part += p.groups) {
+    int seq = part, begin = 0;
+    SeqDev s;
+    if (p.shared) {
+      // the last sequence whose first part is this or an earlier one (those without parts
+      // start where the next does)
+      int lo = 0, hi = seqs - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (line[mid] <= part) lo = mid;
+        else hi = mid - 1;
+      }
+      seq = __builtin_amdgcn_readfirstlane(lo);
+      if (fresh_known) {
+        const int4 k = known[seq];
+        s = block_seq(SeqDev{k.x, k.y, k.z, true});
+        fresh_known = false;
+      } else {
+        s = block_seq(seq_of(p.a.b, P, seq));
+      }
+    } else {
+      s = block_seq(seq_of(p.a.b, P, seq));
+      if (!s.ok && tile == 0 && threadIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+    }
+    const int row0 = tile * kRows, rows = s.ok ? s.fresh * heads : 0;
+    const int total = row0 < rows ? rows_chunks(p, s, row0, kRows) : 0;  // this tile's
+    int end = total;
+    if (p.shared) {
+      const int size = part_chunks(rows_chunks(p, s, 0, rows), share);
+      begin = (part - __builtin_amdgcn_readfirstlane(line[seq])) * size;
+      end = min(begin + size, total);
+    }
+    if (begin >= end) continue;
+    const int pos0 = s.len - s.fresh;
+    // read by scalar loads: they are not counted among the loads to LDS
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(p.a.b.table + (int64_t)seq * p.a.b.table_ld);
+    const int last_nth = (s.len - 1) >> page_log2;
+
+    // Page of this wave's tokens of a chunk; past the sequence's end -1.
+    auto page_of = [&](int chunk) __attribute__((always_inline)) {
+      const int nth = (chunk * 64 + tg * 16) >> page_log2;
+      return nth <= last_nth ? table[nth] : -1;
+    };
+    auto load = [&](int chunk, int slot, int page) __attribute__((always_inline)) {
+      const int t = chunk * 64 + tg * 16;
+      const bool there = page >= 0 && page < pages;
+      if (!there && t < s.len && lane == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+      const int64_t first = ((int64_t)(there ? page : 0) << page_log2) + (t & (P - 1));
+      const int8_t* base = codes + first * (D + rope);
+      int8_t* into = lds + slot * L::kSlot + tg * L::kGroup;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        if (i + 1 < kMine || half == 0) dma16(base, from[i], into + (i + half * kHalf) * 1024);
+      if (W == 4 || half == 1)
+        dma4((g & 1 ? key_scale : latent_scale) + first + n, lds + L::kScales + (slot * 4 + tg) * 256);
+    };
+    lds_barrier();  // the part before has been left, and what was known of the sequences
+    int page = page_of(begin), page1 = page_of(begin + 1), page2 = page_of(begin + 2);
+    load(begin, 0, page);
+
+    // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
+    // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity;
+    // behind it -1152 times the sums of the latent's and the key's parts.
+    float* rowq = tops;
+    {
+      int8_t* ql = lds + L::kSlot;
+      const int sub = threadIdx.x & 15;
+#pragma unroll 1
+      for (int r = threadIdx.x >> 4; r < kRows; r += kThreads / 16) {
+        const int row = row0 + r, i = row / heads, head = row % heads;
+        const bool real = row < rows;
+        const int64_t token = s.first + (int64_t)(real ? i : 0);
+        const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
+        const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
+        constexpr int V = 16 / sizeof(T), N = LB * 4 / V;  // LB * 4 latent reals and 4 of the key a thread
+        float x[LB * 4 + 4];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const int d = (k * 16 + sub) * V;
+          float u[V];
+          if (p.vec) {
+            load_reals<T, V>(ql_from + d, u);
+          } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) u[j] = (float)ql_from[d + j];
+          }
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[k * V + j] = u[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? (float)qr_from[(4 * sub < rope ? 4 * sub : 0) + j] : 0.0f;
+        unsigned top = 0;
+#pragma unroll
+        for (int k = 0; k < LB * 4 + 4; ++k) {
+          if (!real) x[k] = 0.0f;
+          top = max(top, __builtin_bit_cast(unsigned, x[k]) & 0x7FFFFFFFu);
+        }
+#pragma unroll
+        for (int d = 8; d; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+        const bool fine = top < 0x7F800000u;
+        const float step = __builtin_bit_cast(
+            float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
+        const float up = pow2_inverse(step) * 0x1p13f;
+#pragma unroll
+        for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
+        float total_l = 0.0f, total_r = 0.0f;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-          const _Float16 h = (_Float16)rest;
-          q[t][r][2 * b + (k >> 3)][k & 7] = h;
-          rest -= (float)h;
+          int8_t* to_lds = ql + t * L::kQ + r * L::kQRow;
+#pragma unroll
+          for (int k = 0; k < N + 1; ++k) {
+            const int w = k < N ? V : 4, d = k < N ? (k * 16 + sub) * V : D + 4 * sub;
+#pragma unroll
+            for (int j = 0; j < w; j += 4) {
+              v4h y;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                y[e] = (_Float16)x[k * V + j + e];
+                if (kBiased) (k < N ? total_l : total_r) += (float)y[e];
+                x[k * V + j + e] -= (float)y[e];
+              }
+              *reinterpret_cast<v4h*>(to_lds + (d + j) * 2) = y;
+            }
+          }
+        }
+        if constexpr (kBiased) {
+#pragma unroll
+          for (int d = 8; d; d >>= 1) {
+            total_l += __shfl_xor(total_l, d);
+            total_r += __shfl_xor(total_r, d);
+          }
+        }
+        if (sub == 0) {
+          rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
+          rowq[kRows + r] = -1152.0f * total_l;
+          rowq[2 * kRows + r] = -1152.0f * total_r;
         }
       }
-  }
-
-  float m[RT], l[RT], R = 0.0f;
-  v4f o[RT][LB];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    m[r] = kNoMax;
-    l[r] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < LB; ++c) o[r][c] = v4f{0, 0, 0, 0};
-  }
-  const int first_limit = a.causal ? pos0 + row0 / a.heads : s.len - 1;
-  const int32_t* table = a.b.table + (int64_t)seq * a.b.table_ld;
-  const int last_nth = (s.len - 1) >> p.page_log2;
-  const float to_log2 = a.scale * 1.44269504088896340736f;
-
-  // Page numbers two chunks ahead, codes and scales one.
-  v4i kr[KB];
-  v4f next_s, next_rs;
-  int next_page = -1;
-  bool next_there = false;
-  auto lookup = [&](int chunk) {
-    const int nth = (chunk * 64 + wave * 16) >> p.page_log2;
-    next_page = nth <= last_nth ? table[nth] : -1;
-  };
-  auto load = [&](int chunk) {
-    const int t = chunk * 64 + wave * 16;
-    next_there = next_page >= 0 && next_page < a.c.pages;
-    if (!next_there && t < s.len && lane == 0) raise_flag(p.flags, FXPQ_FLAG_RANGE);
-    const int page = next_there ? next_page : 0, slot = t & (P - 1);
-    const int8_t* base = a.c.codes + latent_offset(a.c, page, slot + n);
-#pragma unroll
-    for (int b = 0; b < LB; ++b) kr[b] = *reinterpret_cast<const v4i*>(base + 64 * b + 16 * g);
-    kr[LB] = *reinterpret_cast<const v4i*>(base + 64 * LB + (16 * g < a.c.rope ? 16 * g : 0));
-    const int64_t at = (int64_t)page * P + slot + 4 * g;
-    next_s = *reinterpret_cast<const v4f*>(a.c.scale + at);
-    next_rs = *reinterpret_cast<const v4f*>(a.c.rope_scale + at);
-  };
-  if (begin < end) {
-    lookup(begin);
-    load(begin);
-    lookup(begin + 1);
+    }
     if (threadIdx.x < 2) raised[threadIdx.x] = 0;
     lds_barrier();
-  }
-  for (int chunk = begin; chunk < end; ++chunk) {
-    const int buf = (chunk - begin) & 1;
-    int8_t* cb = lds + buf * L::kCodes;
-    int8_t* pb = lds + 2 * L::kCodes + buf * QT * L::kP;
-    const bool there = next_there;
-    const int t0 = chunk * 64 + wave * 16 + 4 * g;  // this lane's four tokens of S
-    // scales: 0 for what is no token of the sequence (its memory may hold anything)
-    float st[4], cs[4], rs[4];
+    v8h q[QT][QR][2 * KB];  // lane: row n of tile r, dimensions 64 b + 16 g + 8 h + 0..7 at 2 b + h
+    float qn[QR], bias_l[QR], bias_r[QR];
+    int limit[QR];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool in = there && t0 + i < s.len;
-      st[i] = in ? next_s[i] : 0.0f;
-      cs[i] = st[i] * to_log2;
-      rs[i] = (in ? next_rs[i] : 0.0f) * to_log2;
-    }
-#pragma unroll
-    for (int b = 0; b < LB; ++b) *reinterpret_cast<v4i*>(cb + (wave * 16 + n) * L::kRow + 64 * b + 16 * g) = kr[b];
-    v4f sum[RT], turned[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) sum[r] = turned[r] = v4f{0, 0, 0, 0};
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      v8h k[2];
-      codes_to_halves(kr[b], k[0], k[1]);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            v4f& to = b < LB ? sum[r] : turned[r];
-            to = mfma(k[h], q[t][r][2 * b + h], to);
-          }
-    }
-    if (chunk + 1 < end) {
-      load(chunk + 1);
-      lookup(chunk + 2);
-    }
-    float z[RT][4];  // logits, but for the row's power of two
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[r][i] = fmaf(turned[r][i], rs[i], sum[r][i] * cs[i]);
-    if (chunk * 64 + 63 > first_limit || !there) {
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t0 + i > limit[r] || !there) z[r][i] = -INFINITY;
-    }
-    float add[RT], lg[4];
-    auto logs = [&]() {
-      const float inv = R > 0.0f ? pow2_inverse(R) : 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(st[i] * inv), kLeastLog);
-    };
-    auto weigh = [&]() {  // P of this wave's tokens to LDS
-      const float lift = pow2_inverse(R) * kLift;
-      float w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = st[i] * lift;
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        float rest[4];
-        add[r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(z[r][i], qn[r], -m[r]));
-          add[r] += e;
-          rest[i] = e * w[i];
-        }
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          v4h h;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            h[i] = (_Float16)rest[i];
-            rest[i] -= (float)h[i];
-          }
-          *reinterpret_cast<v4h*>(pb + t * L::kP + (r * 16 + n) * L::kPRow + wave * 32 + g * 8) = h;
-        }
-      }
-    };
-    logs();
-    bool over = chunk == begin;
-    if (!over) {
-      bool mine = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) > R;
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        float y = fmaf(z[r][0], qn[r], lg[0]);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
-        mine |= y > m[r] + kSlack;
-      }
-      over = __any(mine);
-    }
-    if (over) {
-      if (lane == 0) raised[buf] = chunk + 1;
-    } else {
-      weigh();
-    }
-    lds_barrier();
-    if (raised[buf] == chunk + 1) {
-      // new references: the scales' first, then each row's, over all waves
-      float most = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
-      most = over_groups(most);
-      if (lane == 0) scales[wave] = most;
-      lds_barrier();
-      most = fmaxf(fmaxf(fmaxf(scales[0], scales[1]), fmaxf(scales[2], scales[3])), 0x1p-110f);
-      // the power of two above it
-      most = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, most) & 0x7F800000u) + 0x00800000u);
-      const float now_r = fmaxf(R, most);
-      const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
-      R = now_r;
-      logs();
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        float y = fmaf(z[r][0], qn[r], lg[0]);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
-        y = over_groups(y);
-        if (g == 0) tops[wave * kRows + r * 16 + n] = y;
-      }
-      lds_barrier();
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const int at = r * 16 + n;
-        const float y = fmaxf(fmaxf(tops[at], tops[kRows + at]), fmaxf(tops[2 * kRows + at], tops[3 * kRows + at]));
-        // what came before weighs `ratio` of what it did against the new R
-        const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
-        const float now = y > before + kSlack ? y : before, down = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
-        m[r] = now;
-        l[r] *= down;
-        const float f = down * ratio;
-#pragma unroll
-        for (int c = 0; c < LB; ++c) o[r][c] *= f;
-      }
-      weigh();
-      lds_barrier();
-    }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) l[r] += add[r];
-    // lane: dimensions LB n + 0 .. LB - 1 of this wave's quarter, of tokens 32 u + 8 g + 0 .. 7
-    const int8_t* cw = cb + wave * (LB * 16) + LB * n;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      unsigned w[8][LB / 4];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned* from = reinterpret_cast<const unsigned*>(cw + (32 * u + 8 * g + j) * L::kRow);
-        if constexpr (LB == 8) {
-          const uint2 v = *reinterpret_cast<const uint2*>(from);
-          w[j][0] = v.x;
-          w[j][1] = v.y;
-        } else {
-          w[j][0] = *from;
-        }
-      }
-      v8h pf[QT][RT];
+    for (int r = 0; r < QR; ++r) {
+      const int row = (half * QR + r) * 16 + n;
+      limit[r] = causal ? pos0 + (row0 + row) / heads : s.len - 1;
+      qn[r] = rowq[row];
+      bias_l[r] = kBiased ? rowq[kRows + row] : 0.0f;
+      bias_r[r] = kBiased ? rowq[2 * kRows + row] : 0.0f;
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-          pf[t][r] = *reinterpret_cast<const v8h*>(pb + t * L::kP + (r * 16 + n) * L::kPRow + u * 64 + g * 16);
+        for (int b = 0; b < 2 * KB; ++b)
+          q[t][r][b] = *reinterpret_cast<const v8h*>(lds + L::kSlot + t * L::kQ + row * L::kQRow +
+                                                     (64 * (b >> 1) + 16 * g + 8 * (b & 1)) * 2);
+    }
+    lds_barrier();
+    if (L::kSlots == 3 && begin + 1 < end) load(begin + 1, 1, page1);
+
+    // references of all rows of the block, the same in all waves; sums of this wave's own
+    float m[RT], l[QR], R = 0.0f;
+    v4f o[RT][CB];
 #pragma unroll
-      for (int c = 0; c < LB; ++c) {
-        v4i f;
+    for (int r = 0; r < RT; ++r) {
+      m[r] = kNoMax;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j] = pair_of(w[2 * j][c / 4], w[2 * j + 1][c / 4], c % 4);
-        const v8h v = __builtin_bit_cast(v8h, f);
+      for (int c = 0; c < CB; ++c) o[r][c] = v4f{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int r = 0; r < QR; ++r) l[r] = 0.0f;
+    auto mine = [&](int r) __attribute__((always_inline)) { return half ? m[(H - 1) * QR + r] : m[r]; };
+    const int first_limit = causal ? pos0 + row0 / heads : s.len - 1;
+    int slot = 0;
+#pragma unroll 1
+    for (int chunk = begin; chunk < end; ++chunk) {
+      const int buf = (chunk - begin) & 1;
+      int8_t* pb = lds + L::kWeights + buf * QT * L::kP;
+      const bool there = page >= 0 && page < pages;
+      // this wave's loads have landed; the next chunk's may be on their way
+      if (L::kSlots == 3 && chunk + 1 < end) wait_vmcnt<kWaveLoads>();
+      else wait_vmcnt<0>();
+      if constexpr (W == 8) lds_barrier();  // and the other half of its tokens
+      else asm volatile("" ::: "memory");
+      const int8_t* own = lds + slot * L::kSlot + tg * L::kGroup;
+      const int t0 = chunk * 64 + tg * 16 + 4 * g;  // this lane's four tokens of S
+      float st[4], cs[4], rs[4];
+      {
+        const float* sc = reinterpret_cast<const float*>(lds + L::kScales + (slot * 4 + tg) * 256) + 4 * g;
+        v4f a = *reinterpret_cast<const v4f*>(sc), b = *reinterpret_cast<const v4f*>(sc + 16);
+        if (!there || chunk * 64 + 64 > s.len) {
+          // scales: 0 for what is no token of the sequence (its memory may hold anything)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool in = there && t0 + i < s.len;
+            a[i] = in ? a[i] : 0.0f;
+            b[i] = in ? b[i] : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          st[i] = a[i];
+          cs[i] = a[i] * to_log2;
+          rs[i] = b[i] * to_log2;
+        }
+      }
+      // all operands first: one wait for LDS
+      v4i raw[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+        raw[b] = *reinterpret_cast<const v4i*>(own + n * L::kRow + (b < LB ? (4 * b + g) ^ (n >> 2) : LB * 4 + g) * 16);
+      __builtin_amdgcn_sched_barrier(0);
+      // two sums for the latent, so that a product need not wait for the last
+      v4f part[2][QR], turned[QR];
+#pragma unroll
+      for (int r = 0; r < QR; ++r) {
+        part[0][r] = v4f{bias_l[r], bias_l[r], bias_l[r], bias_l[r]};
+        part[1][r] = v4f{0, 0, 0, 0};
+        turned[r] = v4f{bias_r[r], bias_r[r], bias_r[r], bias_r[r]};
+      }
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        v8h k[2];
+        codes_to_halves<kBiased>(raw[b], k[0], k[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int r = 0; r < QR; ++r) {
+              v4f& acc = b < LB ? part[h][r] : turned[r];
+              acc = mfma(k[h], q[t][r][2 * b + h], acc);
+            }
+      }
+      v4f sum[QR];
+#pragma unroll
+      for (int r = 0; r < QR; ++r) sum[r] = part[0][r] + part[1][r];
+      float z[QR][4];  // logits, but for the row's power of two
+#pragma unroll
+      for (int r = 0; r < QR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[r][i] = fmaf(turned[r][i], rs[i], sum[r][i] * cs[i]);
+      if (chunk * 64 + 63 > first_limit || !there) {
+#pragma unroll
+        for (int r = 0; r < QR; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (t0 + i > limit[r] || !there) z[r][i] = -INFINITY;
+      }
+      float add[QR], lg[4];
+      auto logs = [&]() __attribute__((always_inline)) {
+        const float inv = R > 0.0f ? pow2_inverse(R) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(st[i] * inv), kLeastLog);
+      };
+      auto weigh = [&]() __attribute__((always_inline)) {  // P of this wave's tokens and rows to LDS
+        const float lift = pow2_inverse(R) * kLift;
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = st[i] * lift;
+#pragma unroll
+        for (int r = 0; r < QR; ++r) {
+          float rest[4];
+          add[r] = 0.0f;
+          const float ref = -mine(r);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(z[r][i], qn[r], ref));
+            add[r] += e;
+            rest[i] = e * w[i];
+          }
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            v4h h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              h[i] = (_Float16)rest[i];
+              rest[i] -= (float)h[i];
+            }
+            *reinterpret_cast<v4h*>(pb + t * L::kP + ((half * QR + r) * 16 + n) * L::kPRow + tg * 32 + g * 8) = h;
+          }
+        }
+      };
+      logs();
+      bool over = chunk == begin;
+      if (!over) {
+        bool some = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) > R;
+#pragma unroll
+        for (int r = 0; r < QR; ++r) {
+          float y = fmaf(z[r][0], qn[r], lg[0]);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
+          some |= y > mine(r) + kSlack;
+        }
+        over = __any(some);
+      }
+      if (over) {
+        if (lane == 0) raised[buf] = chunk + 1;
+      } else {
+        weigh();
+      }
+      lds_barrier();
+      if (raised[buf] == chunk + 1) {
+        // new references: the scales' first, then each row's, over all groups of tokens
+        float most = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
+        most = over_groups(most);
+        if (lane == 0) scales[tg] = most;
+        lds_barrier();
+        most = fmaxf(fmaxf(fmaxf(scales[0], scales[1]), fmaxf(scales[2], scales[3])), 0x1p-110f);
+        // the power of two above it
+        most = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, most) & 0x7F800000u) + 0x00800000u);
+        const float now_r = fmaxf(R, most);
+        const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
+        R = now_r;
+        logs();
+#pragma unroll
+        for (int r = 0; r < QR; ++r) {
+          float y = fmaf(z[r][0], qn[r], lg[0]);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
+          y = over_groups(y);
+          if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = y;
+        }
+        lds_barrier();
+        float down[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const int row = r * 16 + n;
+          const float y = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
+          // what came before weighs `ratio` of what it did against the new R
+          const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
+          const float now = y > before + kSlack ? y : before;
+          down[r] = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
+          m[r] = now;
+          const float f = down[r] * ratio;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) o[r][c] *= f;
+        }
+#pragma unroll
+        for (int r = 0; r < QR; ++r) l[r] *= half ? down[(H - 1) * QR + r] : down[r];
+        weigh();
+        lds_barrier();
+      }
+#pragma unroll
+      for (int r = 0; r < QR; ++r) l[r] += add[r];
+      // all waves have left the chunk before: its slot takes the next but one, or of two
+      // slots the next
+      constexpr int kAhead = L::kSlots - 1;
+      if (chunk + kAhead < end) load(chunk + kAhead, slot == 0 ? kAhead : slot - 1, kAhead == 2 ? page2 : page1);
+      page = page1;
+      page1 = page2;
+      page2 = page_of(chunk + 3);
+      // lane: dimensions CB n + 0 .. CB - 1 of this wave's part, of tokens 32 u + 8 g + 0 .. 7
+      const int8_t* all = lds + slot * L::kSlot;
+      unsigned w[2][8][(CB + 3) / 4];
+      v8h pf[2][QT][RT];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // token 8 (g % 2) + j of group 2 u + g / 2
+          const int byte = wave * CB * 16 + CB * n, piece = (byte >> 4) ^ (2 * (g & 1) + (j >> 2));
+          const int8_t* src = all + (2 * u + (g >> 1)) * L::kGroup + (8 * (g & 1) + j) * L::kRow + piece * 16 + (byte & 15);
+          if constexpr (CB == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(src);
+            w[u][j][0] = v.x;
+            w[u][j][1] = v.y;
+          } else if constexpr (CB == 4) {
+            w[u][j][0] = *reinterpret_cast<const unsigned*>(src);
+          } else {
+            w[u][j][0] = *reinterpret_cast<const uint16_t*>(src);
+          }
+        }
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int r = 0; r < RT; ++r) o[r][c] = mfma(v, pf[t][r], o[r][c]);
+          for (int r = 0; r < RT; ++r)
+            pf[u][t][r] = *reinterpret_cast<const v8h*>(pb + t * L::kP + (r * 16 + n) * L::kPRow + u * 64 + g * 16);
       }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+          v4i f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = pair_of(w[u][2 * j][c / 4], w[u][2 * j + 1][c / 4], c % 4);
+          const v8h v = __builtin_bit_cast(v8h, f);
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) o[r][c] = mfma(v, pf[u][t][r], o[r][c]);
+        }
+      slot = slot == L::kSlots - 1 ? 0 : slot + 1;
     }
-  }
 
-  // the rows' sums over lanes and waves
+    // the rows' sums over lanes and waves
+    lds_barrier();
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    l[r] += __shfl_xor(l[r], 16);
-    l[r] += __shfl_xor(l[r], 32);
-  }
-  lds_barrier();
+    for (int r = 0; r < QR; ++r) {
+      l[r] += __shfl_xor(l[r], 16);
+      l[r] += __shfl_xor(l[r], 32);
+      if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = l[r];
+    }
+    lds_barrier();
+    const bool whole = begin == 0 && end == total;
+    const int64_t place = ((int64_t)part * p.row_tiles + tile) * kRows;
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
-    if (g == 0) tops[wave * kRows + r * 16 + n] = l[r];
-  lds_barrier();
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int at = r * 16 + n, row = row0 + at;
-    if (row >= rows) continue;
-    const float sum = tops[at] + tops[kRows + at] + tops[2 * kRows + at] + tops[3 * kRows + at];
-    const int64_t token = s.first + (int64_t)(row / a.heads);
-    const int head = row % a.heads, d0 = wave * (LB * 16) + 4 * LB * g;
-    const float unit = R * (1.0f / kLift);
-    if (p.splits > 1) {
-      const int64_t to = ((int64_t)split * a.b.tokens + token) * a.heads + head;
+    for (int r = 0; r < RT; ++r) {
+      const int in_tile = r * 16 + n, row = row0 + in_tile;
+      if (row >= rows) continue;
+      const float sum = tops[in_tile] + tops[kRows + in_tile] + tops[2 * kRows + in_tile] + tops[3 * kRows + in_tile];
+      const int d0 = wave * CB * 16 + 4 * CB * g;
+      const float unit = R * (1.0f / kLift);
+      const float f = whole ? (sum == 0.0f ? 0.0f : unit / sum) : unit;
+      float y[4 * CB];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < LB; c += 4)
-          *reinterpret_cast<v4f*>(p.part_o + to * (LB * 64) + d0 + LB * i + c) =
-              v4f{o[r][c][i], o[r][c + 1][i], o[r][c + 2][i], o[r][c + 3][i]} * unit;
-      if (wave == 0 && g == 0) {
-        p.part_ml[2 * to] = m[r];
-        p.part_ml[2 * to + 1] = sum;
+        for (int c = 0; c < CB; ++c) y[i * CB + c] = o[r][c][i] * f;
+      if (!whole) {
+        float* into = p.part_o + (place + in_tile) * D + d0;
+#pragma unroll
+        for (int k = 0; k < 4 * CB; k += 4) *reinterpret_cast<v4f*>(into + k) = v4f{y[k], y[k + 1], y[k + 2], y[k + 3]};
+        if (wave == 0 && g == 0) {
+          p.part_ml[2 * (place + in_tile)] = m[r];
+          p.part_ml[2 * (place + in_tile) + 1] = sum;
+        }
+        continue;
       }
-      continue;
-    }
-    const float f = sum == 0.0f ? 0.0f : unit / sum;
-    T* to = static_cast<T*>(a.out) + token * a.ldo + head * a.hdo + d0;
+      T* into = static_cast<T*>(p.a.out) + (s.first + (int64_t)(row / heads)) * p.a.ldo + row % heads * p.a.hdo + d0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < LB; c += 4) {
-        const float y[4] = {o[r][c][i] * f, o[r][c + 1][i] * f, o[r][c + 2][i] * f, o[r][c + 3][i] * f};
+      for (int k = 0; k < 4 * CB; k += 4) {
+        const float z[4] = {y[k], y[k + 1], y[k + 2], y[k + 3]};
         if (p.vec) {
-          store_reals<T, 4>(to + LB * i + c, y);
+          store_reals<T, 4>(into + k, z);
         } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) to[LB * i + c + k] = (T)y[k];
+          for (int e = 0; e < 4; ++e) into[k + e] = (T)z[e];
         }
       }
+    }
   }
 }
 
-// Joins the splits of each row: one block per new token and head.
-template <typename T>
-__global__ __launch_bounds__(256) void k_latent_join(LatentRun p, int tile_rows) {
-  constexpr int kMany = 256;  // weights kept at a time
-  __shared__ float weight[kMany], red[4], sums[1024];
+// Joins the parts of a row, 8 of them at a time in flight.  A unit of WAYS * Q threads
+// has 4 Q dimensions of one row: a wave has a whole row where rows are many, a block 64
+// dimensions of one where they are few and have many parts.
+template <typename T, int Q, int WAYS>
+__global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile_rows) {
+  constexpr int kAhead = 8, kUnits = 256 / (Q * WAYS);
+  __shared__ float sums[1024], red[256];
   const LatentArgs& a = p.a;
-  const SeqDev s = seq_of(a.b, a.c.page, blockIdx.z);
-  const int i = blockIdx.x, head = blockIdx.y;
-  if (!s.ok || i >= s.fresh) return;
-  const int row = i * a.heads + head;
-  const int total = rows_chunks(p, s, row / tile_rows * tile_rows, tile_rows);
-  const int used = (total + p.split_chunks - 1) / p.split_chunks;
-  const int64_t token = s.first + (int64_t)i, stride = (int64_t)a.b.tokens * a.heads, at0 = token * a.heads + head;
-  const int tid = threadIdx.x, lane = tid & 63;
-  float mx = kNoMax;
-  for (int k = tid; k < used; k += 256) mx = fmaxf(mx, p.part_ml[2 * (k * stride + at0)]);
-#pragma unroll
-  for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-  if (lane == 0) red[tid >> 6] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const int quads = a.c.latent / 4, ways = 256 / quads, x = tid % quads, y = tid / quads;
+  const int pieces = a.c.latent / (4 * Q), tid = threadIdx.x, x = tid % Q, y = tid / Q % WAYS;
+  const int unit = (int)blockIdx.x * kUnits + tid / (Q * WAYS), row = unit / pieces, d0 = unit % pieces * 4 * Q + 4 * x;
+  const SeqDev s = seq_of(a.b, a.c.page, blockIdx.y);
+  const int i = row / a.heads, head = row % a.heads;
+  bool some = s.ok && i < s.fresh;
   float sum = 0.0f;
   v4f v = {0, 0, 0, 0};
-  for (int k0 = 0; k0 < used; k0 += kMany) {
-    const int many = min(kMany, used - k0);
-    __syncthreads();
-    if (tid < many) {
-      const int64_t at = (k0 + tid) * stride + at0;
-      const float w = __builtin_amdgcn_exp2f(p.part_ml[2 * at] - mx);
-      weight[tid] = w;
-      sum += w * p.part_ml[2 * at + 1];
-    }
-    __syncthreads();
-    for (int k = y; k < many; k += ways)
-      v += weight[k] * *reinterpret_cast<const v4f*>(p.part_o + ((k0 + k) * stride + at0) * a.c.latent + 4 * x);
-  }
+  if (some) {
+    const int tile = row / tile_rows, total = rows_chunks(p, s, tile * tile_rows, tile_rows);
+    const int size = part_chunks(rows_chunks(p, s, 0, s.fresh * a.heads), p.line[a.b.seqs]);
+    const int many = (total + size - 1) / size;
+    some = many > 1;  // else written already
+    const int64_t stride = (int64_t)p.row_tiles * tile_rows;
+    const int64_t at0 = p.line[blockIdx.y] * stride + (int64_t)tile * tile_rows + row % tile_rows;
+    const auto part = [&](int k) { return k * stride + at0; };
+    if (some) {
+      float mx = kNoMax;
+      for (int k = 0; k < many; k += kAhead) {
+        float in[kAhead];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  __syncthreads();
-  if (lane == 0) red[tid >> 6] = sum;
-  *reinterpret_cast<v4f*>(sums + 4 * tid) = v;
-  __syncthreads();
-  if (tid >= quads) return;
-  sum = red[0] + red[1] + red[2] + red[3];
-  for (int w = 1; w < ways; ++w) v += *reinterpret_cast<const v4f*>(sums + 4 * (w * quads + x));
+        for (int e = 0; e < kAhead; ++e) in[e] = p.part_ml[2 * part(min(k + e, many - 1))];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) mx = fmaxf(mx, in[e]);
+      }
+      for (int k0 = y; k0 < many; k0 += WAYS * kAhead) {
+        v4f in[kAhead];
+        float w[kAhead], l[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const int64_t at = part(min(k0 + e * WAYS, many - 1));
+          in[e] = *reinterpret_cast<const v4f*>(p.part_o + at * a.c.latent + d0);
+          w[e] = p.part_ml[2 * at];
+          l[e] = p.part_ml[2 * at + 1];
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+          if (k0 + e * WAYS < many) {
+            w[e] = __builtin_amdgcn_exp2f(w[e] - mx);
+            sum += w[e] * l[e];
+            v += w[e] * in[e];
+          }
+      }
+    }
+  }
+  if constexpr (WAYS > 1) {
+    red[tid] = sum;
+    *reinterpret_cast<v4f*>(sums + 4 * tid) = v;
+    __syncthreads();
+    if (y > 0) return;
+    for (int w = 1; w < WAYS; ++w) {
+      sum += red[tid + w * Q];
+      v += *reinterpret_cast<const v4f*>(sums + 4 * (tid + w * Q));
+    }
+  }
+  if (!some) return;
   const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-  T* to = static_cast<T*>(a.out) + token * a.ldo + head * a.hdo + 4 * x;
+  T* to = static_cast<T*>(a.out) + (s.first + (int64_t)i) * a.ldo + head * a.hdo + d0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) to[k] = (T)(v[k] * f);
 }
 
 struct LatentPlan {
-  int rt, row_tiles, splits, split_chunks;
+  int rt, row_tiles, shared, groups, rounds;
   int64_t part, bytes;
 };
 
 LatentPlan plan_latent(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type) {
   LatentPlan p{};
   const int64_t rows = (int64_t)b.max_new * heads;
-  p.rt = rows <= 16 || type == FXPQ_F32 ? 1 : 2;
+  p.rt = rows <= 16 ? 1 : rows <= 32 || type == FXPQ_F32 || k.latent == 512 ? 2 : 4;
   p.row_tiles = (int)((rows + p.rt * 16 - 1) / (p.rt * 16));
-  const int64_t blocks = (int64_t)p.row_tiles * b.seqs, chunks = (b.max_len + 63) / 64;
-  const int64_t slots = (int64_t)c.cus * (p.rt == 1 ? 2 : 1);
-  int64_t per = (blocks * chunks + slots - 1) / slots;
-  per = per < 4 ? 4 : per > 32 && blocks < 4 * slots ? 32 : per;
-  if (blocks >= 4 * slots) per = chunks;
-  p.split_chunks = (int)(per < 1 ? 1 : per);
-  p.splits = (int)((chunks + p.split_chunks - 1) / p.split_chunks);
-  if (p.splits > 1) {
-    p.part = (int64_t)p.splits * b.tokens * heads;
-    p.bytes = p.part * (k.latent + 2) * 4;
-  } else {
-    p.splits = 1;
+  const int64_t blocks = (int64_t)p.row_tiles * b.seqs;
+  p.shared = blocks < 4 * (int64_t)c.cus && b.seqs <= kMostSeqs && p.row_tiles <= c.cus / 8;
+  p.rounds = 1;
+  if (!p.shared) {
+    p.groups = b.seqs;
+    return p;
   }
+  // blocks that fit the chip at a time
+  const int slots = p.rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
+  p.groups = slots / 8 / p.row_tiles * 8;
+  p.rounds = (b.seqs + p.groups - 1) / p.groups;
+  p.part = (int64_t)p.groups * p.rounds * p.row_tiles * p.rt * 16;
+  p.bytes = p.part * (k.latent + 2) * 4 + (b.seqs + 1) * 4;
   return p;
 }
 
-template <typename T, int LB, int RT>
+template <typename T, int LB, int RT, int W>
 hipError_t run_latent(const Ctx& c, const LatentRun& p) {
   constexpr int bytes = LatentLds<LB, RT, sizeof(T) == 4 ? 2 : 1>::kBytes;
-  auto* f = k_latent_attention<T, LB, RT>;
+  auto* f = k_latent_attention<T, LB, RT, W>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  const int64_t blocks = ((int64_t)p.a.b.seqs * p.splits + 7) / 8 * 8 * p.row_tiles;
+  const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * p.row_tiles;
   if (blocks > kMaxBlocks) return hipErrorInvalidValue;
-  f<<<dim3((unsigned)blocks), dim3(256), bytes, c.stream>>>(p);
-  if (p.splits > 1)
-    k_latent_join<T><<<dim3((unsigned)p.a.b.max_new, (unsigned)p.a.heads, (unsigned)p.a.b.seqs), dim3(256), 0,
-                       c.stream>>>(p, RT * 16);
+  f<<<dim3((unsigned)blocks), dim3(W * 64), bytes, c.stream>>>(p);
+  if (p.shared) {
+    const int64_t rows = (int64_t)p.a.b.max_new * p.a.heads;
+    if (rows * p.a.b.seqs >= 1024) {
+      constexpr int kUnits = 4;  // 64 lanes, 256 dimensions each
+      k_latent_join<T, 64, 1><<<dim3((unsigned)((rows * (LB / 4) + kUnits - 1) / kUnits), (unsigned)p.a.b.seqs), dim3(256), 0,
+                                c.stream>>>(p, RT * 16);
+    } else {
+      k_latent_join<T, 16, 16><<<dim3((unsigned)(rows * LB), (unsigned)p.a.b.seqs), dim3(256), 0, c.stream>>>(p, RT * 16);
+    }
+  }
   return hipGetLastError();
 }
 
 template <typename T, int LB>
 hipError_t run_rows(const Ctx& c, const LatentRun& p, int rt) {
-  if constexpr (sizeof(T) == 2)
-    if (rt == 2) return run_latent<T, LB, 2>(c, p);
-  return run_latent<T, LB, 1>(c, p);
+  if (rt == 1) return run_latent<T, LB, 1, 4>(c, p);
+  if constexpr (sizeof(T) == 2 && LB == 4)
+    if (rt == 4) return run_latent<T, LB, 4, 8>(c, p);
+  return run_latent<T, LB, 2, 8>(c, p);
 }
 
 }  // namespace
@@ -573,8 +816,9 @@ hipError_t launch_latent_attention(const Ctx& c, const LatentArgs& a, int type, 
   LatentRun p{};
   p.a = a;
   p.row_tiles = plan.row_tiles;
-  p.splits = plan.splits;
-  p.split_chunks = plan.split_chunks;
+  p.shared = plan.shared;
+  p.groups = plan.groups;
+  p.rounds = plan.rounds;
   while ((1 << p.page_log2) < a.c.page) ++p.page_log2;
   const int64_t size = real_bytes(type);
   const auto fits = [&](const void* at, int64_t ld, int64_t hd) {
@@ -583,6 +827,7 @@ hipError_t launch_latent_attention(const Ctx& c, const LatentArgs& a, int type, 
   p.vec = fits(a.q, a.ldq, a.hdq) && fits(a.qr, a.ldqr, a.hdqr) && fits(a.out, a.ldo, a.hdo);
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o ? p.part_o + plan.part * a.c.latent : nullptr;
+  p.line = p.part_ml ? reinterpret_cast<int*>(p.part_ml + plan.part * 2) : nullptr;
   p.flags = c.sc.flags;
   return for_real(type, [&](auto zero) {
     using T = decltype(zero);

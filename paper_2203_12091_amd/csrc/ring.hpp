@@ -33,6 +33,12 @@ __device__ inline void dma16(const void* base, uint32_t offset, int8_t* lds) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(l) : "memory");
 }
 
+// One 4-byte load per lane: lane l's bytes land at lds + 4 l.
+__device__ inline void dma4(const void* g, int8_t* lds) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(g), "{m0}"(l) : "memory");
+}
+
 // Workgroup barrier without the memory fence __syncthreads() adds: that fence
 // would wait for every outstanding LDS-ring load.  The empty asm statements
 // keep the compiler from moving memory accesses across it.
