@@ -289,40 +289,60 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
         dma4((g & 1 ? key_scale : latent_scale) + first + n, lds + L::kScales + (slot * 4 + tg) * 256);
     };
     lds_barrier();  // the part before has been left, and what was known of the sequences
+    // q as it is to LDS, its loads before the first chunk's
+    int8_t* ql = lds + L::kSlot;
+    constexpr int kQPieces = (D + 64) * (int)sizeof(T) / 16, kQAll = kRows * kQPieces;
     int page = page_of(begin), page1 = page_of(begin + 1), page2 = page_of(begin + 2);
+    if (p.vec) {
+#pragma unroll 1
+      for (int i = wave * 64; i < kQAll; i += kThreads) {
+        const int at = i + lane, r = at / kQPieces, piece = at % kQPieces * (16 / (int)sizeof(T));  // first of 4 or 8 reals
+        const int row = min(row0 + r, rows - 1);  // rows behind the last: any
+        const int64_t token = s.first + (int64_t)(row / heads), head = row % heads;
+        const T* src = piece < D ? static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq + piece
+                                 : static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr + (piece - D < rope ? piece - D : 0);
+        if (at < kQAll) dma16(reinterpret_cast<const int8_t*>(src), ql + i * 16);
+      }
+    }
     load(begin, 0, page);
+    if (p.vec) wait_vmcnt<kWaveLoads>();
+    lds_barrier();
 
     // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
     // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity;
     // behind it -1152 times the sums of the latent's and the key's parts.
     float* rowq = tops;
     {
-      int8_t* ql = lds + L::kSlot;
       const int sub = threadIdx.x & 15;
+      constexpr int V = 16 / sizeof(T), N = LB * 4 / V;  // LB * 4 latent reals and 4 of the key a thread
+      static_assert(sizeof(T) == 2 || kRows * 16 == kThreads, "f32 rows are read before any is written");
 #pragma unroll 1
       for (int r = threadIdx.x >> 4; r < kRows; r += kThreads / 16) {
-        const int row = row0 + r, i = row / heads, head = row % heads;
+        const int row = row0 + r;
         const bool real = row < rows;
-        const int64_t token = s.first + (int64_t)(real ? i : 0);
-        const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
-        const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
-        constexpr int V = 16 / sizeof(T), N = LB * 4 / V;  // LB * 4 latent reals and 4 of the key a thread
         float x[LB * 4 + 4];
+        if (p.vec) {
+          const T* raw = reinterpret_cast<const T*>(ql) + r * (D + 64);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const int d = (k * 16 + sub) * V;
-          float u[V];
-          if (p.vec) {
-            load_reals<T, V>(ql_from + d, u);
-          } else {
+          for (int k = 0; k < N; ++k) {
+            float u[V];
+            load_reals<T, V>(raw + (k * 16 + sub) * V, u);
 #pragma unroll
-            for (int j = 0; j < V; ++j) u[j] = (float)ql_from[d + j];
+            for (int j = 0; j < V; ++j) x[k * V + j] = u[j];
           }
+          float u[4];
+          load_reals<T, 4>(raw + D + 4 * sub, u);
 #pragma unroll
-          for (int j = 0; j < V; ++j) x[k * V + j] = u[j];
+          for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? u[j] : 0.0f;
+        } else {
+          const int64_t token = s.first + (int64_t)(real ? row / heads : 0), head = row % heads;
+          const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
+          const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
+#pragma unroll
+          for (int k = 0; k < LB * 4; ++k) x[k] = (float)ql_from[(k / V * 16 + sub) * V + k % V];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? (float)qr_from[4 * sub + j] : 0.0f;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? (float)qr_from[(4 * sub < rope ? 4 * sub : 0) + j] : 0.0f;
         unsigned top = 0;
 #pragma unroll
         for (int k = 0; k < LB * 4 + 4; ++k) {
@@ -338,6 +358,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
         for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
         float total_l = 0.0f, total_r = 0.0f;
+        if constexpr (sizeof(T) == 4) lds_barrier();
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           int8_t* to_lds = ql + t * L::kQ + r * L::kQRow;
@@ -684,14 +705,14 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 template <typename T, int Q, int WAYS>
 __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile_rows) {
   constexpr int kAhead = 8, kUnits = 256 / (Q * WAYS);
-  __shared__ float sums[1024], red[256];
+  __shared__ float sums[1024], stats[512];
   const LatentArgs& a = p.a;
   const int pieces = a.c.latent / (4 * Q), tid = threadIdx.x, x = tid % Q, y = tid / Q % WAYS;
   const int unit = (int)blockIdx.x * kUnits + tid / (Q * WAYS), row = unit / pieces, d0 = unit % pieces * 4 * Q + 4 * x;
   const SeqDev s = seq_of(a.b, a.c.page, blockIdx.y);
   const int i = row / a.heads, head = row % a.heads;
   bool some = s.ok && i < s.fresh;
-  float sum = 0.0f;
+  float mx = kNoMax, sum = 0.0f;
   v4f v = {0, 0, 0, 0};
   if (some) {
     const int tile = row / tile_rows, total = rows_chunks(p, s, tile * tile_rows, tile_rows);
@@ -702,24 +723,23 @@ __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile
     const int64_t at0 = p.line[blockIdx.y] * stride + (int64_t)tile * tile_rows + row % tile_rows;
     const auto part = [&](int k) { return k * stride + at0; };
     if (some) {
-      float mx = kNoMax;
-      for (int k = 0; k < many; k += kAhead) {
-        float in[kAhead];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) in[e] = p.part_ml[2 * part(min(k + e, many - 1))];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) mx = fmaxf(mx, in[e]);
-      }
       for (int k0 = y; k0 < many; k0 += WAYS * kAhead) {
         v4f in[kAhead];
         float w[kAhead], l[kAhead];
+        float now = mx;
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
           const int64_t at = part(min(k0 + e * WAYS, many - 1));
           in[e] = *reinterpret_cast<const v4f*>(p.part_o + at * a.c.latent + d0);
-          w[e] = p.part_ml[2 * at];
+          w[e] = k0 + e * WAYS < many ? p.part_ml[2 * at] : kNoMax;
           l[e] = p.part_ml[2 * at + 1];
         }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) now = fmaxf(now, w[e]);
+        const float down = __builtin_amdgcn_exp2f(mx - now);
+        sum *= down;
+        v *= down;
+        mx = now;
 #pragma unroll
         for (int e = 0; e < kAhead; ++e)
           if (k0 + e * WAYS < many) {
@@ -731,13 +751,20 @@ __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile
     }
   }
   if constexpr (WAYS > 1) {
-    red[tid] = sum;
+    stats[2 * tid] = mx;
+    stats[2 * tid + 1] = sum;
     *reinterpret_cast<v4f*>(sums + 4 * tid) = v;
     __syncthreads();
     if (y > 0) return;
+    float top = mx;
+    for (int w = 1; w < WAYS; ++w) top = fmaxf(top, stats[2 * (tid + w * Q)]);
+    const float down = __builtin_amdgcn_exp2f(mx - top);
+    sum *= down;
+    v *= down;
     for (int w = 1; w < WAYS; ++w) {
-      sum += red[tid + w * Q];
-      v += *reinterpret_cast<const v4f*>(sums + 4 * (tid + w * Q));
+      const float f = __builtin_amdgcn_exp2f(stats[2 * (tid + w * Q)] - top);
+      sum += f * stats[2 * (tid + w * Q) + 1];
+      v += f * *reinterpret_cast<const v4f*>(sums + 4 * (tid + w * Q));
     }
   }
   if (!some) return;
