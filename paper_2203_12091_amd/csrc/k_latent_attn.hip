@@ -36,11 +36,21 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 struct LatentRun {
   LatentArgs a;
   int row_tiles, shared, groups, rounds, page_log2, vec;
+  unsigned heads_mul;  // row / heads = row * heads_mul >> heads_shift, for rows below 2^30
+  int heads_shift;
   float* part_o;   // [groups * rounds][row_tiles][rows of a tile][latent]
   float* part_ml;  // [groups * rounds][row_tiles][rows of a tile][2]: reference and sum
   int* line;       // [seqs] each sequence's first part; [seqs]: the share
   unsigned* flags;
 };
+__device__ inline int token_of(const LatentRun& p, int row) {
+  return (int)((uint64_t)(unsigned)row * p.heads_mul >> p.heads_shift);
+}
+// ceil(n / d), n below 2^24, by d's reciprocal.
+__device__ inline int quotient_up(int n, int d, float inv) {
+  const int q = (int)((float)n * inv);  // off by one at most
+  return q + (q * d < n ? 1 : 0) - ((q - 1) * d >= n ? 1 : 0);
+}
 // Chunks of each of a sequence's parts, of which there are ceil(chunks / share).
 __device__ inline int part_chunks(int chunks, int share) {
   const int parts = (chunks + share - 1) / share;
@@ -90,11 +100,31 @@ __device__ inline int pair_of(unsigned first, unsigned second, int at) {
 
 __device__ inline v4f mfma(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+// Sums and maxima over rows of 16 lanes, and a wave's sum and running sum.
+template <int CTRL>
+__device__ inline int lanes(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
+template <typename F>
+__device__ inline float over_16(float v, F f) {
+  v = f(v, __builtin_bit_cast(float, lanes<0xB1>(__builtin_bit_cast(int, v))));   // neighbours
+  v = f(v, __builtin_bit_cast(float, lanes<0x4E>(__builtin_bit_cast(int, v))));   // pairs
+  v = f(v, __builtin_bit_cast(float, lanes<0x141>(__builtin_bit_cast(int, v))));  // mirrored halves of a row
+  return f(v, __builtin_bit_cast(float, lanes<0x140>(__builtin_bit_cast(int, v))));
+}
+__device__ inline int running_sum(int v, int lane, int& all) {
+  v += lanes<0x111>(v);  // from 1, 2, 4 and 8 lanes below, in the row
+  v += lanes<0x112>(v);
+  v += lanes<0x114>(v);
+  v += lanes<0x118>(v);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  all = a + b + c + __builtin_amdgcn_readlane(v, 63);
+  return v + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? a + b : a + b + c);
+}
+
 // 64-token chunks that rows row0 .. row0 + rows - 1 of a sequence see.
 __device__ inline int rows_chunks(const LatentRun& p, const SeqDev& s, int row0, int rows) {
   const int last = min(row0 + rows, s.fresh * p.a.heads) - 1;
   if (last < row0) return 0;
-  const int limit = p.a.causal ? s.len - s.fresh + last / p.a.heads : s.len - 1;
+  const int limit = p.a.causal ? s.len - s.fresh + token_of(p, last) : s.len - 1;
   return (limit + 64) >> 6;
 }
 
@@ -119,8 +149,7 @@ struct LatentLds {
   static constexpr int kP = RT * 16 * kPRow;
   static constexpr int kWeights = kScales + kSlots * 4 * 256;  // [2][QT] P
   static constexpr int kStats = kWeights + 2 * QT * kP;
-  static constexpr int kLine = kStats + 4 * RT * 16 * 4 + 64;  // [kMostSeqs] first parts
-  static constexpr int kBytes = kLine + (kMostSeqs + 1) * 4;
+  static constexpr int kBytes = kStats + 4 * RT * 16 * 4 + 64;
   // q as f16 lies in the slots behind the first until the waves have taken it
   static constexpr int kQRow = (LB * 64 + 64) * 2, kQ = RT * 16 * kQRow;
   static_assert(QT * kQ <= (kSlots - 1) * kSlot, "q fits");
@@ -149,7 +178,6 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   float* tops = reinterpret_cast<float*>(lds + L::kStats);          // [4][kRows]
   float* scales = tops + 4 * kRows;                                 // [4]
   volatile int* raised = reinterpret_cast<volatile int*>(scales + 4);  // [2]: chunk + 1 of the last that passed its reference
-  int* line = reinterpret_cast<int*>(lds + L::kLine);
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tg = wave & 3, half = W == 8 ? wave >> 2 : 0;
   const int heads = p.a.heads, causal = p.a.causal, rope = p.a.c.rope, pages = p.a.c.pages, page_log2 = p.page_log2;
@@ -177,93 +205,76 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
     from[i] = (uint32_t)(t * (D + rope) + piece * 16);
   }
 
-  // every wave finds the share and its sequences' first parts by itself: four sequences a lane
-  int part = group, parts = p.groups, share = 1;
-  int4* known = reinterpret_cast<int4*>(lds + L::kSlot);  // what was read, until q comes there
-  bool fresh_known = p.shared;
-  if (p.shared) {
-    constexpr int kOwn = kMostSeqs / 64;
-    int count[kOwn], all = 0;
-#pragma unroll
-    for (int e = 0; e < kOwn; ++e) {
-      const int i = lane + 64 * e;
-      count[e] = 0;
-      if (64 * e < seqs && i < seqs) {
-        const SeqDev d = seq_of(p.a.b, P, i);
-        if (!d.ok && blockIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
-        count[e] = d.ok ? rows_chunks(p, d, 0, d.fresh * heads) : 0;
-        known[i] = int4{d.first, d.fresh, d.len, count[e]};
-      }
-      all += count[e];
-    }
-    auto over_wave = [](int v) {
-#pragma unroll
-      for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-      return __builtin_amdgcn_readfirstlane(v);
-    };
-    all = over_wave(all);
-    share = max((all + p.groups * p.rounds - 1) / (p.groups * p.rounds), kLeastShare);
-    for (;;) {
-      int mine = 0;
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e) mine += (count[e] + share - 1) / share;
-      parts = over_wave(mine);
-      if (parts <= p.groups * p.rounds) break;  // at the latest where no sequence has two
-      share += 1 + share / 16;
-    }
-    int before = 0;
-#pragma unroll
-    for (int e = 0; e < kOwn; ++e) {
-      const int mine = (count[e] + share - 1) / share;
-      int sum = mine;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int other = __shfl_up(sum, d);
-        if (lane >= d) sum += other;
-      }
-      const int i = lane + 64 * e;
-      if (i < seqs) {
-        line[i] = before + sum - mine;
-        if (blockIdx.x == 0 && wave == 0) p.line[i] = before + sum - mine;
-      }
-      before += __shfl(sum, 63);
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.line[seqs] = share;
-    __syncthreads();
-  }
-
-  for (; part < parts; part += p.groups) {
-    int seq = part, begin = 0;
+  int part = group, parts = p.groups;
+  do {
+    int seq = part, begin = 0, size = 0;
     SeqDev s;
     if (p.shared) {
+      // every wave finds the share and the part's sequence by itself, four sequences a lane
+      constexpr int kOwn = kMostSeqs / 64;
+      SeqDev d[kOwn];
+      int count[kOwn], all = 0;
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e) {
+        const int i = lane + 64 * e;
+        count[e] = 0;
+        d[e] = SeqDev{0, 0, 0, false};
+        if (64 * e < seqs) {
+          d[e] = seq_of(p.a.b, P, min(i, seqs - 1));
+          if (!d[e].ok && blockIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+          if (i < seqs && d[e].ok) count[e] = rows_chunks(p, d[e], 0, d[e].fresh * heads);
+          int sum;
+          running_sum(count[e], lane, sum);
+          all += sum;
+        }
+      }
+      const int most = p.groups * p.rounds;
+      int share = max((all + most - 1) / most, kLeastShare), before[kOwn];
+      for (;;) {
+        const float inv = 1.0f / (float)share;
+        parts = 0;
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e)
+          if (64 * e < seqs) {
+            const int mine = quotient_up(count[e], share, inv);
+            int sum;
+            before[e] = parts + running_sum(mine, lane, sum) - mine;
+            parts += sum;
+          }
+        if (parts <= most) break;  // at the latest where no sequence has two
+        share += 1 + share / 16;
+      }
+      if (part >= parts) break;
       // the last sequence whose first part is this or an earlier one (those without parts
       // start where the next does)
-      int lo = 0, hi = seqs - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (line[mid] <= part) lo = mid;
-        else hi = mid - 1;
-      }
-      seq = __builtin_amdgcn_readfirstlane(lo);
-      if (fresh_known) {
-        const int4 k = known[seq];
-        s = block_seq(SeqDev{k.x, k.y, k.z, true});
-        fresh_known = false;
-      } else {
-        s = block_seq(seq_of(p.a.b, P, seq));
-      }
+      seq = -1;
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e)
+        if (64 * e < seqs) {
+          const int i = lane + 64 * e;
+          seq += __popcll(__ballot(i < seqs && before[e] <= part));
+          if (blockIdx.x == 0 && wave == 0 && i < seqs) p.line[i] = before[e];
+        }
+      if (blockIdx.x == 0 && threadIdx.x == 0) p.line[seqs] = share;
+      int chunks = 0, first = 0;
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e)
+        if (seq >> 6 == e) {
+          const int at = seq & 63;
+          s = SeqDev{__builtin_amdgcn_readlane(d[e].first, at), __builtin_amdgcn_readlane(d[e].fresh, at),
+                     __builtin_amdgcn_readlane(d[e].len, at), true};
+          chunks = __builtin_amdgcn_readlane(count[e], at);
+          first = __builtin_amdgcn_readlane(before[e], at);
+        }
+      size = part_chunks(chunks, share);
+      begin = (part - first) * size;
     } else {
       s = block_seq(seq_of(p.a.b, P, seq));
       if (!s.ok && tile == 0 && threadIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
     }
     const int row0 = tile * kRows, rows = s.ok ? s.fresh * heads : 0;
     const int total = row0 < rows ? rows_chunks(p, s, row0, kRows) : 0;  // this tile's
-    int end = total;
-    if (p.shared) {
-      const int size = part_chunks(rows_chunks(p, s, 0, rows), share);
-      begin = (part - __builtin_amdgcn_readfirstlane(line[seq])) * size;
-      end = min(begin + size, total);
-    }
+    const int end = p.shared ? min(begin + size, total) : total;
     if (begin >= end) continue;
     const int pos0 = s.len - s.fresh;
     // read by scalar loads: they are not counted among the loads to LDS
@@ -288,7 +299,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       if (W == 4 || half == 1)
         dma4((g & 1 ? key_scale : latent_scale) + first + n, lds + L::kScales + (slot * 4 + tg) * 256);
     };
-    lds_barrier();  // the part before has been left, and what was known of the sequences
+    lds_barrier();  // the part before has been left
     // q as it is to LDS, its loads before the first chunk's
     int8_t* ql = lds + L::kSlot;
     constexpr int kQPieces = (D + 64) * (int)sizeof(T) / 16, kQAll = kRows * kQPieces;
@@ -298,7 +309,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       for (int i = wave * 64; i < kQAll; i += kThreads) {
         const int at = i + lane, r = at / kQPieces, piece = at % kQPieces * (16 / (int)sizeof(T));  // first of 4 or 8 reals
         const int row = min(row0 + r, rows - 1);  // rows behind the last: any
-        const int64_t token = s.first + (int64_t)(row / heads), head = row % heads;
+        const int i_token = token_of(p, row);
+        const int64_t token = s.first + (int64_t)i_token, head = row - i_token * heads;
         const T* src = piece < D ? static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq + piece
                                  : static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr + (piece - D < rope ? piece - D : 0);
         if (at < kQAll) dma16(reinterpret_cast<const int8_t*>(src), ql + i * 16);
@@ -335,7 +347,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? u[j] : 0.0f;
         } else {
-          const int64_t token = s.first + (int64_t)(real ? row / heads : 0), head = row % heads;
+          const int i_token = real ? token_of(p, row) : 0;
+          const int64_t token = s.first + (int64_t)i_token, head = real ? row - i_token * heads : 0;
           const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
           const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
 #pragma unroll
@@ -349,8 +362,11 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
           if (!real) x[k] = 0.0f;
           top = max(top, __builtin_bit_cast(unsigned, x[k]) & 0x7FFFFFFFu);
         }
-#pragma unroll
-        for (int d = 8; d; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+        // (the bits of magnitudes are ordered as integers, NaN above infinity)
+        top = max(top, (unsigned)lanes<0xB1>((int)top));
+        top = max(top, (unsigned)lanes<0x4E>((int)top));
+        top = max(top, (unsigned)lanes<0x141>((int)top));
+        top = max(top, (unsigned)lanes<0x140>((int)top));
         const bool fine = top < 0x7F800000u;
         const float step = __builtin_bit_cast(
             float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
@@ -379,11 +395,9 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
           }
         }
         if constexpr (kBiased) {
-#pragma unroll
-          for (int d = 8; d; d >>= 1) {
-            total_l += __shfl_xor(total_l, d);
-            total_r += __shfl_xor(total_r, d);
-          }
+          const auto plus = [](float a, float b) { return a + b; };
+          total_l = over_16(total_l, plus);
+          total_r = over_16(total_r, plus);
         }
         if (sub == 0) {
           rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
@@ -400,7 +414,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
     for (int r = 0; r < QR; ++r) {
       const int row = (half * QR + r) * 16 + n;
-      limit[r] = causal ? pos0 + (row0 + row) / heads : s.len - 1;
+      limit[r] = causal ? pos0 + token_of(p, row0 + row) : s.len - 1;
       qn[r] = rowq[row];
       bias_l[r] = kBiased ? rowq[kRows + row] : 0.0f;
       bias_r[r] = kBiased ? rowq[2 * kRows + row] : 0.0f;
@@ -426,7 +440,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
     for (int r = 0; r < QR; ++r) l[r] = 0.0f;
     auto mine = [&](int r) __attribute__((always_inline)) { return half ? m[(H - 1) * QR + r] : m[r]; };
-    const int first_limit = causal ? pos0 + row0 / heads : s.len - 1;
+    const int first_limit = causal ? pos0 + token_of(p, row0) : s.len - 1;
     int slot = 0;
 #pragma unroll 1
     for (int chunk = begin; chunk < end; ++chunk) {
@@ -684,7 +698,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
         }
         continue;
       }
-      T* into = static_cast<T*>(p.a.out) + (s.first + (int64_t)(row / heads)) * p.a.ldo + row % heads * p.a.hdo + d0;
+      const int token = token_of(p, row);
+      T* into = static_cast<T*>(p.a.out) + (s.first + (int64_t)token) * p.a.ldo + (row - token * heads) * p.a.hdo + d0;
 #pragma unroll
       for (int k = 0; k < 4 * CB; k += 4) {
         const float z[4] = {y[k], y[k + 1], y[k + 2], y[k + 3]};
@@ -696,7 +711,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
         }
       }
     }
-  }
+  } while ((part += p.groups) < parts);
 }
 
 // Joins the parts of a row, 8 of them at a time in flight.  A unit of WAYS * Q threads
@@ -710,7 +725,7 @@ __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile
   const int pieces = a.c.latent / (4 * Q), tid = threadIdx.x, x = tid % Q, y = tid / Q % WAYS;
   const int unit = (int)blockIdx.x * kUnits + tid / (Q * WAYS), row = unit / pieces, d0 = unit % pieces * 4 * Q + 4 * x;
   const SeqDev s = seq_of(a.b, a.c.page, blockIdx.y);
-  const int i = row / a.heads, head = row % a.heads;
+  const int i = token_of(p, row), head = row - i * a.heads;
   bool some = s.ok && i < s.fresh;
   float mx = kNoMax, sum = 0.0f;
   v4f v = {0, 0, 0, 0};
@@ -847,6 +862,10 @@ hipError_t launch_latent_attention(const Ctx& c, const LatentArgs& a, int type, 
   p.groups = plan.groups;
   p.rounds = plan.rounds;
   while ((1 << p.page_log2) < a.c.page) ++p.page_log2;
+  int log2 = 0;
+  while ((1 << log2) < a.heads) ++log2;
+  p.heads_shift = 30 + log2;
+  p.heads_mul = (unsigned)(((uint64_t(1) << p.heads_shift) + a.heads - 1) / a.heads);
   const int64_t size = real_bytes(type);
   const auto fits = [&](const void* at, int64_t ld, int64_t hd) {
     return (uintptr_t)at % 16 == 0 && ld * size % 16 == 0 && hd * size % 16 == 0;
