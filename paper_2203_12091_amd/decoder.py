@@ -1,4 +1,4 @@
-"""One decoder layer of a language model in 8-bit integers: the serving operators
+"""Decoder layers of a language model in 8-bit integers: the serving operators
 of libfxpq as they are used together.
 
     x -> norm -> quantize per token -> query / key / value product
@@ -7,11 +7,21 @@ of libfxpq as they are used together.
       -> norm -> quantize -> route each token to its experts -> grouped product
       -> gate -> quantize -> grouped product -> weighted sum over the experts -> + x
 
+``LatentLayer`` is the same with latent attention: one latent vector and one rotated
+key a token for all heads, in a cache of their own,
+
+    ... -> query product, latent and key product -> norm of the latent
+      -> append both to the paged 8-bit latent cache, rotating key and queries
+      -> few new tokens: queries through the keys' weights, attention over the latents,
+         values' weights;  prompts: read the latents, product to keys and values,
+         attention over those
+      -> quantize -> output product -> + x -> ...
+
 ``Layer`` holds weights quantized per output channel (by the same call that
-quantizes tokens: a weight row is an output channel), ``Cache`` the pages and which
-sequence owns them.  Norms, the gate and the router are elementary torch
-operations.  ``python -m paper_2203_12091_amd.decoder`` runs a prompt and some steps
-of decoding and prints their times.
+quantizes tokens: a weight row is an output channel), ``Cache`` and ``LatentCache`` the
+pages and which sequence owns them.  Norms, the gate and the router are elementary
+torch operations.  ``python -m paper_2203_12091_amd.decoder [latent]`` runs a prompt and
+some steps of decoding and prints their times.
 """
 import math
 import sys
@@ -42,16 +52,11 @@ def quantize_rows(h, x, rule=fx.SCALE_MAX):
     return codes, scale
 
 
-class Cache:
-    """Pages of an 8-bit key / value cache, handed out to sequences as they grow."""
+class Pages:
+    """Pages of a cache, handed out to sequences as they grow."""
 
-    def __init__(self, pages, page, heads, dim, max_pages_per_seq, max_seqs, device="cuda:0"):
+    def __init__(self, pages, page, max_pages_per_seq, max_seqs, device):
         self.page, self.device, self.max_pages = page, device, max_pages_per_seq
-        zeros = lambda *s, **kw: torch.zeros(*s, device=device, **kw)  # noqa: E731
-        self.k = zeros(pages, heads, page, dim, dtype=torch.int8)
-        self.v = zeros(pages, heads, page // 16, dim, 16, dtype=torch.int8)
-        self.k_scale, self.v_scale = zeros(pages, heads), zeros(pages, heads)
-        self.desc = fx.kv_cache(self.k, self.v, self.k_scale, self.v_scale, pages, page, heads, dim)
         self.free = list(range(pages - 1, -1, -1))
         self.owned = {}   # sequence -> its pages
         self.length = {}  # sequence -> its tokens
@@ -79,6 +84,8 @@ class Cache:
         batch = fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(seqs),
                             self.max_pages, sum(new), max(new), max(length))
         batch.grown = dict(zip(seqs, new))
+        batch.held = sum(length)
+        batch.rows = put(torch.tensor([0] + length).cumsum(0).to(torch.int32))  # where each sequence's tokens begin
         return batch
 
     def retract(self, batch):
@@ -100,24 +107,55 @@ class Cache:
         self.length.pop(seq, None)
 
 
+class Cache(Pages):
+    """An 8-bit key / value cache."""
+
+    def __init__(self, pages, page, heads, dim, max_pages_per_seq, max_seqs, device="cuda:0"):
+        super().__init__(pages, page, max_pages_per_seq, max_seqs, device)
+        zeros = lambda *s, **kw: torch.zeros(*s, device=device, **kw)  # noqa: E731
+        self.k = zeros(pages, heads, page, dim, dtype=torch.int8)
+        self.v = zeros(pages, heads, page // 16, dim, 16, dtype=torch.int8)
+        self.k_scale, self.v_scale = zeros(pages, heads), zeros(pages, heads)
+        self.desc = fx.kv_cache(self.k, self.v, self.k_scale, self.v_scale, pages, page, heads, dim)
+
+
+class LatentCache(Pages):
+    """An 8-bit cache of latents and shared keys."""
+
+    def __init__(self, pages, page, latent, rope, max_pages_per_seq, max_seqs, device="cuda:0"):
+        super().__init__(pages, page, max_pages_per_seq, max_seqs, device)
+        self.codes = torch.zeros(pages, page, latent + rope, dtype=torch.int8, device=device)
+        self.scale, self.rope_scale = torch.zeros(pages, page, device=device), torch.zeros(pages, page, device=device)
+        self.desc = fx.latent_cache(self.codes, self.scale, self.rope_scale, pages, page, latent, rope)
+
+
 class Layer:
     """Random weights of one decoder layer, quantized per output channel."""
 
     def __init__(self, hidden, q_heads, kv_heads, dim, experts, top, inner, positions=4096, seed=0,
                  dtype=torch.bfloat16, device="cuda:0"):
-        self.h = fx.Handle(torch.device(device).index or 0)
-        self.hidden, self.q_heads, self.kv_heads, self.dim = hidden, q_heads, kv_heads, dim
-        self.experts, self.top, self.inner, self.dtype, self.device = experts, top, inner, dtype, device
-        g = torch.Generator(device=device).manual_seed(seed)
-        weight = lambda *s: torch.randn(*s, generator=g, device=device) * s[-1] ** -0.5  # noqa: E731
+        self.q_heads, self.kv_heads, self.dim = q_heads, kv_heads, dim
+        weight = self._begin(hidden, experts, top, inner, seed, dtype, device)
         self.qkv = quantize_rows(self.h, weight((q_heads + 2 * kv_heads) * dim, hidden))
         self.out = quantize_rows(self.h, weight(hidden, q_heads * dim))
-        self.router = weight(experts, hidden)
-        self.up = quantize_rows(self.h, weight(experts * 2 * inner, hidden))
-        self.down = quantize_rows(self.h, weight(experts * hidden, inner))
-        self.norm = [torch.ones(hidden, device=device) for _ in range(2)]
-        ang = torch.arange(positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, dim, 2) / dim)
-        self.rotary = fx.rotary(ang.cos().float().to(device), ang.sin().float().to(device), positions, dim)
+        self._rest(weight, positions, dim)
+
+    def _begin(self, hidden, experts, top, inner, seed, dtype, device):
+        """What every layer has; the source of its weights."""
+        self.h = fx.Handle(torch.device(device).index or 0)
+        self.hidden, self.experts, self.top, self.inner = hidden, experts, top, inner
+        self.dtype, self.device = dtype, device
+        g = torch.Generator(device=device).manual_seed(seed)
+        return lambda *s: torch.randn(*s, generator=g, device=device) * s[-1] ** -0.5
+
+    def _rest(self, weight, positions, dims):
+        """The experts, the norms and the rotation of `dims` dimensions."""
+        self.router = weight(self.experts, self.hidden)
+        self.up = quantize_rows(self.h, weight(self.experts * 2 * self.inner, self.hidden))
+        self.down = quantize_rows(self.h, weight(self.experts * self.hidden, self.inner))
+        self.norm = [torch.ones(self.hidden, device=self.device) for _ in range(2)]
+        ang = torch.arange(positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, dims, 2) / dims)
+        self.rotary = fx.rotary(ang.cos().float().to(self.device), ang.sin().float().to(self.device), positions, dims)
 
     def _workspace(self, need):
         # one for each call: the allocator hands memory on in the order of the current
@@ -183,6 +221,12 @@ class Layer:
         y = self._grouped(codes, scale, None, offsets, self.down, self.hidden)
         return (y[place].view(x.shape[0], self.top, self.hidden).float() * weight[..., None]).sum(1).to(self.dtype)
 
+    def _check_cache(self, cache):
+        if not isinstance(cache, Cache):
+            raise ValueError(f"a {type(cache).__name__} for keys and values of each head")
+        if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
+            raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
+
     def forward(self, x, cache, batch):
         """x: the batch's new tokens, [tokens][hidden].  Everything runs on torch's
         current stream (quantize_rows, the first call of each half, says so).  Where it
@@ -192,8 +236,7 @@ class Layer:
         try:
             if x.shape != (batch.tokens, self.hidden):
                 raise ValueError(f"x is {tuple(x.shape)}, the batch's tokens are {(batch.tokens, self.hidden)}")
-            if (cache.desc.heads, cache.desc.dim) != (self.kv_heads, self.dim):
-                raise ValueError(f"a cache of {cache.desc.heads} heads of {cache.desc.dim} for {self.kv_heads} of {self.dim}")
+            self._check_cache(cache)
             if batch.max_len > self.rotary.positions:
                 raise ValueError(f"a sequence of {batch.max_len} tokens: at most {self.rotary.positions}")
             x = x + self.attend(self._norm(x, self.norm[0]), cache, batch)
@@ -203,10 +246,93 @@ class Layer:
             raise
 
 
-def main(prompt=512, steps=16, seqs=8):
-    layer = Layer(1024, 16, 4, 64, experts=8, top=2, inner=1024)
+class LatentLayer(Layer):
+    """The same with latent attention: `heads` heads of nope + rope dimensions with values
+    of vdim, all made of one latent vector a token."""
+
+    # New tokens of a sequence up to which queries go to the latents rather than latents to
+    # keys and values: 2048 tokens of context, 16 heads of 128 + 64 and 128, latents of 512:
+    FEW = 32
+
+    def __init__(self, hidden, heads, nope, rope, vdim, latent, experts, top, inner, positions=4096, seed=0,
+                 dtype=torch.bfloat16, device="cuda:0"):
+        self.heads, self.nope, self.rope, self.vdim, self.latent = heads, nope, rope, vdim, latent
+        weight = self._begin(hidden, experts, top, inner, seed, dtype, device)
+        self.q = quantize_rows(self.h, weight(heads * (nope + rope), hidden))
+        self.into = quantize_rows(self.h, weight(latent + rope, hidden))
+        # each head's keys' and values' weights; absorbed, the keys' lie the other way
+        kv = weight(heads, nope + vdim, latent)
+        self.kv = quantize_rows(self.h, kv.flatten(0, 1))
+        self.absorb = quantize_rows(self.h, kv[:, :nope].transpose(1, 2).reshape(heads * latent, nope))
+        self.value = quantize_rows(self.h, kv[:, nope:].reshape(heads * vdim, latent))
+        self.out = quantize_rows(self.h, weight(hidden, heads * vdim))
+        self.latent_norm = torch.ones(latent, device=device)
+        self._rest(weight, positions, rope)
+
+    def _check_cache(self, cache):
+        if not isinstance(cache, LatentCache):
+            raise ValueError(f"a {type(cache).__name__} for latents")
+        if (cache.desc.latent, cache.desc.rope) != (self.latent, self.rope):
+            raise ValueError(f"a cache of {cache.desc.latent} + {cache.desc.rope} for {self.latent} + {self.rope}")
+
+    def attend(self, x, cache, batch):
+        t, dt, width = x.shape[0], TYPES[self.dtype], self.nope + self.rope
+        q, cr = self._linear(x, self.q), self._linear(x, self.into)
+        c = self._norm(cr[:, : self.latent], self.latent_norm)
+        turn = q.view(t, self.heads, width)[:, :, self.nope :]  # rotated in place
+        fx.latent_append(self.h, cache.desc, batch, self.rotary, fx.SCALE_MAX, c, self.latent, cr[:, self.latent :],
+                         self.latent + self.rope, turn, self.heads * width, width, turn, self.heads * width, width,
+                         self.heads, dt)
+        # (a batch made by hand does not say how many tokens its sequences hold)
+        few = batch.max_new <= self.FEW or not hasattr(batch, "held")
+        return self._linear((self.absorbed if few else self.expanded)(q, cache, batch), self.out)
+
+    def absorbed(self, q, cache, batch):
+        """Attention over the latents: [tokens][heads * vdim]."""
+        t, H, dt, width = q.shape[0], self.heads, TYPES[self.dtype], self.nope + self.rope
+        rows, apart = q.view(t, H, width), max(t, 1) * self.latent  # a head's tokens lie together
+        # grouped by head, as experts are: token after token of the first head, then the next
+        offsets = torch.arange(H + 1, dtype=torch.int32, device=self.device) * t
+        order = torch.arange(t * H, dtype=torch.int32, device=self.device).view(t, H).t().contiguous().view(-1)
+        codes, scale = quantize_rows(self.h, rows.reshape(t * H, width)[:, : self.nope])
+        ql = self._grouped(codes, scale, order, offsets, self.absorb, self.latent)
+        out = torch.empty(H, t, self.latent, dtype=self.dtype, device=self.device)
+        need = fx.latent_attention_workspace(self.h, cache.desc, batch, H)
+        fx.latent_attention(self.h, cache.desc, batch, ql, self.latent, apart, rows[:, :, self.nope :], H * width, width, H,
+                            1 / math.sqrt(width), True, out, self.latent, apart, dt, self._workspace(need), need)
+        codes, scale = quantize_rows(self.h, out.view(H * t, self.latent))
+        v = self._grouped(codes, scale, None, offsets, self.value, self.vdim)
+        return v.view(H, t, self.vdim).transpose(0, 1).reshape(t, H * self.vdim)
+
+    def expanded(self, q, cache, batch):
+        """Attention over keys and values made of the latents: [tokens][heads * vdim]."""
+        t, H, dt, width = q.shape[0], self.heads, TYPES[self.dtype], self.nope + self.vdim
+        held, start = batch.held, batch.rows
+        codes = torch.empty(held, self.latent, dtype=torch.int8, device=self.device)
+        scale = torch.empty(held, device=self.device)
+        key = torch.empty(held, self.rope, dtype=self.dtype, device=self.device)
+        fx.latent_read(self.h, cache.desc, batch, start, held, codes, self.latent, scale, None, 0, key, self.rope, dt)
+        w, w_scale = self.kv
+        kv = torch.empty(held, H * width, dtype=self.dtype, device=self.device)
+        need = fx.token_gemm_workspace(held, H * width, self.latent)
+        fx.token_gemm(self.h, held, H * width, self.latent, codes, self.latent, scale, w, w_scale, None, kv, dt, H * width,
+                      self._workspace(need), need)
+        desc = fx.expanded_kv(kv, H * width, width, key, self.rope, kv[:, self.nope :], H * width, width, start, held, H,
+                              self.nope, self.rope, self.vdim)
+        out = torch.empty(t, H * self.vdim, dtype=self.dtype, device=self.device)
+        fx.expanded_attention(self.h, desc, batch, q, q.shape[1], 1 / math.sqrt(self.nope + self.rope), True, out,
+                              H * self.vdim, dt)
+        return out
+
+
+def main(prompt=512, steps=16, seqs=8, latent=False):
     pages = -(-(2 * prompt + steps + 1) // 16)
-    cache = Cache(pages=seqs * pages, page=16, heads=4, dim=64, max_pages_per_seq=pages, max_seqs=seqs)
+    if latent:
+        layer = LatentLayer(1024, 16, 64, 32, 64, 256, experts=8, top=2, inner=1024)
+        cache = LatentCache(pages=seqs * pages, page=16, latent=256, rope=32, max_pages_per_seq=pages, max_seqs=seqs)
+    else:
+        layer = Layer(1024, 16, 4, 64, experts=8, top=2, inner=1024)
+        cache = Cache(pages=seqs * pages, page=16, heads=4, dim=64, max_pages_per_seq=pages, max_seqs=seqs)
     ids = list(range(seqs))
     # the first prompt and step load the kernels
     for name, new, count in (("first prompt", [prompt] * seqs, 1), ("first step", [1] * seqs, 1),
@@ -225,4 +351,4 @@ def main(prompt=512, steps=16, seqs=8):
 
 
 if __name__ == "__main__":
-    sys.exit(main())
+    sys.exit(main(latent="latent" in sys.argv[1:]))

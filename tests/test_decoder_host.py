@@ -174,3 +174,48 @@ def test_failed_forward_of_a_batch_made_by_hand(dec):
     with pytest.raises(ValueError):
         layer.forward(torch.zeros(4, 64), cache, batch)
     assert cache.length == {} and len(cache.free) == 8
+
+
+def make_latent(dec, **kw):
+    layer = dec.LatentLayer(64, 4, 64, 32, 64, 256, experts=4, top=2, inner=48, dtype=torch.float32, device="cpu", **kw)
+    cache = dec.LatentCache(pages=8, page=16, latent=256, rope=32, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    return layer, cache
+
+
+@pytest.fixture
+def latent(dec, monkeypatch):
+    rec = dec.fx
+    monkeypatch.setattr(type(rec), "latent_cache", lambda self, codes, scale, rope_scale, pages, page, latent, rope:
+                        types.SimpleNamespace(pages=pages, page=page, latent=latent, rope=rope), raising=False)
+    monkeypatch.setattr(type(rec), "latent_attention_workspace", lambda self, *a: 1024, raising=False)
+    return dec
+
+
+def test_latent_layer_takes_the_form_that_its_new_tokens_ask_for(latent):
+    layer, cache = make_latent(latent)
+    for new, want in ((1, "latent_attention"), (layer.FEW, "latent_attention"), (layer.FEW + 1, "expanded_attention")):
+        batch = cache.extend([new], [new])
+        latent.fx.calls.clear()
+        layer.forward(torch.zeros(new, 64), cache, batch)
+        names = latent.fx.names()
+        assert want in names and names.index("latent_append") < names.index(want)
+        assert ("latent_read" in names) == (want == "expanded_attention")
+        assert batch.held == new and batch.rows.tolist() == [0, new]
+        cache.release(new)
+
+
+def test_latent_layer_without_new_tokens_and_with_another_cache(latent):
+    layer, cache = make_latent(latent)
+    cache.extend([0], [5])
+    assert layer.forward(torch.zeros(0, 64), cache, cache.extend([0], [0])).shape == (0, 64)
+    batch = cache.extend([0], [2])
+    small = latent.LatentCache(pages=8, page=16, latent=512, rope=32, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    heads = latent.Cache(pages=8, page=16, heads=2, dim=16, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    for other in (small, heads):
+        with pytest.raises(ValueError):
+            layer.forward(torch.zeros(2, 64), other, batch)
+    assert cache.length == {0: 7}
+    other_layer, _ = make(latent)
+    with pytest.raises(ValueError):
+        other_layer.forward(torch.zeros(2, 64), cache, cache.extend([0], [2]))
+    assert cache.length == {0: 7}  # that cache took its batch back
