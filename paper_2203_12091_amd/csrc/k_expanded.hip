@@ -65,8 +65,6 @@ __device__ inline float over_groups(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
-template <typename T>
-__device__ inline bool real_finite(T x) { return finite((float)x); }
 
 // Panels of 128 bytes of a token's row, and a piece's place in its row.
 template <typename T>

@@ -112,10 +112,10 @@ __device__ inline unsigned codes4(const float* x, float inv) {
   return pack4((int)rintf(x[0] * inv), (int)rintf(x[1] * inv), (int)rintf(x[2] * inv), (int)rintf(x[3] * inv));
 }
 
-// blockIdx.x: first the keys' blocks, four waves of one token each, then the queries',
-// `q_tokens` tokens each; y: sequence.  LB: latent dimensions of a lane.
+// blockIdx.x: first the keys' blocks, four waves of one token each, then the queries', one
+// token each; y: sequence.  LB: latent dimensions of a lane.
 template <typename T, int LB, bool VEC>
-__global__ __launch_bounds__(256) void k_latent_append(LatentAppendArgs a, int key_blocks, int q_tokens) {
+__global__ __launch_bounds__(256) void k_latent_append(LatentAppendArgs a, int key_blocks) {
   const SeqDev s = seq_of(a.b, a.c.page, blockIdx.y);
   if (!s.ok || (s.fresh > 0 && a.rot.dims && s.len > a.rot.positions)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(a.flags, FXPQ_FLAG_RANGE);
@@ -123,26 +123,25 @@ __global__ __launch_bounds__(256) void k_latent_append(LatentAppendArgs a, int k
   }
   const int pos0 = s.len - s.fresh, R = a.c.rope;
   if ((int)blockIdx.x >= key_blocks) {
-    const int t0 = ((int)blockIdx.x - key_blocks) * q_tokens, per = R / 2 / kPairs, work = a.heads * per;
-    for (int t = t0; t < min(t0 + q_tokens, s.fresh); ++t) {
-      const int64_t row = s.first + (int64_t)t;
-      for (int i = threadIdx.x; i < work; i += 256) {
-        const int head = i / per, p0 = i % per * kPairs;
-        float y1[kPairs], y2[kPairs];
-        rotated<T, VEC>(static_cast<const T*>(a.q) + row * a.ldq + head * a.hdq, p0, a.rot, R, pos0 + (int64_t)t, y1, y2);
-        T* to = static_cast<T*>(a.q_out) + row * a.ldqo + head * a.hdqo;
-        if (a.rot.interleaved) {
-          float y[2 * kPairs];
+    const int t = (int)blockIdx.x - key_blocks, per = R / 2 / kPairs, work = a.heads * per;
+    if (t >= s.fresh) return;
+    const int64_t row = s.first + (int64_t)t;
+    for (int i = threadIdx.x; i < work; i += 256) {
+      const int head = i / per, p0 = i % per * kPairs;
+      float y1[kPairs], y2[kPairs];
+      rotated<T, VEC>(static_cast<const T*>(a.q) + row * a.ldq + head * a.hdq, p0, a.rot, R, pos0 + (int64_t)t, y1, y2);
+      T* to = static_cast<T*>(a.q_out) + row * a.ldqo + head * a.hdqo;
+      if (a.rot.interleaved) {
+        float y[2 * kPairs];
 #pragma unroll
-          for (int k = 0; k < kPairs; ++k) {
-            y[2 * k] = y1[k];
-            y[2 * k + 1] = y2[k];
-          }
-          put<T, VEC>(to + 2 * p0, y);
-        } else {
-          put<T, VEC>(to + p0, y1);
-          put<T, VEC>(to + p0 + R / 2, y2);
+        for (int k = 0; k < kPairs; ++k) {
+          y[2 * k] = y1[k];
+          y[2 * k + 1] = y2[k];
         }
+        put<T, VEC>(to + 2 * p0, y);
+      } else {
+        put<T, VEC>(to + p0, y1);
+        put<T, VEC>(to + p0 + R / 2, y2);
       }
     }
     return;
@@ -260,12 +259,11 @@ hipError_t launch_latent_append(const Ctx& c, LatentAppendArgs a, int type) {
     const bool vec = fits16(a.latent, a.ldc, 0, size) && fits16(a.key, a.ldr, 0, size) &&
                      (!a.heads || (fits16(a.q, a.ldq, a.hdq, size) && fits16(a.q_out, a.ldqo, a.hdqo, size))) &&
                      fits16(a.rot.cos, 0, 0, 4) && fits16(a.rot.sin, 0, 0, 4);
-    const int key_blocks = (a.b.max_new + 3) / 4, q_tokens = 1;
-    const int q_blocks = a.heads ? (a.b.max_new + q_tokens - 1) / q_tokens : 0;
+    const int key_blocks = (a.b.max_new + 3) / 4, q_blocks = a.heads ? a.b.max_new : 0;
     if ((int64_t)key_blocks + q_blocks > kMaxBlocks) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(key_blocks + q_blocks), (unsigned)a.b.seqs);
     auto run = [&](auto lb, auto v) {
-      k_latent_append<T, decltype(lb)::value, decltype(v)::value><<<grid, dim3(256), 0, c.stream>>>(a, key_blocks, q_tokens);
+      k_latent_append<T, decltype(lb)::value, decltype(v)::value><<<grid, dim3(256), 0, c.stream>>>(a, key_blocks);
       return hipGetLastError();
     };
     using std::integral_constant;

@@ -65,6 +65,7 @@ constexpr float kSlack = 8.0f;
 constexpr float kLift = 64.0f;
 constexpr int kLeastShare = 2;  // chunks
 constexpr float kLeastLog = -50.0f;  // of s_t / R, where it only moves the reference
+constexpr float kFar = 0x1p24f;  // logits past this have steps above 1: s_t / R would be rounded
 
 __device__ inline void lds_barrier() {
   asm volatile("" ::: "memory");
@@ -523,6 +524,13 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
         for (int i = 0; i < 4; ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(st[i] * inv), kLeastLog);
       };
+      auto top_of = [&](int r) __attribute__((always_inline)) {  // this lane's largest logit with s_t / R
+        float y = fmaf(z[r][0], qn[r], lg[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
+        return y;
+      };
+      auto is_far = [](float y) __attribute__((always_inline)) { return fabsf(y) > kFar && y != -INFINITY; };
       auto weigh = [&]() __attribute__((always_inline)) {  // P of this wave's tokens and rows to LDS
         const float lift = pow2_inverse(R) * kLift;
         float w[4];
@@ -557,10 +565,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
         bool some = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) > R;
 #pragma unroll
         for (int r = 0; r < QR; ++r) {
-          float y = fmaf(z[r][0], qn[r], lg[0]);
-#pragma unroll
-          for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
-          some |= y > mine(r) + kSlack;
+          const float y = top_of(r);
+          some |= y > mine(r) + kSlack || is_far(y);
         }
         over = __any(some);
       }
@@ -582,13 +588,19 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
         const float now_r = fmaxf(R, most);
         const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
         R = now_r;
+        // past kFar s_t / R (below 1) is left out of references: a logit's rounding would move it
+        // by more than they may be off
         logs();
+        bool far = false;
+#pragma unroll
+        for (int r = 0; r < QR; ++r) far |= is_far(top_of(r));
+        if (__any(far)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lg[i] = 0.0f;
+        }
 #pragma unroll
         for (int r = 0; r < QR; ++r) {
-          float y = fmaf(z[r][0], qn[r], lg[0]);
-#pragma unroll
-          for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
-          y = over_groups(y);
+          const float y = over_groups(top_of(r));
           if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = y;
         }
         lds_barrier();
@@ -596,10 +608,10 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           const int row = r * 16 + n;
-          const float y = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
+          const float top = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
           // what came before weighs `ratio` of what it did against the new R
           const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
-          const float now = y > before + kSlack ? y : before;
+          const float now = top > before + kSlack ? top : before;
           down[r] = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
           m[r] = now;
           const float f = down[r] * ratio;

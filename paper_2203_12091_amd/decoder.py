@@ -84,8 +84,6 @@ class Pages:
         batch = fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(seqs),
                             self.max_pages, sum(new), max(new), max(length))
         batch.grown = dict(zip(seqs, new))
-        batch.held = sum(length)
-        batch.rows = put(torch.tensor([0] + length).cumsum(0).to(torch.int32))  # where each sequence's tokens begin
         return batch
 
     def retract(self, batch):
@@ -127,6 +125,13 @@ class LatentCache(Pages):
         self.codes = torch.zeros(pages, page, latent + rope, dtype=torch.int8, device=device)
         self.scale, self.rope_scale = torch.zeros(pages, page, device=device), torch.zeros(pages, page, device=device)
         self.desc = fx.latent_cache(self.codes, self.scale, self.rope_scale, pages, page, latent, rope)
+
+    def extend(self, seqs, new):
+        batch = super().extend(seqs, new)
+        # all tokens of the sequences, and where each one's begin among them
+        rows = torch.tensor([0] + [self.length[s] for s in seqs]).cumsum(0)
+        batch.held, batch.rows = int(rows[-1]), rows.to(torch.int32).to(self.device)
+        return batch
 
 
 class Layer:

@@ -408,6 +408,77 @@ def test_latent_attention_of_huge_logits(fx, h, t, sign):
     assert ((got.double() - want).abs() <= want * ((lens[0] + 64) * 2.0 ** -23 + HALF_ULP[t] + 2.0 ** -22)).all()
 
 
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads", [4, 20])
+@pytest.mark.parametrize("size", [2.0 ** 14, 2.0 ** 30, 2.0 ** 70], ids=["2^14", "2^30", "2^70"])
+def test_latent_attention_of_large_logits_takes_the_largest(fx, h, t, heads, size):
+    """Logits past 2^24, which fp32 holds in steps above one: one token takes all.  The
+    logits of a row differ by 2^-9 of their size and more, so that all other weights are 0;
+    the result is off by the weight's rounding, which the sum does not share, and its own."""
+    lens = [1000]
+    cache = Cache(fx, lens, 256, 32, 64)
+    cache.fill(lens, 31, spread=0.6)
+    g = torch.Generator().manual_seed(2)
+    up = min(size, 2.0 ** 15) if t == "f16" else size
+    for scale in (0.7 * size / up, -0.7 * size / up) if size > 2.0 ** 14 else (0.7 * 2.0 ** 14, -0.7 * 2.0 ** 13):
+        q = (torch.rand(1, heads, 256, generator=g) + 1).mul(up).mul(torch.rand(1, heads, 256, generator=g).sub(0.5).sign()).to(TYPES[t])
+        qr = torch.zeros(1, heads, 32).to(TYPES[t])
+        _, v, _ = cache.held(0, lens[0])
+        x = q[0].double() @ v.t() * scale
+        top = x.topk(2, -1)
+        told = (top.values[:, 0] - top.values[:, 1]) / x.abs().amax(-1) > 2.0 ** -9
+        assert told.sum() >= heads // 2
+        want = v[top.indices[:, 0]]
+        got = run_latent(fx, h, cache, [1], lens, q, qr, scale, 0, t)[0].double()
+        assert fx.sync_status(h) == 0
+        uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+        assert ((got - want).abs() <= want.abs() * (uP + 8 * 2.0 ** -24 + 1.01 * HALF_ULP[t]))[told].all()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("power", [20, 24, 28, 60, 105])
+def test_latent_attention_of_equal_large_logits(fx, h, t, sign, power):
+    """Equal tokens, of logits that no float holds exactly: every weight is the same."""
+    lens = [700]
+    cache = Cache(fx, lens, 256, 32, 64)
+    cache.codes.fill_(101)
+    cache.scale.fill_(0.0137)
+    cache.rope_scale.fill_(0.0137)
+    q = torch.full((1, 20, 256), sign * 0.37 * 2.0 ** power).to(TYPES[t])
+    got = run_latent(fx, h, cache, [1], lens, q, torch.zeros(1, 20, 32).to(TYPES[t]), 1.1, 0, t)
+    assert fx.sync_status(h) == 0
+    want = 101 * float(torch.tensor(0.0137))
+    uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+    assert ((got.double() - want).abs() <= want * ((lens[0] + 64) * 2.0 ** -23 + HALF_ULP[t] * 1.01 + uP + 2.0 ** -22)).all()
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("below", [3, 9, 21, 34, 45])
+def test_latent_attention_of_large_logits_and_uneven_scales(fx, h, t, below):
+    """One token takes all through the shared key, and its latent's scale is 2^-below of
+    the others', whose logits are 0.  Weights are written as f16 and a scale's power of two
+    is in them: the result is off by 2^-24 of the others' values, besides its roundings."""
+    lens = [300]
+    cache = Cache(fx, lens, 256, 32, 64)
+    cache.codes.fill_(90)
+    cache.codes[..., 256:] = 0
+    cache.scale.fill_(1.0)
+    cache.rope_scale.fill_(1.0)
+    page = int(cache.table[0, 2])
+    cache.codes[page, 5, 256:] = 101
+    cache.scale[page, 5] = 2.0 ** -below
+    want = 90 * 2.0 ** -below
+    for power in range(20, 33):
+        for heads in (4, 20):
+            qr = torch.full((1, heads, 32), 0.37).to(TYPES[t])
+            scale = 2.0 ** power / (0.37 * 32 * 101)
+            got = run_latent(fx, h, cache, [1], lens, torch.zeros(1, heads, 256).to(TYPES[t]), qr, scale, 0, t).double()
+            assert fx.sync_status(h) == 0
+            uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+            assert ((got - want).abs() <= 90 * 2.0 ** -24 + want * (uP + 8 * 2.0 ** -24 + 1.01 * HALF_ULP[t])).all(), (power, heads)
+
+
 def test_latent_attention_page_outside_the_cache(fx, h):
     """Its tokens are not seen, and the flag is raised; a query that sees nothing gets 0."""
     lens = [100]
