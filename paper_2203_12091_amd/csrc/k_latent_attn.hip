@@ -30,9 +30,9 @@ typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 // How the work is split.  shared: each sequence's chunks are cut into equal parts of at
-// most `share` chunks, and the share is the smallest for which no group of row_tiles
-// blocks has more than `rounds` parts, whatever the sequences' lengths; parts of a
-// sequence are joined afterwards.  Otherwise a block takes a row tile of a sequence whole.
+// most `share` chunks, a block for each part and row tile; `groups` parts run at a time
+// and there are blocks for `rounds` times as many.  Parts of a sequence are joined
+// afterwards.  Otherwise a block takes a row tile of a sequence whole.
 struct LatentRun {
   LatentArgs a;
   int row_tiles, shared, groups, rounds, page_log2, vec;
@@ -64,6 +64,7 @@ constexpr float kSlack = 8.0f;
 // largest keep all 11 bits and smaller ones lose at most 2^-31 of it.
 constexpr float kLift = 64.0f;
 constexpr int kLeastShare = 2;  // chunks
+constexpr int kStartCost = 4;   // chunks that take as long as a block's start
 constexpr float kLeastLog = -50.0f;  // of s_t / R, where it only moves the reference
 constexpr float kFar = 0x1p24f;  // logits past this have steps above 1: s_t / R would be rounded
 
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   const unsigned oct = blockIdx.x / 8;
   const int group = (int)(oct / (unsigned)p.row_tiles * 8 + blockIdx.x % 8);
   const int tile = p.row_tiles - 1 - (int)(oct % (unsigned)p.row_tiles);  // the last rows see the most tokens
-  if (group >= p.groups) return;
+  if (group >= p.groups * p.rounds) return;
 
   // This lane's 16 bytes of each load of a group, whose tokens lie one after another in
   // their page.
@@ -206,524 +207,535 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
     from[i] = (uint32_t)(t * (D + rope) + piece * 16);
   }
 
-  int part = group, parts = p.groups;
-  do {
-    int seq = part, begin = 0, size = 0;
-    SeqDev s;
-    if (p.shared) {
-      // every wave finds the share and the part's sequence by itself, four sequences a lane
-      constexpr int kOwn = kMostSeqs / 64;
-      SeqDev d[kOwn];
-      int count[kOwn], all = 0;
+  const int part = group;
+  int seq = part, begin = 0, size = 0;
+  SeqDev s;
+  if (p.shared) {
+    // every wave finds the share and the part's sequence by itself, four sequences a lane
+    constexpr int kOwn = kMostSeqs / 64;
+    SeqDev d[kOwn];
+    int count[kOwn], all = 0;
 #pragma unroll
-      for (int e = 0; e < kOwn; ++e) {
-        const int i = lane + 64 * e;
-        count[e] = 0;
-        d[e] = SeqDev{0, 0, 0, false};
+    for (int e = 0; e < kOwn; ++e) {
+      const int i = lane + 64 * e;
+      count[e] = 0;
+      d[e] = SeqDev{0, 0, 0, false};
+      if (64 * e < seqs) {
+        d[e] = seq_of(p.a.b, P, min(i, seqs - 1));
+        if (!d[e].ok && blockIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+        if (i < seqs && d[e].ok) count[e] = rows_chunks(p, d[e], 0, d[e].fresh * heads);
+        int sum;
+        running_sum(count[e], lane, sum);
+        all += sum;
+      }
+    }
+    int parts, before[kOwn];
+    auto cut = [&](int share) __attribute__((always_inline)) {
+      const float inv = 1.0f / (float)share;
+      parts = 0;
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e)
         if (64 * e < seqs) {
-          d[e] = seq_of(p.a.b, P, min(i, seqs - 1));
-          if (!d[e].ok && blockIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
-          if (i < seqs && d[e].ok) count[e] = rows_chunks(p, d[e], 0, d[e].fresh * heads);
+          const int mine = quotient_up(count[e], share, inv);
           int sum;
-          running_sum(count[e], lane, sum);
-          all += sum;
+          before[e] = parts + running_sum(mine, lane, sum) - mine;
+          parts += sum;
         }
-      }
-      const int most = p.groups * p.rounds;
-      int share = max((all + most - 1) / most, kLeastShare), before[kOwn];
-      for (;;) {
-        const float inv = 1.0f / (float)share;
-        parts = 0;
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e)
-          if (64 * e < seqs) {
-            const int mine = quotient_up(count[e], share, inv);
-            int sum;
-            before[e] = parts + running_sum(mine, lane, sum) - mine;
-            parts += sum;
-          }
-        if (parts <= most) break;  // at the latest where no sequence has two
-        share += 1 + share / 16;
-      }
-      if (part >= parts) break;
-      // the last sequence whose first part is this or an earlier one (those without parts
-      // start where the next does)
-      seq = -1;
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e)
-        if (64 * e < seqs) {
-          const int i = lane + 64 * e;
-          seq += __popcll(__ballot(i < seqs && before[e] <= part));
-          if (blockIdx.x == 0 && wave == 0 && i < seqs) p.line[i] = before[e];
-        }
-      if (blockIdx.x == 0 && threadIdx.x == 0) p.line[seqs] = share;
-      int chunks = 0, first = 0;
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e)
-        if (seq >> 6 == e) {
-          const int at = seq & 63;
-          s = SeqDev{__builtin_amdgcn_readlane(d[e].first, at), __builtin_amdgcn_readlane(d[e].fresh, at),
-                     __builtin_amdgcn_readlane(d[e].len, at), true};
-          chunks = __builtin_amdgcn_readlane(count[e], at);
-          first = __builtin_amdgcn_readlane(before[e], at);
-        }
-      size = part_chunks(chunks, share);
-      begin = (part - first) * size;
-    } else {
-      s = block_seq(seq_of(p.a.b, P, seq));
-      if (!s.ok && tile == 0 && threadIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
-    }
-    const int row0 = tile * kRows, rows = s.ok ? s.fresh * heads : 0;
-    const int total = row0 < rows ? rows_chunks(p, s, row0, kRows) : 0;  // this tile's
-    const int end = p.shared ? min(begin + size, total) : total;
-    if (begin >= end) continue;
-    const int pos0 = s.len - s.fresh;
-    // read by scalar loads: they are not counted among the loads to LDS
-    const auto* table = (const __attribute__((address_space(4))) int32_t*)(p.a.b.table + (int64_t)seq * p.a.b.table_ld);
-    const int last_nth = (s.len - 1) >> page_log2;
-
-    // Page of this wave's tokens of a chunk; past the sequence's end -1.
-    auto page_of = [&](int chunk) __attribute__((always_inline)) {
-      const int nth = (chunk * 64 + tg * 16) >> page_log2;
-      return nth <= last_nth ? table[nth] : -1;
     };
-    auto load = [&](int chunk, int slot, int page) __attribute__((always_inline)) {
-      const int t = chunk * 64 + tg * 16;
-      const bool there = page >= 0 && page < pages;
-      if (!there && t < s.len && lane == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
-      const int64_t first = ((int64_t)(there ? page : 0) << page_log2) + (t & (P - 1));
-      const int8_t* base = codes + first * (D + rope);
-      int8_t* into = lds + slot * L::kSlot + tg * L::kGroup;
-#pragma unroll
-      for (int i = 0; i < kMine; ++i)
-        if (i + 1 < kMine || half == 0) dma16(base, from[i], into + (i + half * kHalf) * 1024);
-      if (W == 4 || half == 1)
-        dma4((g & 1 ? key_scale : latent_scale) + first + n, lds + L::kScales + (slot * 4 + tg) * 256);
-    };
-    lds_barrier();  // the part before has been left
-    // q as it is to LDS, its loads before the first chunk's
-    int8_t* ql = lds + L::kSlot;
-    constexpr int kQPieces = (D + 64) * (int)sizeof(T) / 16, kQAll = kRows * kQPieces;
-    int page = page_of(begin), page1 = page_of(begin + 1), page2 = page_of(begin + 2);
-    if (p.vec) {
-#pragma unroll 1
-      for (int i = wave * 64; i < kQAll; i += kThreads) {
-        const int at = i + lane, r = at / kQPieces, piece = at % kQPieces * (16 / (int)sizeof(T));  // first of 4 or 8 reals
-        const int row = min(row0 + r, rows - 1);  // rows behind the last: any
-        const int i_token = token_of(p, row);
-        const int64_t token = s.first + (int64_t)i_token, head = row - i_token * heads;
-        const T* src = piece < D ? static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq + piece
-                                 : static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr + (piece - D < rope ? piece - D : 0);
-        if (at < kQAll) dma16(reinterpret_cast<const int8_t*>(src), ql + i * 16);
+    // the share for which the parts, `groups` at a time, take the least time; there is one
+    // whose parts have blocks, at the latest where no sequence has two
+    const int most = p.groups * p.rounds;
+    int share = 0, cost = 0x7FFFFFFF;
+    for (int next = max((all + most - 1) / most, kLeastShare);; next += 1 + next / 16) {
+      cut(next);
+      if (parts > most) continue;
+      const int turns = (parts + p.groups - 1) / p.groups, now = turns * (next + kStartCost);
+      if (now < cost) {
+        cost = now;
+        share = next;
+      }
+      if (turns <= 1 || next + kStartCost >= cost) {
+        if (share != next) cut(share);
+        break;
       }
     }
-    load(begin, 0, page);
-    if (p.vec) wait_vmcnt<kWaveLoads>();
-    lds_barrier();
+    if (part >= parts) return;
+    // the last sequence whose first part is this or an earlier one (those without parts
+    // start where the next does)
+    seq = -1;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e)
+      if (64 * e < seqs) {
+        const int i = lane + 64 * e;
+        seq += __popcll(__ballot(i < seqs && before[e] <= part));
+        if (blockIdx.x == 0 && wave == 0 && i < seqs) p.line[i] = before[e];
+      }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.line[seqs] = share;
+    int chunks = 0, first = 0;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e)
+      if (seq >> 6 == e) {
+        const int at = seq & 63;
+        s = SeqDev{__builtin_amdgcn_readlane(d[e].first, at), __builtin_amdgcn_readlane(d[e].fresh, at),
+                   __builtin_amdgcn_readlane(d[e].len, at), true};
+        chunks = __builtin_amdgcn_readlane(count[e], at);
+        first = __builtin_amdgcn_readlane(before[e], at);
+      }
+    size = part_chunks(chunks, share);
+    begin = (part - first) * size;
+  } else {
+    s = block_seq(seq_of(p.a.b, P, seq));
+    if (!s.ok && tile == 0 && threadIdx.x == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+  }
+  const int row0 = tile * kRows, rows = s.ok ? s.fresh * heads : 0;
+  const int total = row0 < rows ? rows_chunks(p, s, row0, kRows) : 0;  // this tile's
+  const int end = p.shared ? min(begin + size, total) : total;
+  if (begin >= end) return;
+  const int pos0 = s.len - s.fresh;
+  // read by scalar loads: they are not counted among the loads to LDS
+  const auto* table = (const __attribute__((address_space(4))) int32_t*)(p.a.b.table + (int64_t)seq * p.a.b.table_ld);
+  const int last_nth = (s.len - 1) >> page_log2;
 
-    // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
-    // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity;
-    // behind it -1152 times the sums of the latent's and the key's parts.
-    float* rowq = tops;
-    {
-      const int sub = threadIdx.x & 15;
-      constexpr int V = 16 / sizeof(T), N = LB * 4 / V;  // LB * 4 latent reals and 4 of the key a thread
-      static_assert(sizeof(T) == 2 || kRows * 16 == kThreads, "f32 rows are read before any is written");
+  // Page of this wave's tokens of a chunk; past the sequence's end -1.
+  auto page_of = [&](int chunk) __attribute__((always_inline)) {
+    const int nth = (chunk * 64 + tg * 16) >> page_log2;
+    return nth <= last_nth ? table[nth] : -1;
+  };
+  auto load = [&](int chunk, int slot, int page) __attribute__((always_inline)) {
+    const int t = chunk * 64 + tg * 16;
+    const bool there = page >= 0 && page < pages;
+    if (!there && t < s.len && lane == 0) raise_flag(flags, FXPQ_FLAG_RANGE);
+    const int64_t first = ((int64_t)(there ? page : 0) << page_log2) + (t & (P - 1));
+    const int8_t* base = codes + first * (D + rope);
+    int8_t* into = lds + slot * L::kSlot + tg * L::kGroup;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+      if (i + 1 < kMine || half == 0) dma16(base, from[i], into + (i + half * kHalf) * 1024);
+    if (W == 4 || half == 1)
+      dma4((g & 1 ? key_scale : latent_scale) + first + n, lds + L::kScales + (slot * 4 + tg) * 256);
+  };
+  // q as it is to LDS, its loads before the first chunk's
+  int8_t* ql = lds + L::kSlot;
+  constexpr int kQPieces = (D + 64) * (int)sizeof(T) / 16, kQAll = kRows * kQPieces;
+  int page = page_of(begin), page1 = page_of(begin + 1), page2 = page_of(begin + 2);
+  if (p.vec) {
 #pragma unroll 1
-      for (int r = threadIdx.x >> 4; r < kRows; r += kThreads / 16) {
-        const int row = row0 + r;
-        const bool real = row < rows;
-        float x[LB * 4 + 4];
-        if (p.vec) {
-          const T* raw = reinterpret_cast<const T*>(ql) + r * (D + 64);
+    for (int i = wave * 64; i < kQAll; i += kThreads) {
+      const int at = i + lane, r = at / kQPieces, piece = at % kQPieces * (16 / (int)sizeof(T));  // first of 4 or 8 reals
+      const int row = min(row0 + r, rows - 1);  // rows behind the last: any
+      const int i_token = token_of(p, row);
+      const int64_t token = s.first + (int64_t)i_token, head = row - i_token * heads;
+      const T* src = piece < D ? static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq + piece
+                               : static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr + (piece - D < rope ? piece - D : 0);
+      if (at < kQAll) dma16(reinterpret_cast<const int8_t*>(src), ql + i * 16);
+    }
+  }
+  load(begin, 0, page);
+  if (p.vec) wait_vmcnt<kWaveLoads>();
+  lds_barrier();
+
+  // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
+  // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity;
+  // behind it -1152 times the sums of the latent's and the key's parts.
+  float* rowq = tops;
+  {
+    const int sub = threadIdx.x & 15;
+    constexpr int V = 16 / sizeof(T), N = LB * 4 / V;  // LB * 4 latent reals and 4 of the key a thread
+    static_assert(sizeof(T) == 2 || kRows * 16 == kThreads, "f32 rows are read before any is written");
+#pragma unroll 1
+    for (int r = threadIdx.x >> 4; r < kRows; r += kThreads / 16) {
+      const int row = row0 + r;
+      const bool real = row < rows;
+      float x[LB * 4 + 4];
+      if (p.vec) {
+        const T* raw = reinterpret_cast<const T*>(ql) + r * (D + 64);
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            float u[V];
-            load_reals<T, V>(raw + (k * 16 + sub) * V, u);
+        for (int k = 0; k < N; ++k) {
+          float u[V];
+          load_reals<T, V>(raw + (k * 16 + sub) * V, u);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[k * V + j] = u[j];
-          }
-          float u[4];
-          load_reals<T, 4>(raw + D + 4 * sub, u);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? u[j] : 0.0f;
-        } else {
-          const int i_token = real ? token_of(p, row) : 0;
-          const int64_t token = s.first + (int64_t)i_token, head = real ? row - i_token * heads : 0;
-          const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
-          const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
-#pragma unroll
-          for (int k = 0; k < LB * 4; ++k) x[k] = (float)ql_from[(k / V * 16 + sub) * V + k % V];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? (float)qr_from[4 * sub + j] : 0.0f;
+          for (int j = 0; j < V; ++j) x[k * V + j] = u[j];
         }
-        unsigned top = 0;
+        float u[4];
+        load_reals<T, 4>(raw + D + 4 * sub, u);
 #pragma unroll
-        for (int k = 0; k < LB * 4 + 4; ++k) {
-          if (!real) x[k] = 0.0f;
-          top = max(top, __builtin_bit_cast(unsigned, x[k]) & 0x7FFFFFFFu);
-        }
-        // (the bits of magnitudes are ordered as integers, NaN above infinity)
-        top = max(top, (unsigned)lanes<0xB1>((int)top));
-        top = max(top, (unsigned)lanes<0x4E>((int)top));
-        top = max(top, (unsigned)lanes<0x141>((int)top));
-        top = max(top, (unsigned)lanes<0x140>((int)top));
-        const bool fine = top < 0x7F800000u;
-        const float step = __builtin_bit_cast(
-            float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
-        const float up = pow2_inverse(step) * 0x1p13f;
+        for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? u[j] : 0.0f;
+      } else {
+        const int i_token = real ? token_of(p, row) : 0;
+        const int64_t token = s.first + (int64_t)i_token, head = real ? row - i_token * heads : 0;
+        const T* ql_from = static_cast<const T*>(p.a.q) + token * p.a.ldq + head * p.a.hdq;
+        const T* qr_from = static_cast<const T*>(p.a.qr) + token * p.a.ldqr + head * p.a.hdqr;
 #pragma unroll
-        for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
-        float total_l = 0.0f, total_r = 0.0f;
-        if constexpr (sizeof(T) == 4) lds_barrier();
+        for (int k = 0; k < LB * 4; ++k) x[k] = (float)ql_from[(k / V * 16 + sub) * V + k % V];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          int8_t* to_lds = ql + t * L::kQ + r * L::kQRow;
+        for (int j = 0; j < 4; ++j) x[LB * 4 + j] = 4 * sub < rope ? (float)qr_from[4 * sub + j] : 0.0f;
+      }
+      unsigned top = 0;
 #pragma unroll
-          for (int k = 0; k < N + 1; ++k) {
-            const int w = k < N ? V : 4, d = k < N ? (k * 16 + sub) * V : D + 4 * sub;
+      for (int k = 0; k < LB * 4 + 4; ++k) {
+        if (!real) x[k] = 0.0f;
+        top = max(top, __builtin_bit_cast(unsigned, x[k]) & 0x7FFFFFFFu);
+      }
+      // (the bits of magnitudes are ordered as integers, NaN above infinity)
+      top = max(top, (unsigned)lanes<0xB1>((int)top));
+      top = max(top, (unsigned)lanes<0x4E>((int)top));
+      top = max(top, (unsigned)lanes<0x141>((int)top));
+      top = max(top, (unsigned)lanes<0x140>((int)top));
+      const bool fine = top < 0x7F800000u;
+      const float step = __builtin_bit_cast(
+          float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
+      const float up = pow2_inverse(step) * 0x1p13f;
 #pragma unroll
-            for (int j = 0; j < w; j += 4) {
-              v4h y;
+      for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
+      float total_l = 0.0f, total_r = 0.0f;
+      if constexpr (sizeof(T) == 4) lds_barrier();
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                y[e] = (_Float16)x[k * V + j + e];
-                if (kBiased) (k < N ? total_l : total_r) += (float)y[e];
-                x[k * V + j + e] -= (float)y[e];
-              }
-              *reinterpret_cast<v4h*>(to_lds + (d + j) * 2) = y;
+      for (int t = 0; t < QT; ++t) {
+        int8_t* to_lds = ql + t * L::kQ + r * L::kQRow;
+#pragma unroll
+        for (int k = 0; k < N + 1; ++k) {
+          const int w = k < N ? V : 4, d = k < N ? (k * 16 + sub) * V : D + 4 * sub;
+#pragma unroll
+          for (int j = 0; j < w; j += 4) {
+            v4h y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              y[e] = (_Float16)x[k * V + j + e];
+              if (kBiased) (k < N ? total_l : total_r) += (float)y[e];
+              x[k * V + j + e] -= (float)y[e];
             }
+            *reinterpret_cast<v4h*>(to_lds + (d + j) * 2) = y;
           }
-        }
-        if constexpr (kBiased) {
-          const auto plus = [](float a, float b) { return a + b; };
-          total_l = over_16(total_l, plus);
-          total_r = over_16(total_r, plus);
-        }
-        if (sub == 0) {
-          rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
-          rowq[kRows + r] = -1152.0f * total_l;
-          rowq[2 * kRows + r] = -1152.0f * total_r;
         }
       }
+      if constexpr (kBiased) {
+        const auto plus = [](float a, float b) { return a + b; };
+        total_l = over_16(total_l, plus);
+        total_r = over_16(total_r, plus);
+      }
+      if (sub == 0) {
+        rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
+        rowq[kRows + r] = -1152.0f * total_l;
+        rowq[2 * kRows + r] = -1152.0f * total_r;
+      }
     }
-    if (threadIdx.x < 2) raised[threadIdx.x] = 0;
-    lds_barrier();
-    v8h q[QT][QR][2 * KB];  // lane: row n of tile r, dimensions 64 b + 16 g + 8 h + 0..7 at 2 b + h
-    float qn[QR], bias_l[QR], bias_r[QR];
-    int limit[QR];
+  }
+  if (threadIdx.x < 2) raised[threadIdx.x] = 0;
+  lds_barrier();
+  v8h q[QT][QR][2 * KB];  // lane: row n of tile r, dimensions 64 b + 16 g + 8 h + 0..7 at 2 b + h
+  float qn[QR], bias_l[QR], bias_r[QR];
+  int limit[QR];
 #pragma unroll
-    for (int r = 0; r < QR; ++r) {
-      const int row = (half * QR + r) * 16 + n;
-      limit[r] = causal ? pos0 + token_of(p, row0 + row) : s.len - 1;
-      qn[r] = rowq[row];
-      bias_l[r] = kBiased ? rowq[kRows + row] : 0.0f;
-      bias_r[r] = kBiased ? rowq[2 * kRows + row] : 0.0f;
+  for (int r = 0; r < QR; ++r) {
+    const int row = (half * QR + r) * 16 + n;
+    limit[r] = causal ? pos0 + token_of(p, row0 + row) : s.len - 1;
+    qn[r] = rowq[row];
+    bias_l[r] = kBiased ? rowq[kRows + row] : 0.0f;
+    bias_r[r] = kBiased ? rowq[2 * kRows + row] : 0.0f;
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int b = 0; b < 2 * KB; ++b)
-          q[t][r][b] = *reinterpret_cast<const v8h*>(lds + L::kSlot + t * L::kQ + row * L::kQRow +
-                                                     (64 * (b >> 1) + 16 * g + 8 * (b & 1)) * 2);
-    }
-    lds_barrier();
-    if (L::kSlots == 3 && begin + 1 < end) load(begin + 1, 1, page1);
+      for (int b = 0; b < 2 * KB; ++b)
+        q[t][r][b] = *reinterpret_cast<const v8h*>(lds + L::kSlot + t * L::kQ + row * L::kQRow +
+                                                   (64 * (b >> 1) + 16 * g + 8 * (b & 1)) * 2);
+  }
+  lds_barrier();
+  if (L::kSlots == 3 && begin + 1 < end) load(begin + 1, 1, page1);
 
-    // references of all rows of the block, the same in all waves; sums of this wave's own
-    float m[RT], l[QR], R = 0.0f;
-    v4f o[RT][CB];
+  // references of all rows of the block, the same in all waves; sums of this wave's own
+  float m[RT], l[QR], R = 0.0f;
+  v4f o[RT][CB];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      m[r] = kNoMax;
+  for (int r = 0; r < RT; ++r) {
+    m[r] = kNoMax;
 #pragma unroll
-      for (int c = 0; c < CB; ++c) o[r][c] = v4f{0, 0, 0, 0};
-    }
+    for (int c = 0; c < CB; ++c) o[r][c] = v4f{0, 0, 0, 0};
+  }
 #pragma unroll
-    for (int r = 0; r < QR; ++r) l[r] = 0.0f;
-    auto mine = [&](int r) __attribute__((always_inline)) { return half ? m[(H - 1) * QR + r] : m[r]; };
-    const int first_limit = causal ? pos0 + token_of(p, row0) : s.len - 1;
-    int slot = 0;
+  for (int r = 0; r < QR; ++r) l[r] = 0.0f;
+  auto mine = [&](int r) __attribute__((always_inline)) { return half ? m[(H - 1) * QR + r] : m[r]; };
+  const int first_limit = causal ? pos0 + token_of(p, row0) : s.len - 1;
+  int slot = 0;
 #pragma unroll 1
-    for (int chunk = begin; chunk < end; ++chunk) {
-      const int buf = (chunk - begin) & 1;
-      int8_t* pb = lds + L::kWeights + buf * QT * L::kP;
-      const bool there = page >= 0 && page < pages;
-      // this wave's loads have landed; the next chunk's may be on their way
-      if (L::kSlots == 3 && chunk + 1 < end) wait_vmcnt<kWaveLoads>();
-      else wait_vmcnt<0>();
-      if constexpr (W == 8) lds_barrier();  // and the other half of its tokens
-      else asm volatile("" ::: "memory");
-      const int8_t* own = lds + slot * L::kSlot + tg * L::kGroup;
-      const int t0 = chunk * 64 + tg * 16 + 4 * g;  // this lane's four tokens of S
-      float st[4], cs[4], rs[4];
-      {
-        const float* sc = reinterpret_cast<const float*>(lds + L::kScales + (slot * 4 + tg) * 256) + 4 * g;
-        v4f a = *reinterpret_cast<const v4f*>(sc), b = *reinterpret_cast<const v4f*>(sc + 16);
-        if (!there || chunk * 64 + 64 > s.len) {
-          // scales: 0 for what is no token of the sequence (its memory may hold anything)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool in = there && t0 + i < s.len;
-            a[i] = in ? a[i] : 0.0f;
-            b[i] = in ? b[i] : 0.0f;
-          }
-        }
+  for (int chunk = begin; chunk < end; ++chunk) {
+    const int buf = (chunk - begin) & 1;
+    int8_t* pb = lds + L::kWeights + buf * QT * L::kP;
+    const bool there = page >= 0 && page < pages;
+    // this wave's loads have landed; the next chunk's may be on their way
+    if (L::kSlots == 3 && chunk + 1 < end) wait_vmcnt<kWaveLoads>();
+    else wait_vmcnt<0>();
+    if constexpr (W == 8) lds_barrier();  // and the other half of its tokens
+    else asm volatile("" ::: "memory");
+    const int8_t* own = lds + slot * L::kSlot + tg * L::kGroup;
+    const int t0 = chunk * 64 + tg * 16 + 4 * g;  // this lane's four tokens of S
+    float st[4], cs[4], rs[4];
+    {
+      const float* sc = reinterpret_cast<const float*>(lds + L::kScales + (slot * 4 + tg) * 256) + 4 * g;
+      v4f a = *reinterpret_cast<const v4f*>(sc), b = *reinterpret_cast<const v4f*>(sc + 16);
+      if (!there || chunk * 64 + 64 > s.len) {
+        // scales: 0 for what is no token of the sequence (its memory may hold anything)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          st[i] = a[i];
-          cs[i] = a[i] * to_log2;
-          rs[i] = b[i] * to_log2;
+          const bool in = there && t0 + i < s.len;
+          a[i] = in ? a[i] : 0.0f;
+          b[i] = in ? b[i] : 0.0f;
         }
       }
-      // all operands first: one wait for LDS
-      v4i raw[KB];
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
-        raw[b] = *reinterpret_cast<const v4i*>(own + n * L::kRow + (b < LB ? (4 * b + g) ^ (n >> 2) : LB * 4 + g) * 16);
-      __builtin_amdgcn_sched_barrier(0);
-      // two sums for the latent, so that a product need not wait for the last
-      v4f part[2][QR], turned[QR];
-#pragma unroll
-      for (int r = 0; r < QR; ++r) {
-        part[0][r] = v4f{bias_l[r], bias_l[r], bias_l[r], bias_l[r]};
-        part[1][r] = v4f{0, 0, 0, 0};
-        turned[r] = v4f{bias_r[r], bias_r[r], bias_r[r], bias_r[r]};
+      for (int i = 0; i < 4; ++i) {
+        st[i] = a[i];
+        cs[i] = a[i] * to_log2;
+        rs[i] = b[i] * to_log2;
       }
+    }
+    // all operands first: one wait for LDS
+    v4i raw[KB];
 #pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        v8h k[2];
-        codes_to_halves<kBiased>(raw[b], k[0], k[1]);
+    for (int b = 0; b < KB; ++b)
+      raw[b] = *reinterpret_cast<const v4i*>(own + n * L::kRow + (b < LB ? (4 * b + g) ^ (n >> 2) : LB * 4 + g) * 16);
+    __builtin_amdgcn_sched_barrier(0);
+    // two sums for the latent, so that a product need not wait for the last
+    v4f part[2][QR], turned[QR];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int r = 0; r < QR; ++r) {
+      part[0][r] = v4f{bias_l[r], bias_l[r], bias_l[r], bias_l[r]};
+      part[1][r] = v4f{0, 0, 0, 0};
+      turned[r] = v4f{bias_r[r], bias_r[r], bias_r[r], bias_r[r]};
+    }
 #pragma unroll
-          for (int t = 0; t < QT; ++t)
+    for (int b = 0; b < KB; ++b) {
+      v8h k[2];
+      codes_to_halves<kBiased>(raw[b], k[0], k[1]);
 #pragma unroll
-            for (int r = 0; r < QR; ++r) {
-              v4f& acc = b < LB ? part[h][r] : turned[r];
-              acc = mfma(k[h], q[t][r][2 * b + h], acc);
-            }
-      }
-      v4f sum[QR];
-#pragma unroll
-      for (int r = 0; r < QR; ++r) sum[r] = part[0][r] + part[1][r];
-      float z[QR][4];  // logits, but for the row's power of two
-#pragma unroll
-      for (int r = 0; r < QR; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[r][i] = fmaf(turned[r][i], rs[i], sum[r][i] * cs[i]);
-      if (chunk * 64 + 63 > first_limit || !there) {
-#pragma unroll
-        for (int r = 0; r < QR; ++r)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (t0 + i > limit[r] || !there) z[r][i] = -INFINITY;
-      }
-      float add[QR], lg[4];
-      auto logs = [&]() __attribute__((always_inline)) {
-        const float inv = R > 0.0f ? pow2_inverse(R) : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(st[i] * inv), kLeastLog);
-      };
-      auto top_of = [&](int r) __attribute__((always_inline)) {  // this lane's largest logit with s_t / R
-        float y = fmaf(z[r][0], qn[r], lg[0]);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
-        return y;
-      };
-      auto is_far = [](float y) __attribute__((always_inline)) { return fabsf(y) > kFar && y != -INFINITY; };
-      auto weigh = [&]() __attribute__((always_inline)) {  // P of this wave's tokens and rows to LDS
-        const float lift = pow2_inverse(R) * kLift;
-        float w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = st[i] * lift;
-#pragma unroll
-        for (int r = 0; r < QR; ++r) {
-          float rest[4];
-          add[r] = 0.0f;
-          const float ref = -mine(r);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(z[r][i], qn[r], ref));
-            add[r] += e;
-            rest[i] = e * w[i];
-          }
-#pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            v4h h;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              h[i] = (_Float16)rest[i];
-              rest[i] -= (float)h[i];
-            }
-            *reinterpret_cast<v4h*>(pb + t * L::kP + ((half * QR + r) * 16 + n) * L::kPRow + tg * 32 + g * 8) = h;
-          }
-        }
-      };
-      logs();
-      bool over = chunk == begin;
-      if (!over) {
-        bool some = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) > R;
-#pragma unroll
-        for (int r = 0; r < QR; ++r) {
-          const float y = top_of(r);
-          some |= y > mine(r) + kSlack || is_far(y);
-        }
-        over = __any(some);
-      }
-      if (over) {
-        if (lane == 0) raised[buf] = chunk + 1;
-      } else {
-        weigh();
-      }
-      lds_barrier();
-      if (raised[buf] == chunk + 1) {
-        // new references: the scales' first, then each row's, over all groups of tokens
-        float most = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
-        most = over_groups(most);
-        if (lane == 0) scales[tg] = most;
-        lds_barrier();
-        most = fmaxf(fmaxf(fmaxf(scales[0], scales[1]), fmaxf(scales[2], scales[3])), 0x1p-110f);
-        // the power of two above it
-        most = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, most) & 0x7F800000u) + 0x00800000u);
-        const float now_r = fmaxf(R, most);
-        const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
-        R = now_r;
-        // past kFar s_t / R (below 1) is left out of references: a logit's rounding would move it
-        // by more than they may be off
-        logs();
-        bool far = false;
-#pragma unroll
-        for (int r = 0; r < QR; ++r) far |= is_far(top_of(r));
-        if (__any(far)) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) lg[i] = 0.0f;
-        }
-#pragma unroll
-        for (int r = 0; r < QR; ++r) {
-          const float y = over_groups(top_of(r));
-          if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = y;
-        }
-        lds_barrier();
-        float down[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const int row = r * 16 + n;
-          const float top = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
-          // what came before weighs `ratio` of what it did against the new R
-          const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
-          const float now = top > before + kSlack ? top : before;
-          down[r] = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
-          m[r] = now;
-          const float f = down[r] * ratio;
-#pragma unroll
-          for (int c = 0; c < CB; ++c) o[r][c] *= f;
-        }
-#pragma unroll
-        for (int r = 0; r < QR; ++r) l[r] *= half ? down[(H - 1) * QR + r] : down[r];
-        weigh();
-        lds_barrier();
-      }
-#pragma unroll
-      for (int r = 0; r < QR; ++r) l[r] += add[r];
-      // all waves have left the chunk before: its slot takes the next but one, or of two
-      // slots the next
-      constexpr int kAhead = L::kSlots - 1;
-      if (chunk + kAhead < end) load(chunk + kAhead, slot == 0 ? kAhead : slot - 1, kAhead == 2 ? page2 : page1);
-      page = page1;
-      page1 = page2;
-      page2 = page_of(chunk + 3);
-      // lane: dimensions CB n + 0 .. CB - 1 of this wave's part, of tokens 32 u + 8 g + 0 .. 7
-      const int8_t* all = lds + slot * L::kSlot;
-      unsigned w[2][8][(CB + 3) / 4];
-      v8h pf[2][QT][RT];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          // token 8 (g % 2) + j of group 2 u + g / 2
-          const int byte = wave * CB * 16 + CB * n, piece = (byte >> 4) ^ (2 * (g & 1) + (j >> 2));
-          const int8_t* src = all + (2 * u + (g >> 1)) * L::kGroup + (8 * (g & 1) + j) * L::kRow + piece * 16 + (byte & 15);
-          if constexpr (CB == 8) {
-            const uint2 v = *reinterpret_cast<const uint2*>(src);
-            w[u][j][0] = v.x;
-            w[u][j][1] = v.y;
-          } else if constexpr (CB == 4) {
-            w[u][j][0] = *reinterpret_cast<const unsigned*>(src);
-          } else {
-            w[u][j][0] = *reinterpret_cast<const uint16_t*>(src);
-          }
-        }
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int r = 0; r < RT; ++r)
-            pf[u][t][r] = *reinterpret_cast<const v8h*>(pb + t * L::kP + (r * 16 + n) * L::kPRow + u * 64 + g * 16);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          v4i f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = pair_of(w[u][2 * j][c / 4], w[u][2 * j + 1][c / 4], c % 4);
-          const v8h v = __builtin_bit_cast(v8h, f);
-#pragma unroll
-          for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) o[r][c] = mfma(v, pf[u][t][r], o[r][c]);
-        }
-      slot = slot == L::kSlots - 1 ? 0 : slot + 1;
+          for (int r = 0; r < QR; ++r) {
+            v4f& acc = b < LB ? part[h][r] : turned[r];
+            acc = mfma(k[h], q[t][r][2 * b + h], acc);
+          }
     }
-
-    // the rows' sums over lanes and waves
-    lds_barrier();
+    v4f sum[QR];
 #pragma unroll
-    for (int r = 0; r < QR; ++r) {
-      l[r] += __shfl_xor(l[r], 16);
-      l[r] += __shfl_xor(l[r], 32);
-      if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = l[r];
+    for (int r = 0; r < QR; ++r) sum[r] = part[0][r] + part[1][r];
+    float z[QR][4];  // logits, but for the row's power of two
+#pragma unroll
+    for (int r = 0; r < QR; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[r][i] = fmaf(turned[r][i], rs[i], sum[r][i] * cs[i]);
+    if (chunk * 64 + 63 > first_limit || !there) {
+#pragma unroll
+      for (int r = 0; r < QR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t0 + i > limit[r] || !there) z[r][i] = -INFINITY;
+    }
+    float add[QR], lg[4];
+    auto logs = [&]() __attribute__((always_inline)) {
+      const float inv = R > 0.0f ? pow2_inverse(R) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lg[i] = fmaxf(__builtin_amdgcn_logf(st[i] * inv), kLeastLog);
+    };
+    auto top_of = [&](int r) __attribute__((always_inline)) {  // this lane's largest logit with s_t / R
+      float y = fmaf(z[r][0], qn[r], lg[0]);
+#pragma unroll
+      for (int i = 1; i < 4; ++i) y = fmaxf(y, fmaf(z[r][i], qn[r], lg[i]));
+      return y;
+    };
+    auto is_far = [](float y) __attribute__((always_inline)) { return fabsf(y) > kFar && y != -INFINITY; };
+    auto weigh = [&]() __attribute__((always_inline)) {  // P of this wave's tokens and rows to LDS
+      const float lift = pow2_inverse(R) * kLift;
+      float w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = st[i] * lift;
+#pragma unroll
+      for (int r = 0; r < QR; ++r) {
+        float rest[4];
+        add[r] = 0.0f;
+        const float ref = -mine(r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(z[r][i], qn[r], ref));
+          add[r] += e;
+          rest[i] = e * w[i];
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          v4h h;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            h[i] = (_Float16)rest[i];
+            rest[i] -= (float)h[i];
+          }
+          *reinterpret_cast<v4h*>(pb + t * L::kP + ((half * QR + r) * 16 + n) * L::kPRow + tg * 32 + g * 8) = h;
+        }
+      }
+    };
+    logs();
+    bool over = chunk == begin;
+    if (!over) {
+      bool some = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])) > R;
+#pragma unroll
+      for (int r = 0; r < QR; ++r) {
+        const float y = top_of(r);
+        some |= y > mine(r) + kSlack || is_far(y);
+      }
+      over = __any(some);
+    }
+    if (over) {
+      if (lane == 0) raised[buf] = chunk + 1;
+    } else {
+      weigh();
     }
     lds_barrier();
-    const bool whole = begin == 0 && end == total;
-    const int64_t place = ((int64_t)part * p.row_tiles + tile) * kRows;
+    if (raised[buf] == chunk + 1) {
+      // new references: the scales' first, then each row's, over all groups of tokens
+      float most = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
+      most = over_groups(most);
+      if (lane == 0) scales[tg] = most;
+      lds_barrier();
+      most = fmaxf(fmaxf(fmaxf(scales[0], scales[1]), fmaxf(scales[2], scales[3])), 0x1p-110f);
+      // the power of two above it
+      most = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, most) & 0x7F800000u) + 0x00800000u);
+      const float now_r = fmaxf(R, most);
+      const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
+      R = now_r;
+      // past kFar s_t / R (below 1) is left out of references: a logit's rounding would move it
+      // by more than they may be off
+      logs();
+      bool far = false;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int in_tile = r * 16 + n, row = row0 + in_tile;
-      if (row >= rows) continue;
-      const float sum = tops[in_tile] + tops[kRows + in_tile] + tops[2 * kRows + in_tile] + tops[3 * kRows + in_tile];
-      const int d0 = wave * CB * 16 + 4 * CB * g;
-      const float unit = R * (1.0f / kLift);
-      const float f = whole ? (sum == 0.0f ? 0.0f : unit / sum) : unit;
-      float y[4 * CB];
+      for (int r = 0; r < QR; ++r) far |= is_far(top_of(r));
+      if (__any(far)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < CB; ++c) y[i * CB + c] = o[r][c][i] * f;
-      if (!whole) {
-        float* into = p.part_o + (place + in_tile) * D + d0;
-#pragma unroll
-        for (int k = 0; k < 4 * CB; k += 4) *reinterpret_cast<v4f*>(into + k) = v4f{y[k], y[k + 1], y[k + 2], y[k + 3]};
-        if (wave == 0 && g == 0) {
-          p.part_ml[2 * (place + in_tile)] = m[r];
-          p.part_ml[2 * (place + in_tile) + 1] = sum;
-        }
-        continue;
+        for (int i = 0; i < 4; ++i) lg[i] = 0.0f;
       }
-      const int token = token_of(p, row);
-      T* into = static_cast<T*>(p.a.out) + (s.first + (int64_t)token) * p.a.ldo + (row - token * heads) * p.a.hdo + d0;
 #pragma unroll
-      for (int k = 0; k < 4 * CB; k += 4) {
-        const float z[4] = {y[k], y[k + 1], y[k + 2], y[k + 3]};
-        if (p.vec) {
-          store_reals<T, 4>(into + k, z);
+      for (int r = 0; r < QR; ++r) {
+        const float y = over_groups(top_of(r));
+        if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = y;
+      }
+      lds_barrier();
+      float down[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int row = r * 16 + n;
+        const float top = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
+        // what came before weighs `ratio` of what it did against the new R
+        const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
+        const float now = top > before + kSlack ? top : before;
+        down[r] = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
+        m[r] = now;
+        const float f = down[r] * ratio;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[r][c] *= f;
+      }
+#pragma unroll
+      for (int r = 0; r < QR; ++r) l[r] *= half ? down[(H - 1) * QR + r] : down[r];
+      weigh();
+      lds_barrier();
+    }
+#pragma unroll
+    for (int r = 0; r < QR; ++r) l[r] += add[r];
+    // all waves have left the chunk before: its slot takes the next but one, or of two
+    // slots the next
+    constexpr int kAhead = L::kSlots - 1;
+    if (chunk + kAhead < end) load(chunk + kAhead, slot == 0 ? kAhead : slot - 1, kAhead == 2 ? page2 : page1);
+    page = page1;
+    page1 = page2;
+    page2 = page_of(chunk + 3);
+    // lane: dimensions CB n + 0 .. CB - 1 of this wave's part, of tokens 32 u + 8 g + 0 .. 7
+    const int8_t* all = lds + slot * L::kSlot;
+    unsigned w[2][8][(CB + 3) / 4];
+    v8h pf[2][QT][RT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        // token 8 (g % 2) + j of group 2 u + g / 2
+        const int byte = wave * CB * 16 + CB * n, piece = (byte >> 4) ^ (2 * (g & 1) + (j >> 2));
+        const int8_t* src = all + (2 * u + (g >> 1)) * L::kGroup + (8 * (g & 1) + j) * L::kRow + piece * 16 + (byte & 15);
+        if constexpr (CB == 8) {
+          const uint2 v = *reinterpret_cast<const uint2*>(src);
+          w[u][j][0] = v.x;
+          w[u][j][1] = v.y;
+        } else if constexpr (CB == 4) {
+          w[u][j][0] = *reinterpret_cast<const unsigned*>(src);
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) into[k + e] = (T)z[e];
+          w[u][j][0] = *reinterpret_cast<const uint16_t*>(src);
         }
       }
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          pf[u][t][r] = *reinterpret_cast<const v8h*>(pb + t * L::kP + (r * 16 + n) * L::kPRow + u * 64 + g * 16);
     }
-  } while ((part += p.groups) < parts);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        v4i f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = pair_of(w[u][2 * j][c / 4], w[u][2 * j + 1][c / 4], c % 4);
+        const v8h v = __builtin_bit_cast(v8h, f);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) o[r][c] = mfma(v, pf[u][t][r], o[r][c]);
+      }
+    slot = slot == L::kSlots - 1 ? 0 : slot + 1;
+  }
+
+  // the rows' sums over lanes and waves
+  lds_barrier();
+#pragma unroll
+  for (int r = 0; r < QR; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = l[r];
+  }
+  lds_barrier();
+  const bool whole = begin == 0 && end == total;
+  const int64_t place = ((int64_t)part * p.row_tiles + tile) * kRows;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int in_tile = r * 16 + n, row = row0 + in_tile;
+    if (row >= rows) continue;
+    const float sum = tops[in_tile] + tops[kRows + in_tile] + tops[2 * kRows + in_tile] + tops[3 * kRows + in_tile];
+    const int d0 = wave * CB * 16 + 4 * CB * g;
+    const float unit = R * (1.0f / kLift);
+    const float f = whole ? (sum == 0.0f ? 0.0f : unit / sum) : unit;
+    float y[4 * CB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < CB; ++c) y[i * CB + c] = o[r][c][i] * f;
+    if (!whole) {
+      float* into = p.part_o + (place + in_tile) * D + d0;
+#pragma unroll
+      for (int k = 0; k < 4 * CB; k += 4) *reinterpret_cast<v4f*>(into + k) = v4f{y[k], y[k + 1], y[k + 2], y[k + 3]};
+      if (wave == 0 && g == 0) {
+        p.part_ml[2 * (place + in_tile)] = m[r];
+        p.part_ml[2 * (place + in_tile) + 1] = sum;
+      }
+      continue;
+    }
+    const int token = token_of(p, row);
+    T* into = static_cast<T*>(p.a.out) + (s.first + (int64_t)token) * p.a.ldo + (row - token * heads) * p.a.hdo + d0;
+#pragma unroll
+    for (int k = 0; k < 4 * CB; k += 4) {
+      const float z[4] = {y[k], y[k + 1], y[k + 2], y[k + 3]};
+      if (p.vec) {
+        store_reals<T, 4>(into + k, z);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) into[k + e] = (T)z[e];
+      }
+    }
+  }
 }
 
 // Joins the parts of a row, 8 of them at a time in flight.  A unit of WAYS * Q threads
@@ -803,28 +815,41 @@ __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile
 
 struct LatentPlan {
   int rt, row_tiles, shared, groups, rounds;
+  int64_t each;  // chunks of a block, by the bounds
   int64_t part, bytes;
 };
 
-LatentPlan plan_latent(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type) {
+LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type, int rt) {
   LatentPlan p{};
-  const int64_t rows = (int64_t)b.max_new * heads;
-  p.rt = rows <= 16 ? 1 : rows <= 32 || type == FXPQ_F32 || k.latent == 512 ? 2 : 4;
-  p.row_tiles = (int)((rows + p.rt * 16 - 1) / (p.rt * 16));
-  const int64_t blocks = (int64_t)p.row_tiles * b.seqs;
-  p.shared = blocks < 4 * (int64_t)c.cus && b.seqs <= kMostSeqs && p.row_tiles <= c.cus / 8;
+  const int64_t rows = (int64_t)b.max_new * heads, chunks = (b.max_len + 63) / 64;
+  p.rt = rt;
+  p.row_tiles = (int)((rows + rt * 16 - 1) / (rt * 16));
   p.rounds = 1;
+  p.shared = (int64_t)p.row_tiles * b.seqs < 4 * (int64_t)c.cus && b.seqs <= kMostSeqs && p.row_tiles <= c.cus / 8;
   if (!p.shared) {
     p.groups = b.seqs;
+    p.each = chunks;
     return p;
   }
-  // blocks that fit the chip at a time
-  const int slots = p.rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
+  // parts whose blocks fit the chip at a time; two for each sequence, so that few long ones
+  // among many can be cut
+  const int slots = rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
   p.groups = slots / 8 / p.row_tiles * 8;
-  p.rounds = (b.seqs + p.groups - 1) / p.groups;
-  p.part = (int64_t)p.groups * p.rounds * p.row_tiles * p.rt * 16;
+  p.rounds = (2 * b.seqs + p.groups - 1) / p.groups;
+  p.each = chunks * b.seqs / p.groups;
+  p.part = (int64_t)p.groups * p.rounds * p.row_tiles * rt * 16;
   p.bytes = p.part * (k.latent + 2) * 4 + (b.seqs + 1) * 4;
   return p;
+}
+
+LatentPlan plan_latent(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type) {
+  const int64_t rows = (int64_t)b.max_new * heads;
+  for (int rt = type == FXPQ_F32 ? k.latent == 512 ? 1 : 2 : k.latent == 512 ? 2 : 4; rt > 1; rt /= 2) {
+    if (rows <= rt * 8) continue;
+    const LatentPlan p = plan_with(c, k, b, heads, type, rt);
+    if (p.each >= (rt == 4 ? 12 : 4)) return p;
+  }
+  return plan_with(c, k, b, heads, type, 1);
 }
 
 template <typename T, int LB, int RT, int W>
@@ -833,7 +858,7 @@ hipError_t run_latent(const Ctx& c, const LatentRun& p) {
   auto* f = k_latent_attention<T, LB, RT, W>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
-  const int64_t blocks = ((int64_t)p.groups + 7) / 8 * 8 * p.row_tiles;
+  const int64_t blocks = ((int64_t)p.groups * p.rounds + 7) / 8 * 8 * p.row_tiles;
   if (blocks > kMaxBlocks) return hipErrorInvalidValue;
   f<<<dim3((unsigned)blocks), dim3(W * 64), bytes, c.stream>>>(p);
   if (p.shared) {
@@ -851,10 +876,14 @@ hipError_t run_latent(const Ctx& c, const LatentRun& p) {
 
 template <typename T, int LB>
 hipError_t run_rows(const Ctx& c, const LatentRun& p, int rt) {
-  if (rt == 1) return run_latent<T, LB, 1, 4>(c, p);
-  if constexpr (sizeof(T) == 2 && LB == 4)
-    if (rt == 4) return run_latent<T, LB, 4, 8>(c, p);
-  return run_latent<T, LB, 2, 8>(c, p);
+  if constexpr (sizeof(T) == 4 && LB == 8) {
+    return run_latent<T, LB, 1, 4>(c, p);
+  } else {
+    if (rt == 1) return run_latent<T, LB, 1, 4>(c, p);
+    if constexpr (sizeof(T) == 2 && LB == 4)
+      if (rt == 4) return run_latent<T, LB, 4, 8>(c, p);
+    return run_latent<T, LB, 2, 8>(c, p);
+  }
 }
 
 }  // namespace
