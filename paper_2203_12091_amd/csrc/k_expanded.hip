@@ -466,8 +466,11 @@ hipError_t run(const Ctx& c, const ExpandedRun& p) {
 
 template <typename T, int D, int VD>
 hipError_t run_rows(const Ctx& c, const ExpandedRun& p) {
-  if constexpr (sizeof(T) == 4) return run<T, D, VD, 1>(c, p);
-  else return p.a.b.max_new <= 64 ? run<T, D, VD, 1>(c, p) : run<T, D, VD, 2>(c, p);
+  if constexpr (sizeof(T) == 2) {
+    const int64_t blocks = ((int64_t)p.a.b.max_new + 127) / 128 * p.a.b.seqs * p.a.kv.heads;
+    if (blocks >= 2 * (int64_t)c.cus) return run<T, D, VD, 2>(c, p);
+  }
+  return run<T, D, VD, 1>(c, p);
 }
 
 template <typename T, int VD>

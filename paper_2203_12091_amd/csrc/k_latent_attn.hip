@@ -30,12 +30,12 @@ typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 // How the work is split.  shared: each sequence's chunks are cut into equal parts of at
-// most `share` chunks, a block for each part and row tile; `groups` parts run at a time
-// and there are blocks for `rounds` times as many.  Parts of a sequence are joined
-// afterwards.  Otherwise a block takes a row tile of a sequence whole.
+// most `share` chunks (`least` or more), a block for each part and row tile; `groups` parts
+// run at a time and there are blocks for `rounds` times as many.  Parts of a sequence are
+// joined afterwards.  Otherwise a block takes a row tile of a sequence whole.
 struct LatentRun {
   LatentArgs a;
-  int row_tiles, shared, groups, rounds, page_log2, vec;
+  int row_tiles, shared, groups, rounds, least, page_log2, vec;
   unsigned heads_mul;  // row / heads = row * heads_mul >> heads_shift, for rows below 2^30
   int heads_shift;
   float* part_o;   // [groups * rounds][row_tiles][rows of a tile][latent]
@@ -63,8 +63,6 @@ constexpr float kSlack = 8.0f;
 // P is written as f16: 2^kLift at the reference, so that weights down to 2^-20 of the
 // largest keep all 11 bits and smaller ones lose at most 2^-31 of it.
 constexpr float kLift = 64.0f;
-constexpr int kLeastShare = 2;  // chunks
-constexpr int kStartCost = 4;   // chunks that take as long as a block's start
 constexpr float kLeastLog = -50.0f;  // of s_t / R, where it only moves the reference
 constexpr float kFar = 0x1p24f;  // logits past this have steps above 1: s_t / R would be rounded
 
@@ -242,22 +240,32 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
           parts += sum;
         }
     };
-    // the share for which the parts, `groups` at a time, take the least time; there is one
-    // whose parts have blocks, at the latest where no sequence has two
     const int most = p.groups * p.rounds;
-    int share = 0, cost = 0x7FFFFFFF;
-    for (int next = max((all + most - 1) / most, kLeastShare);; next += 1 + next / 16) {
-      cut(next);
-      if (parts > most) continue;
-      const int turns = (parts + p.groups - 1) / p.groups, now = turns * (next + kStartCost);
-      if (now < cost) {
-        cost = now;
-        share = next;
+    int share;
+    if (p.rounds == 1) {
+      // the smallest share that leaves no more parts than run at a time (at the latest
+      // where no sequence has two)
+      for (share = max((all + most - 1) / most, p.least);; share += 1 + share / 16) {
+        cut(share);
+        if (parts <= most) break;
       }
-      if (turns <= 1 || next + kStartCost >= cost) {
-        if (share != next) cut(share);
-        break;
+    } else {
+      // sequences no longer than the mean stay whole, or nearly: all / share + active parts
+      // at most, and no share above the longest
+      int active = 0, top = 0;
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e) {
+        active += __popcll(__ballot(count[e] > 0));
+        top = max(top, count[e]);
       }
+      top = max(top, lanes<0xB1>(top));
+      top = max(top, lanes<0x4E>(top));
+      top = max(top, lanes<0x141>(top));
+      top = max(top, lanes<0x140>(top));
+      top = max(max(__builtin_amdgcn_readlane(top, 0), __builtin_amdgcn_readlane(top, 16)),
+                max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)));
+      share = max(min((all + most - active - 1) / (most - active), top), p.least);
+      cut(share);
     }
     if (part >= parts) return;
     // the last sequence whose first part is this or an earlier one (those without parts
@@ -814,7 +822,7 @@ __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile
 }
 
 struct LatentPlan {
-  int rt, row_tiles, shared, groups, rounds;
+  int rt, row_tiles, shared, groups, rounds, least;
   int64_t each;  // chunks of a block, by the bounds
   int64_t part, bytes;
 };
@@ -836,6 +844,7 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
   const int slots = rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
   p.groups = slots / 8 / p.row_tiles * 8;
   p.rounds = (2 * b.seqs + p.groups - 1) / p.groups;
+  p.least = b.seqs * p.row_tiles <= 4 ? 1 : 2;
   p.each = chunks * b.seqs / p.groups;
   p.part = (int64_t)p.groups * p.rounds * p.row_tiles * rt * 16;
   p.bytes = p.part * (k.latent + 2) * 4 + (b.seqs + 1) * 4;
@@ -863,7 +872,7 @@ hipError_t run_latent(const Ctx& c, const LatentRun& p) {
   f<<<dim3((unsigned)blocks), dim3(W * 64), bytes, c.stream>>>(p);
   if (p.shared) {
     const int64_t rows = (int64_t)p.a.b.max_new * p.a.heads;
-    if (rows * p.a.b.seqs >= 1024) {
+    if (rows * p.a.b.seqs >= 256) {
       constexpr int kUnits = 4;  // 64 lanes, 256 dimensions each
       k_latent_join<T, 64, 1><<<dim3((unsigned)((rows * (LB / 4) + kUnits - 1) / kUnits), (unsigned)p.a.b.seqs), dim3(256), 0,
                                 c.stream>>>(p, RT * 16);
@@ -902,6 +911,7 @@ hipError_t launch_latent_attention(const Ctx& c, const LatentArgs& a, int type, 
   p.shared = plan.shared;
   p.groups = plan.groups;
   p.rounds = plan.rounds;
+  p.least = plan.least;
   while ((1 << p.page_log2) < a.c.page) ++p.page_log2;
   int log2 = 0;
   while ((1 << log2) < a.heads) ++log2;

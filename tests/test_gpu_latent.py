@@ -344,6 +344,26 @@ def test_latent_attention_of_short_sequences_under_wide_bounds(fx, h, t, new):
         check_latent(got, cache, lens, new, q, qr, 0.3, 1, t)
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [(256, 100, 128, 90, 3000), (512, 150, 40, 40, 1500), (256, 230, 20, 200, 900), (512, 40, 70, 64, 64)], ids=str)
+def test_latent_attention_of_many_uneven_sequences(fx, h, t, case):
+    """More sequences than run at a time, one of them far longer, some without new tokens."""
+    latent, S, heads, most, longest = case
+    note("latent attention", t, case)
+    rng = np.random.default_rng(S)
+    lens = rng.integers(1, most + 1, S).tolist()
+    lens[S // 3] = longest
+    new = [0 if i % 17 == 3 else 1 for i in range(S)]
+    cache = Cache(fx, lens, latent, 32, 64, seed=S)
+    cache.fill(lens, 21)
+    g = torch.Generator().manual_seed(S)
+    q = torch.randn(sum(new), heads, latent, generator=g).to(TYPES[t])
+    qr = torch.randn(sum(new), heads, 32, generator=g).to(TYPES[t])
+    got = run_latent(fx, h, cache, new, lens, q, qr, 0.05, 1, t)
+    assert fx.sync_status(h) == 0
+    check_latent(got, cache, lens, new, q, qr, 0.05, 1, t)
+
+
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("heads", [4, 33])
 def test_latent_attention_extremes(fx, h, t, heads):
