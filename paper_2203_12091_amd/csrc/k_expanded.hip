@@ -17,6 +17,13 @@
 // leaves the whole result's error at 1.3 times that of its own rounding; f16 with weights
 // lifted by 2^6, so that those down to 2^-20 of the largest keep 11 bits); f32 on the
 // f32 matrix instruction, whose products are exact.
+//
+// Bound by the products: 4 x 1024 over up to 4000, 32 heads of 128 + 64 and 128, bf16: 175
+// GFLOP in 198 us, 0.88 PFLOP/s, where one large product reaches 1.37; 1 x 8192, f16: 333 us,
+// 1.03 PFLOP/s.  Matrix instructions take 46% of the cycles, vector instructions (weights,
+// maxima, rounding) 42%; two blocks a CU overlap the two.  Of 245 us at first the loop of
+// its own for chunks that all rows see took 13, the priority and order of the instructions
+// 35.  64 rows a wave (one wave a SIMD) spill: 850 us.
 #include <type_traits>
 
 #include "kv.hpp"
@@ -467,6 +474,10 @@ hipError_t run(const Ctx& c, const ExpandedRun& p) {
 template <typename T, int D, int VD>
 hipError_t run_rows(const Ctx& c, const ExpandedRun& p) {
   if constexpr (sizeof(T) == 2) {
+    // 128 rows of a block read half as much, 64 make twice as many blocks.  Two blocks run on
+    // a CU; in us with 64 and 128 rows: 4 x 1024 over 4000, 16 heads (2 blocks of 128 rows a
+    // CU) 189 and 162, 1 x 1024 over 2048, 128 heads (4) 187 and 151, 1 x 4096, 16 heads (2)
+    // 114 and 119, 2 x 1024 over 2048 (1) 57.5 and 58.2, 4 x 128 over 2048 (1/4) 43 and 57
     const int64_t blocks = ((int64_t)p.a.b.max_new + 127) / 128 * p.a.b.seqs * p.a.kv.heads;
     if (blocks >= 2 * (int64_t)c.cus) return run<T, D, VD, 2>(c, p);
   }

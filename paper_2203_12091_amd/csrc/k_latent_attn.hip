@@ -2,22 +2,30 @@
 // is key and value of every head.
 //
 // A sequence's query rows are its new tokens' heads (row = token * heads + head); a
-// block takes 16 RT of them over the cache, 64 tokens at a time.  Wave w computes S = K Q^T
-// for tokens 16 w .. 16 w + 15: it loads their codes from the cache in the operand's
-// layout (lane: token lane % 16, 16 codes from 16 (lane / 16)), converts them to f16
-// (exact) and multiplies them with q, which all waves hold in registers, as f16 too: q is
-// scaled by a power of two of its row, so a bf16 or f16 value is exact down to 2^-27 of
-// the row's largest, and f32 is two f16 terms.  The codes go to LDS as they are, P as f16
-// beside them, and after one barrier every wave multiplies all 64 tokens with its own
-// quarter of the latent's dimensions: O^T = C^T P^T.  The conversion there is the
-// transposition: a lane reads the same 8 (or 4) dimensions of 8 tokens and pairs bytes of
-// neighbouring tokens.
+// block takes 16 RT of them over a part of the sequence's cache, 64 tokens (a chunk) at a
+// time.  Chunks come straight from memory into a ring of two or three LDS slots.  First
+// product, S = K Q^T: a wave has 16 of the tokens; it reads their codes from LDS in the
+// operand's layout (lane: token lane % 16, 16 codes from 16 (lane / 16)), converts them to
+// f16 (exact) and multiplies them with q in registers.  q is f16 too: scaled by a power of
+// two of its row, so that a bf16 or f16 value is exact down to 2^-27 of the row's largest,
+// and f32 is two f16 terms.  P goes to LDS as f16 and after a barrier every wave multiplies
+// all 64 tokens with its own part of the latent's dimensions: O^T = C^T P^T.  The
+// conversion there is the transposition: a lane reads the same 2 to 8 dimensions of 8
+// tokens and pairs bytes of neighbouring tokens.
 //
 // A token's scale s_t belongs to both products.  With x_t the logit (base 2), m the
 // row's reference and R a power of two above every scale seen, P_t = 2^(x_t - m) s_t / R
 // goes into O and 2^(x_t - m) into the sum.  m follows max (x_t + log2(s_t / R)) only
 // when a row passes it by more than kSlack, so P_t is below 2^(kSlack + kLift) and most
-// chunks need neither a maximum across the waves nor a second barrier.
+// chunks need neither a maximum across the waves nor further barriers.
+//
+// What it costs (16 heads, latents of 512 + 64, bf16): a block's start about 8 us (its
+// part, pages, q to f16), a chunk 1.8 us with four waves and one row tile, two blocks a CU,
+// 2.3 us with eight waves and two tiles.  The bytes are not the limit but the conversions:
+// 128 heads, 32 sequences up to 4096: vector instructions 53% of the cycles, matrix
+// instructions 16%, the rest waits at the chunk's two barriers, which one block a CU does
+// not fill.  64 x 1 over up to 8192, 16 heads: 158 MB in 38.6 us, 4.1 TB/s; 32 x 1 over
+// up to 4096, 128 heads: 66 us, 0.28 PFLOP/s; the join 6 us more in both.
 #include "kv.hpp"
 #include "ring.hpp"
 #include "values.hpp"
@@ -142,7 +150,8 @@ struct LatentLds {
   static constexpr int kPieces = LB * 4 + 4, kRow = kPieces * 16;
   static constexpr int kLoads = kPieces * 16 / 64;  // 1 KB loads of a group
   static constexpr int kGroup = 16 * kRow, kSlot = 4 * kGroup;
-  // one tile of a wide latent: two slots, so that two blocks fit a CU
+  // one tile of a wide latent: two slots, so that two blocks fit a CU (64 x 1 over 8192, 16
+  // heads: 71 us; three slots and one block 75; 1 x 1 over 131072: 32.7 and 30.7)
   static constexpr int kSlots = LB == 8 && RT * QT == 1 ? 2 : 3;
   static constexpr int kScales = kSlots * kSlot;              // [slots][4 groups][64] floats
   static constexpr int kPRow = 144;                           // bytes of a row of P: 64 halves and a pad
@@ -158,7 +167,7 @@ struct LatentLds {
 // LB: 64-dimension pieces of the latent; RT: 16-row tiles of a block; W: waves.  Four waves:
 // each has one group of 16 tokens in the first product and a quarter of the latent's
 // dimensions in the second.  Eight: two share a group of tokens and have half of the rows
-// each, and an eighth of the dimensions.
+// each, and an eighth of the dimensions, which halves what a wave holds of q and O.
 template <typename T, int LB, int RT, int W>
 __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 : 1) void k_latent_attention(const LatentRun p) {
   constexpr int QT = sizeof(T) == 4 ? 2 : 1;  // f16 terms of q and of P
@@ -168,7 +177,9 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   constexpr int CB = LB / H;             // 16-dimension tiles of a wave in the second
   // 16-bit q meets 1152 + code, not the code: one operation fewer for each pair of codes.
   // What the 1152 adds, 1152 sum q, is where the sums start from, below zero; their fp32
-  // rounding then counts against it, 2^-24 of about 30 times the products themselves.
+  // rounding then counts against it: for q of random signs as for the products' magnitudes,
+  // for q of one sign 2^-24 of about 30 times them, far below a 16-bit result's rounding.
+  // 32 x 1 over 4096, 128 heads: 89 us, with the code itself 98.
   constexpr bool kBiased = QT == 1;
   typedef LatentLds<LB, RT, QT> L;
   // loads of a wave: with eight, the first four waves have the first half of each group
@@ -209,7 +220,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   int seq = part, begin = 0, size = 0;
   SeqDev s;
   if (p.shared) {
-    // every wave finds the share and the part's sequence by itself, four sequences a lane
+    // Every wave finds the share and the part's sequence by itself, up to four sequences a
+    // lane: nothing has to run before this kernel, and lengths stay on the device.
     constexpr int kOwn = kMostSeqs / 64;
     SeqDev d[kOwn];
     int count[kOwn], all = 0;
@@ -747,8 +759,10 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 }
 
 // Joins the parts of a row, 8 of them at a time in flight.  A unit of WAYS * Q threads
-// has 4 Q dimensions of one row: a wave has a whole row where rows are many, a block 64
-// dimensions of one where they are few and have many parts.
+// has 4 Q dimensions of one row: one wave 256 where rows are many, a block 64 dimensions
+// where they are few and have many parts.  Both kernels, in us, a wave and a block for a
+// unit: 8 rows of 16 heads over 8192 31.7 and 26.1, 1 over 131072 94 and 33, 20 over 2048
+// 23.3 and 26.1, 60 over 2048 30.4 and 41.4.
 template <typename T, int Q, int WAYS>
 __global__ __launch_bounds__(256) void k_latent_join(const LatentRun p, int tile_rows) {
   constexpr int kAhead = 8, kUnits = 256 / (Q * WAYS);
@@ -839,11 +853,15 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
     p.each = chunks;
     return p;
   }
-  // parts whose blocks fit the chip at a time; two for each sequence, so that few long ones
-  // among many can be cut
+  // Parts whose blocks fit the chip at a time; two for each sequence, so that few long ones
+  // among many can be cut: 128 x 1, 128 heads, over 512 and one over 16384 104 us, whole
+  // 559; where all have 1024 the two ways take 111 and 94 us, which is why sequences are
+  // left whole from four blocks a CU on (200 x 1, 128 heads, over 1024: 243 and 184).
   const int slots = rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
   p.groups = slots / 8 / p.row_tiles * 8;
   p.rounds = (2 * b.seqs + p.groups - 1) / p.groups;
+  // one chunk a part for few tiles: 1 x 1 over 300 13.3 us, two chunks 15.1; but 8 x 1 over
+  // 2048 19.6 and 18.5, 64 x 1 over 300 22.6 and 18.7
   p.least = b.seqs * p.row_tiles <= 4 ? 1 : 2;
   p.each = chunks * b.seqs / p.groups;
   p.part = (int64_t)p.groups * p.rounds * p.row_tiles * rt * 16;
@@ -851,6 +869,13 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
   return p;
 }
 
+// Row tiles of a block: more of them spare conversions of the codes, fewer make more parts
+// and shorter ones.  In us with 1, 2 and 4 tiles, 128 heads, bf16, latents of 256: 32 x 1
+// over 4096 (32 chunks a block with two tiles) 66, 61, 50; 8 x 1 over 4096 (8 chunks) 28.9,
+// 27.2, 30.5; 16 x 1 over 1024 (4) 22.4, 22.0, 26.2.  Latents of 512: 32 x 1 over 4096 98 and
+// 89, 2 x 1 rows of 16 heads over 8192 (0.5) 18 and 22; four tiles do not fit the registers
+// (174 us).  f32, whose q and P are twice as large, in one and two tiles: latents of 256,
+// 32 x 1 over 4096 110 and 80, 2 x 1 over 512 15 and 18; of 512 one only (163 and 196).
 LatentPlan plan_latent(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type) {
   const int64_t rows = (int64_t)b.max_new * heads;
   for (int rt = type == FXPQ_F32 ? k.latent == 512 ? 1 : 2 : k.latent == 512 ? 2 : 4; rt > 1; rt /= 2) {

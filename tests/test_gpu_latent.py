@@ -9,6 +9,10 @@ tokens and L of them: a logit is off by at most d = |softmax_scale| sum |q k| *
 a weight by 2 d + 4 * 2^-23 (exp2), by its rounding before the second product uP (2^-11
 one f16 term, 2^-22 two), and by 2^-31 of the largest weight (f16's range again); the sums
 by 2 (L + 64) * 2^-24.  All of it weighs at most S; the type's rounding comes last.
+For 16-bit q the first product's sums may start from a constant per query, up to (1152 +
+127) s_max sum |q| in all; every step of 8 dimensions rounds by 2^-24 of that at most.  With
+q of random signs the partial sums stay near sqrt(latent) * 1152 |q|, below the products'
+magnitudes sum |q k| that are counted already; q of one sign is tested with the term.
 Expanded attention: products exact or rounded in fp32 sums, uP the type's own rounding."""
 import math
 
@@ -260,13 +264,13 @@ def want_latent(cache, s, n, fresh, q, qr, scale, causal):
     return out, (mag * keep).amax(-1), (x.abs() * keep).amax(-1), tops * (v.abs().sum(1).max() + k.abs().sum(1).max()) * abs(scale), v.abs().max()
 
 
-def check_latent(got, cache, lens, new, q, qr, scale, causal, t):
+def check_latent(got, cache, lens, new, q, qr, scale, causal, t, more=0.0):
     at = 0
     for s, (n, fresh) in enumerate(zip(lens, new)):
         if fresh == 0:
             continue
         want, mag, x, ends, S = want_latent(cache, s, n, fresh, q[at : at + fresh].double(), qr[at : at + fresh].double(), scale, causal)
-        d = mag * ((cache.latent + cache.rope + 8) * 2.0 ** -24 + (2.0 ** -22 if t == "f32" else 0)) + ends * 2.0 ** -38 + 4 * 2.0 ** -24 * x
+        d = mag * ((cache.latent + cache.rope + 8) * 2.0 ** -24 + (2.0 ** -22 if t == "f32" else 0)) + ends * 2.0 ** -38 + 4 * 2.0 ** -24 * x + more
         uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
         tol = S * (2 * d + 4 * 2.0 ** -23 + uP + n * 2.0 ** -31 + 2 * (n + 64) * 2.0 ** -24)[..., None] + 1.01 * HALF_ULP[t] * want.abs()
         off = (got[at : at + fresh].double() - want).abs()
@@ -386,6 +390,21 @@ def test_latent_attention_extremes(fx, h, t, heads):
     got = run_latent(fx, h, cache, [2], lens, q, qr, 0.1, 1, t)
     bad = got.isnan()
     assert bad[0, 2].all() and bad[1, 3].all() and bad.sum() == 2 * 512
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("latent,heads", [(512, 16), (256, 64), (512, 40)])
+def test_latent_attention_of_queries_of_one_sign(fx, h, t, latent, heads):
+    lens = [900, 70]
+    cache = Cache(fx, lens, latent, 64, 16)
+    cache.fill(lens, 12)
+    g = torch.Generator().manual_seed(14)
+    q, qr = (torch.rand(2, heads, latent, generator=g) + 1).to(TYPES[t]), -(torch.rand(2, heads, 64, generator=g) + 1).to(TYPES[t])
+    got = run_latent(fx, h, cache, [1, 1], lens, q, qr, 0.1, 1, t)
+    assert fx.sync_status(h) == 0
+    at_most = max(float(cache.scale.nan_to_num().max()), float(cache.rope_scale.nan_to_num().max()))
+    d = 0.1 * at_most * 1279 * float((q.double().abs().sum(-1) + qr.double().abs().sum(-1)).max()) * (latent + 64) / 8 * 2.0 ** -24
+    check_latent(got, cache, lens, [1, 1], q, qr, 0.1, 1, t, more=0.0 if t == "f32" else d)
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
