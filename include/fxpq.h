@@ -799,8 +799,8 @@ fxpq_status fxpq_latent_read(fxpq_handle h, const fxpq_latent_cache* cache,
  * over all tokens of the sequence, or with causal != 0 over those up to the
  * query's own.  q: `latent` reals of each token and head at token * ldq + head *
  * hdq, q_rope: `rope` reals at token * ldqr + head * hdqr, out: `latent` reals at
- * token * ldo + head * hdo (strides in any order; out's rows must not overlap).
- * A query that sees no token gets 0, one that holds a NaN or an infinity NaN.
+ * token * ldo + head * hdo (strides in any order; out's rows overlap neither each
+ * other nor an input).  A query that sees no token gets 0, one that holds a NaN or an infinity NaN.
  * workspace as for fxpq_token_gemm.
  */
 fxpq_status fxpq_latent_attention_workspace(fxpq_handle h, const fxpq_latent_cache* cache,
@@ -834,8 +834,8 @@ typedef struct {
  *     o_h = sum_j softmax_j(softmax_scale * (q_h[: nope] . k_jh + q_h[nope :] . key_j)) v_jh
  * over all rows of the sequence, or with causal != 0 over those up to the query's
  * own (the new tokens are the sequence's last rows).  q: rows of heads * (nope +
- * rope) reals, row stride ldq; out: rows of heads * vdim reals, row stride ldo.  A
- * query that sees no token gets 0; keys and values that a query does not see have no
+ * rope) reals, row stride ldq; out: rows of heads * vdim reals, row stride ldo, apart
+ * from all inputs.  A query that sees no token gets 0; keys and values that a query does not see have no
  * part in its result, whatever they hold.  Of the batch start, length, seqs, tokens,
  * max_new and max_len are used (table is not, and may be NULL).  A sequence whose
  * numbers contradict the bounds or kv->start is skipped and raises FXPQ_FLAG_RANGE.

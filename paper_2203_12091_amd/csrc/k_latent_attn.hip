@@ -64,7 +64,9 @@ __device__ inline int part_chunks(int chunks, int share) {
   const int parts = (chunks + share - 1) / share;
   return parts == 0 ? 1 : (chunks + parts - 1) / parts;
 }
-constexpr int kMostSeqs = 256;  // of a call that is shared
+// Sequences of a call that is shared, four a lane.  (With 512 every call's start takes 0.3 us
+// more; 400 x 1, 16 heads, over 1 to 4096 143 us in place of 173, 32 heads over 1024 149 of 94.)
+constexpr int kMostSeqs = 256;
 
 constexpr float kNoMax = -3.40282347e38f;  // reference before any token
 constexpr float kSlack = 8.0f;
