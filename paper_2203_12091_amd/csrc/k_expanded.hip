@@ -18,6 +18,8 @@
 // lifted by 2^6, so that those down to 2^-20 of the largest keep 11 bits); f32 on the
 // f32 matrix instruction, whose products are exact.
 //
+// Where there are few rows the four waves take the same 16 and share the tokens of a chunk.
+//
 // Bound by the products: 4 x 1024 over up to 4000, 32 heads of 128 + 64 and 128, bf16: 175
 // GFLOP in 198 us, 0.88 PFLOP/s, where one large product reaches 1.37; 1 x 8192, f16: 333 us,
 // 1.03 PFLOP/s.  Matrix instructions take 46% of the cycles, vector instructions (weights,
@@ -36,7 +38,7 @@ namespace {
 template <typename T>
 struct Operand {
   typedef T v8 __attribute__((ext_vector_type(8)));
-  static constexpr int kTok = sizeof(T) == 4 ? 32 : 64;  // tokens of a chunk
+  static constexpr int kTok = sizeof(T) == 4 ? 32 : 64;  // tokens of a wave's chunk
 };
 __device__ inline v4f mfma8(Operand<_Float16>::v8 a, Operand<_Float16>::v8 b, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -68,17 +70,18 @@ __device__ inline float scaled(float x, float f) {
 #pragma clang fp contract(off)
   return x * f;
 }
+__device__ inline bool is_far(float m) { return fabsf(m) > kFar && m != kNoMax; }
 __device__ inline float over_groups(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
 // Panels of 128 bytes of a token's row, and a piece's place in its row.
-template <typename T>
+template <typename T, int TOK>
 struct Panels {
   static constexpr int kDims = 128 / (int)sizeof(T);
   static constexpr int of(int dims) { return (dims + kDims - 1) / kDims; }
-  static constexpr int kBytes = Operand<T>::kTok * 128;
+  static constexpr int kBytes = TOK * 128;  // of a panel of TOK tokens
 };
 __device__ inline int key_swap(int tok) { return (tok >> 1) & 7; }
 template <typename T>
@@ -87,7 +90,7 @@ __device__ inline int value_swap(int tok) {
 }
 
 // A thread's piece of each panel, real by real.
-template <typename T>
+template <typename T, int TOK>
 __device__ inline void copy_pieces(const int8_t* from, int panels, int8_t* to) {
   constexpr int kPiece = 16 / (int)sizeof(T);
 #pragma unroll 1
@@ -96,7 +99,7 @@ __device__ inline void copy_pieces(const int8_t* from, int panels, int8_t* to) {
     Reals<T, kPiece> x;
 #pragma unroll
     for (int k = 0; k < kPiece; ++k) x.v[k] = src[k];
-    *reinterpret_cast<Reals<T, kPiece>*>(to + q * Panels<T>::kBytes) = x;
+    *reinterpret_cast<Reals<T, kPiece>*>(to + q * Panels<T, TOK>::kBytes) = x;
   }
 }
 
@@ -116,13 +119,13 @@ __device__ inline int value_at(int j, int g, int n) {
 }
 // Eight tokens of one dimension: tokens 4 g + 0..3 of the 16-token tiles 2 u and 2 u + 1,
 // dimension 16 j + n, from `at` = value_at of j.
-template <typename T>
+template <typename T, int TOK>
 __device__ inline typename Operand<T>::v8 value_operand(LdsAt at, int u, int j) {
   typename Operand<T>::v8 v;
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      v[k] = lds_read<float>(at + (j >> 1) * Panels<T>::kBytes + (32 * u + 16 * (k >> 2) + (k & 3)) * 128);
+      v[k] = lds_read<float>(at + (j >> 1) * Panels<T, TOK>::kBytes + (32 * u + 16 * (k >> 2) + (k & 3)) * 128);
   } else {
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef short v8s __attribute__((ext_vector_type(8)));
@@ -130,21 +133,25 @@ __device__ inline typename Operand<T>::v8 value_operand(LdsAt at, int u, int j) 
     v4s part[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-      part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Quad)(at + (j >> 2) * Panels<T>::kBytes + (32 * u + 16 * k) * 128));
+      part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Quad)(at + (j >> 2) * Panels<T, TOK>::kBytes + (32 * u + 16 * k) * 128));
     v = __builtin_bit_cast(typename Operand<T>::v8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
   return v;
 }
 
-// D: dimensions of a query and key (nope + rope: up to 128 64 + 32 or 64, else 128 + 32 or 64); VD: of a value; NC: 16-row tiles of a wave.
-template <typename T, int D, int VD, int NC>
+// D: dimensions of a query and key (nope + rope: up to 128 64 + 32 or 64, else 128 + 32 or
+// 64); VD: of a value; NC: 16-row tiles of a wave.  SPLIT: the four waves have the same 16
+// rows and a quarter of each chunk's 128 tokens; what they found is joined at the end.
+template <typename T, int D, int VD, int NC, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun p) {
   typedef typename Operand<T>::v8 v8;
-  constexpr int kTok = Operand<T>::kTok, TT = kTok / 16, S = sizeof(T);
+  static_assert(!SPLIT || (NC == 1 && sizeof(T) == 2), "a wave's 32 tokens are one operand");
+  constexpr int kTok = SPLIT ? 128 : Operand<T>::kTok, kOwn = SPLIT ? 32 : kTok;  // of a chunk and of a wave in it
+  constexpr int TT = kOwn / 16, S = sizeof(T);
   constexpr int kSteps = D / 32, DT = VD / 16;
-  constexpr int kRows = NC * 64;
+  constexpr int kRows = SPLIT ? 16 : NC * 64;
   constexpr int kPiece = 16 / S;  // reals of a 16-byte piece
-  typedef Panels<T> Pan;
+  typedef Panels<T, kTok> Pan;
   constexpr int KP = Pan::of(D), VP = Pan::of(VD), kStage = (KP + VP) * Pan::kBytes;
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
   const int pos0 = s.len - s.fresh;
   const int last = min(row0 + kRows, s.fresh) - 1;
   const int end = ((causal ? pos0 + last : s.len - 1) + kTok) / kTok;
-  const int wrow = row0 + wave * NC * 16;
+  const int wrow = SPLIT ? row0 : row0 + wave * NC * 16, wtok = SPLIT ? wave * kOwn : 0;
   const int wlast = min(wrow + NC * 16, s.fresh) - 1;
   const int wave_end = wlast < wrow ? 0 : ((causal ? pos0 + wlast : s.len - 1) + kTok) / kTok;
 
@@ -204,10 +211,10 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
           dma16(values + row_at * ldv * S + q * 128, vo, to_lds + (KP + q) * Pan::kBytes + half * 4096);
       } else {
         const int64_t row = row_at + r;
-        copy_pieces<T>(keys + (row * ldk * S + kpiece * 16), nope_panels, to_lds + half * 4096 + lane * 16);
-        copy_pieces<T>(shared + (row * ldr * S + rpiece * 16), KP - nope_panels,
+        copy_pieces<T, kTok>(keys + (row * ldk * S + kpiece * 16), nope_panels, to_lds + half * 4096 + lane * 16);
+        copy_pieces<T, kTok>(shared + (row * ldr * S + rpiece * 16), KP - nope_panels,
                        to_lds + nope_panels * Pan::kBytes + half * 4096 + lane * 16);
-        copy_pieces<T>(values + (row * ldv * S + vpiece * 16), VP, to_lds + KP * Pan::kBytes + half * 4096 + lane * 16);
+        copy_pieces<T, kTok>(values + (row * ldv * S + vpiece * 16), VP, to_lds + KP * Pan::kBytes + half * 4096 + lane * 16);
       }
     }
   };
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
   const int first_limit = causal ? pos0 + wrow : s.len - 1;
   constexpr float kLift = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
 
-  const LdsAt first = lds_at(lds);
+  const LdsAt first = lds_at(lds) + wtok * 128;
   constexpr int kValueBases = S == 4 ? 2 : 4;
   int kat[2], vat[kValueBases];
 #pragma unroll
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
     }
     __builtin_amdgcn_s_setprio(0);
     constexpr int N = 4 * TT;  // this lane's tokens: 16 (i / 4) + 4 g + i % 4 of the chunk
-    const int t0 = chunk * kTok + 4 * g;
+    const int t0 = chunk * kTok + wtok + 4 * g;
     float x[NC][N], f = f_log2;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
         l[c] *= down;
 #pragma unroll
         for (int j = 0; j < DT; ++j) o[c][j] *= down;
-        far |= now > kFar || (now < -kFar && now != kNoMax);
+        far |= is_far(now);
       }
       far = __any(far);
     }
@@ -347,11 +354,13 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
 #pragma unroll
     for (int c = 0; c < NC; ++c) ref[c] = kLift - m[c];
     if (far) {
+      // (row by row again)
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
+        const bool mine = is_far(m[c]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[c][i] = scaled(x[c][i], f) - m[c];
-        ref[c] = kLift;
+        for (int i = 0; i < N; ++i) x[c][i] = mine ? scaled(x[c][i], f) - m[c] + kLift : fmaf(x[c][i], f, ref[c]);
+        ref[c] = 0.0f;
       }
       f = 1.0f;
     }
@@ -368,7 +377,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
     constexpr int kAhead = 4;  // operands read ahead
     v8 v[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) v[j] = value_operand<T>(vb + vat[j % kValueBases], j / DT, j % DT);
+    for (int j = 0; j < kAhead; ++j) v[j] = value_operand<T, kTok>(vb + vat[j % kValueBases], j / DT, j % DT);
 #pragma unroll
     for (int i = 0; i < 8; ++i) weigh(0, i);
     // Where some rows do not see some tokens, a value that is not finite must not meet
@@ -392,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][k % DT] = mfma8(v[k % kAhead], w[c][k / DT], o[c][k % DT]);
         const int ahead = k + kAhead;
-        if (ahead < N / 8 * DT) v[k % kAhead] = value_operand<T>(vb + vat[ahead % kValueBases], ahead / DT, ahead % DT);
+        if (ahead < N / 8 * DT) v[k % kAhead] = value_operand<T, kTok>(vb + vat[ahead % kValueBases], ahead / DT, ahead % DT);
         if (N > 8 && k < DT)
 #pragma unroll
           for (int i = 0; i < 8 / DT; ++i) weigh(1, k * (8 / DT) + i);
@@ -405,14 +414,14 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       for (int u = 0; u < N / 8; ++u)
 #pragma unroll
         for (int j = 0; j < DT; ++j) {
-          v8 y = value_operand<T>(vb + vat[j % kValueBases], u, j);
+          v8 y = value_operand<T, kTok>(vb + vat[j % kValueBases], u, j);
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[k] = finite((float)y[k]) ? y[k] : (T)0.0f;
 #pragma unroll
           for (int c = 0; c < NC; ++c) o[c][j] = mfma8(y, u ? w[c][N / 8 - 1] : w[c][0], o[c][j]);
         }
 #pragma unroll 1
-      for (int t = 0; t < kTok; ++t) {
+      for (int t = wtok; t < wtok + kOwn; ++t) {
         const int at = chunk * kTok + t;
         if (at >= s.len) break;
 #pragma unroll
@@ -440,12 +449,45 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
   for (int c = 0; c < NC; ++c) {
     l[c] += __shfl_xor(l[c], 16);
     l[c] += __shfl_xor(l[c], 32);
+  }
+  constexpr int kTiles = SPLIT ? DT / 4 : DT;  // 16-dimension tiles that a wave writes
+  const int j0 = SPLIT ? wave * kTiles : 0;
+  if constexpr (SPLIT) {
+    v4f* parts = reinterpret_cast<v4f*>(lds);                         // [wave][tile][lane]
+    float* stats = reinterpret_cast<float*>(lds + 4 * DT * 64 * 16);  // [wave][row]: reference, sum
+    __syncthreads();  // the chunks have been read
+#pragma unroll
+    for (int j = 0; j < DT; ++j) parts[(wave * DT + j) * 64 + lane] = o[0][j];
+    if (g == 0) {
+      stats[(wave * 16 + n) * 2] = m[0];
+      stats[(wave * 16 + n) * 2 + 1] = l[0];
+    }
+    __syncthreads();
+    float ms[4], top = kNoMax;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      ms[w] = stats[(w * 16 + n) * 2];
+      top = fmaxf(top, ms[w]);
+    }
+    l[0] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) o[0][j] = v4f{0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ms[w] - top);
+      l[0] += f * stats[(w * 16 + n) * 2 + 1];
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) o[0][j] += f * parts[(w * DT + j0 + j) * 64 + lane];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
     const int row = wrow + c * 16 + n;
     if (row >= s.fresh) continue;
     const float f = l[c] == 0.0f ? 0.0f : 1.0f / l[c];
-    T* at = static_cast<T*>(p.a.out) + (s.first + (int64_t)row) * p.a.ldo + (int64_t)head * VD + 4 * g;
+    T* at = static_cast<T*>(p.a.out) + (s.first + (int64_t)row) * p.a.ldo + (int64_t)head * VD + 16 * j0 + 4 * g;
 #pragma unroll
-    for (int j = 0; j < DT; ++j) {
+    for (int j = 0; j < kTiles; ++j) {
       const float y[4] = {o[c][j][0] * f, o[c][j][1] * f, o[c][j][2] * f, o[c][j][3] * f};
       if (p.vec_out) {
         store_reals<T, 4>(at + 16 * j, y);
@@ -457,14 +499,15 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
   }
 }
 
-template <typename T, int D, int VD, int NC>
+template <typename T, int D, int VD, int NC, bool SPLIT = false>
 hipError_t run(const Ctx& c, const ExpandedRun& p) {
-  constexpr int bytes = 2 * (Panels<T>::of(D) + Panels<T>::of(VD)) * Panels<T>::kBytes;
-  auto* f = k_expanded_attention<T, D, VD, NC>;
+  typedef Panels<T, SPLIT ? 128 : Operand<T>::kTok> Pan;
+  constexpr int bytes = 2 * (Pan::of(D) + Pan::of(VD)) * Pan::kBytes, rows = SPLIT ? 16 : NC * 64;
+  auto* f = k_expanded_attention<T, D, VD, NC, SPLIT>;
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(f), bytes);
   if (e != hipSuccess) return e;
   ExpandedRun r = p;
-  r.row_tiles = (p.a.b.max_new + NC * 64 - 1) / (NC * 64);
+  r.row_tiles = (p.a.b.max_new + rows - 1) / rows;
   const int64_t blocks = (int64_t)r.row_tiles * p.a.b.seqs * p.a.kv.heads;
   if (blocks > kMaxBlocks) return hipErrorInvalidValue;
   f<<<dim3((unsigned)blocks), dim3(256), bytes, c.stream>>>(r);
@@ -480,6 +523,11 @@ hipError_t run_rows(const Ctx& c, const ExpandedRun& p) {
     // 114 and 119, 2 x 1024 over 2048 (1) 57.5 and 58.2, 4 x 128 over 2048 (1/4) 43 and 57
     const int64_t blocks = ((int64_t)p.a.b.max_new + 127) / 128 * p.a.b.seqs * p.a.kv.heads;
     if (blocks >= 2 * (int64_t)c.cus) return run<T, D, VD, 2>(c, p);
+    // where tiles of 16 rows do not fill the chip, the waves share the tokens: 1 x 64 over 8192,
+    // 16 heads, 75 us, 64 rows a block 141; 4 x 64 over 2048 29 and 43, 2 x 77 over 127 11.0 and
+    // 13.6, but 16 x 16 over 300 17.6 and 15.1.  (A token of f32 takes twice the LDS.)
+    const int64_t tiles = ((int64_t)p.a.b.max_new + 15) / 16 * p.a.b.seqs * p.a.kv.heads;
+    if (tiles <= c.cus) return run<T, D, VD, 1, true>(c, p);
   }
   return run<T, D, VD, 1>(c, p);
 }
@@ -505,7 +553,7 @@ hipError_t launch_expanded_attention(const Ctx& c, const ExpandedArgs& a, int ty
   };
   p.vec = fits(a.kv.k, a.kv.ldk, a.kv.hdk) && fits(a.kv.v, a.kv.ldv, a.kv.hdv) && fits(a.kv.key, a.kv.ld_key, 0) &&
           fits(a.q, a.ldq, 0);
-  // 64 rows have to lie within 32-bit offsets of each other
+  // a chunk's rows (32 of f32, 128 of other types at most) have to lie within 32-bit offsets of each other
   constexpr int64_t kNear = int64_t(1) << 24;
   p.vec = p.vec && a.kv.ldk < kNear && a.kv.ldv < kNear && a.kv.ld_key < kNear;
   p.vec_out = fits(a.out, a.ldo, 0);

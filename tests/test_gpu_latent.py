@@ -548,6 +548,12 @@ EXPANDED = [  # (nope, rope, vdim, heads, new, lengths, causal)
     (64, 32, 128, 8, [300], [333], 1),
     (128, 32, 128, 1, [129, 33], [129, 1025], 1),
     (128, 64, 64, 4, [31, 32, 33], [31, 95, 97], 1),
+    (64, 64, 64, 3, [16, 2], [4000, 129], 1),
+    # many rows: 64 and 128 of them a block
+    (128, 64, 128, 40, [90, 3], [200, 77], 1),
+    (128, 64, 128, 64, [150, 129, 140, 1], [400, 129, 150, 300], 1),
+    (64, 32, 64, 64, [140, 150, 1, 0], [150, 170, 40, 9], 0),
+    (64, 32, 128, 70, [65, 129, 128, 64], [65, 130, 300, 64], 1),
 ]
 
 
@@ -617,12 +623,13 @@ def test_expanded_attention(fx, h, t, case):
 
 
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("fresh,before,q0", [(90, 110, 50), (128, 0, 5), (200, 7, 130)])
-def test_expanded_attention_sees_nothing_of_masked_places(fx, h, t, fresh, before, q0):
+@pytest.mark.parametrize("fresh,before,q0,heads", [(90, 110, 50, 2), (128, 0, 5, 2), (200, 7, 130, 2), (3, 300, 1, 2), (90, 110, 50, 40),
+                                                   (150, 60, 20, 40), (200, 7, 130, 256), (150, 30, 20, 256)])
+def test_expanded_attention_sees_nothing_of_masked_places(fx, h, t, fresh, before, q0, heads):
     """NaN and infinities in keys, shared keys and values that a query does not see leave
     its result alone, bit for bit; a query that sees one in a value has it in that dimension
     only, one that sees one in a key is NaN."""
-    c, new, lens = (128, 64, 128, 2, 1), [fresh, 40], [before + fresh, 40]
+    c, new, lens = (128, 64, 128, heads, 1), [fresh, 40], [before + fresh, 40]
     q, k, key, v = heads_of(c, new, lens, t, 6)
     clean = run_expanded(fx, h, c, new, lens, q, k, key, v, 0.1, t)
     at = before + q0  # the place of the first sequence's query q0
