@@ -257,8 +257,8 @@ class LatentLayer(Layer):
 
     # New tokens of a sequence up to which queries go to the latents rather than latents to
     # keys and values.  Eight sequences, 16 heads of 128 + 64 and 128, latents of 512, both ways
-    # in us: 32 new tokens over 2048 109 and 127, 48 143 and 128; 32 over 8192 209 and 397, 64
-    # 351 and 408; 1 over 256 51 and 42.
+    # in us: 32 new tokens over 2048 107 and 125, 48 142 and 127; 32 over 8192 203 and 373, 64
+    # 348 and 408, 96 619 and 393; 1 over 256 50 and 44.
     FEW = 32
 
     def __init__(self, hidden, heads, nope, rope, vdim, latent, experts, top, inner, positions=4096, seed=0,
