@@ -6,7 +6,10 @@
 // time.  Chunks come straight from memory into a ring of two or three LDS slots.  First
 // product, S = K Q^T: a wave has 16 of the tokens; it reads their codes from LDS in the
 // operand's layout (lane: token lane % 16, 16 codes from 16 (lane / 16)), converts them to
-// f16 (exact) and multiplies them with q in registers.  q is f16 too: scaled by a power of
+// f16 (exact) and multiplies them with q in registers.  (Products with 1152 + code, whose
+// sums start from what that adds, would spare an operation for every two codes, 32 x 1 over
+// 4096, 128 heads in 69 us in place of 76; but where a few channels take the scale and leave
+// the other codes at some steps, such sums leave logits off by 0.05.)  q is f16 too: scaled by a power of
 // two of its row, so that a bf16 or f16 value is exact down to 2^-27 of the row's largest,
 // and f32 is two f16 terms.  P goes to LDS as f16 and after a barrier every wave multiplies
 // all 64 tokens with its own part of the latent's dimensions: O^T = C^T P^T.  The
@@ -89,16 +92,14 @@ __device__ inline unsigned unbiased(unsigned biased) {
   const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
   return __builtin_bit_cast(unsigned, __builtin_bit_cast(v2h, biased) - off);
 }
-// 16 codes as two operands of 8; BIASED: 1152 more than each code.
-template <bool BIASED>
+// 16 codes as two operands of 8.
 __device__ inline void codes_to_halves(v4i w, v8h& lo, v8h& hi) {
-  const auto halves = [](unsigned biased) { return BIASED ? biased : unbiased(biased); };
   v4i r[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const unsigned u = (unsigned)w[i] ^ 0x80808080u;
-    r[i >> 1][2 * (i & 1)] = (int)halves(__builtin_amdgcn_perm(0x64646464u, u, 0x04010400u));
-    r[i >> 1][2 * (i & 1) + 1] = (int)halves(__builtin_amdgcn_perm(0x64646464u, u, 0x04030402u));
+    r[i >> 1][2 * (i & 1)] = (int)unbiased(__builtin_amdgcn_perm(0x64646464u, u, 0x04010400u));
+    r[i >> 1][2 * (i & 1) + 1] = (int)unbiased(__builtin_amdgcn_perm(0x64646464u, u, 0x04030402u));
   }
   lo = __builtin_bit_cast(v8h, r[0]);
   hi = __builtin_bit_cast(v8h, r[1]);
@@ -110,16 +111,9 @@ __device__ inline int pair_of(unsigned first, unsigned second, int at) {
 
 __device__ inline v4f mfma(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// Sums and maxima over rows of 16 lanes, and a wave's sum and running sum.
+// Another lane of the 16 of a row, and a wave's sum and running sum.
 template <int CTRL>
 __device__ inline int lanes(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
-template <typename F>
-__device__ inline float over_16(float v, F f) {
-  v = f(v, __builtin_bit_cast(float, lanes<0xB1>(__builtin_bit_cast(int, v))));   // neighbours
-  v = f(v, __builtin_bit_cast(float, lanes<0x4E>(__builtin_bit_cast(int, v))));   // pairs
-  v = f(v, __builtin_bit_cast(float, lanes<0x141>(__builtin_bit_cast(int, v))));  // mirrored halves of a row
-  return f(v, __builtin_bit_cast(float, lanes<0x140>(__builtin_bit_cast(int, v))));
-}
 __device__ inline int running_sum(int v, int lane, int& all) {
   v += lanes<0x111>(v);  // from 1, 2, 4 and 8 lanes below, in the row
   v += lanes<0x112>(v);
@@ -177,12 +171,6 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   constexpr int kRows = RT * 16, D = LB * 64, kThreads = W * 64;
   constexpr int H = W / 4, QR = RT / H;  // row tiles of a wave in the first product
   constexpr int CB = LB / H;             // 16-dimension tiles of a wave in the second
-  // 16-bit q meets 1152 + code, not the code: one operation fewer for each pair of codes.
-  // What the 1152 adds, 1152 sum q, is where the sums start from, below zero; their fp32
-  // rounding then counts against it: for q of random signs as for the products' magnitudes,
-  // for q of one sign 2^-24 of about 30 times them, far below a 16-bit result's rounding.
-  // 32 x 1 over 4096, 128 heads: 89 us, with the code itself 98.
-  constexpr bool kBiased = QT == 1;
   typedef LatentLds<LB, RT, QT> L;
   // loads of a wave: with eight, the first four waves have the first half of each group
   constexpr int kHalf = (L::kLoads + H - 1) / H, kWaveLoads = W == 8 ? kHalf : L::kLoads + 1;
@@ -357,8 +345,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   lds_barrier();
 
   // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
-  // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity;
-  // behind it -1152 times the sums of the latent's and the key's parts.
+  // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity.
   float* rowq = tops;
   {
     const int sub = threadIdx.x & 15;
@@ -409,7 +396,6 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       const float up = pow2_inverse(step) * 0x1p13f;
 #pragma unroll
       for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
-      float total_l = 0.0f, total_r = 0.0f;
       if constexpr (sizeof(T) == 4) lds_barrier();
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
@@ -423,37 +409,25 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               y[e] = (_Float16)x[k * V + j + e];
-              if (kBiased) (k < N ? total_l : total_r) += (float)y[e];
               x[k * V + j + e] -= (float)y[e];
             }
             *reinterpret_cast<v4h*>(to_lds + (d + j) * 2) = y;
           }
         }
       }
-      if constexpr (kBiased) {
-        const auto plus = [](float a, float b) { return a + b; };
-        total_l = over_16(total_l, plus);
-        total_r = over_16(total_r, plus);
-      }
-      if (sub == 0) {
-        rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
-        rowq[kRows + r] = -1152.0f * total_l;
-        rowq[2 * kRows + r] = -1152.0f * total_r;
-      }
+      if (sub == 0) rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
     }
   }
   if (threadIdx.x < 2) raised[threadIdx.x] = 0;
   lds_barrier();
   v8h q[QT][QR][2 * KB];  // lane: row n of tile r, dimensions 64 b + 16 g + 8 h + 0..7 at 2 b + h
-  float qn[QR], bias_l[QR], bias_r[QR];
+  float qn[QR];
   int limit[QR];
 #pragma unroll
   for (int r = 0; r < QR; ++r) {
     const int row = (half * QR + r) * 16 + n;
     limit[r] = causal ? pos0 + token_of(p, row0 + row) : s.len - 1;
     qn[r] = rowq[row];
-    bias_l[r] = kBiased ? rowq[kRows + row] : 0.0f;
-    bias_r[r] = kBiased ? rowq[2 * kRows + row] : 0.0f;
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -519,15 +493,11 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
     // two sums for the latent, so that a product need not wait for the last
     v4f part[2][QR], turned[QR];
 #pragma unroll
-    for (int r = 0; r < QR; ++r) {
-      part[0][r] = v4f{bias_l[r], bias_l[r], bias_l[r], bias_l[r]};
-      part[1][r] = v4f{0, 0, 0, 0};
-      turned[r] = v4f{bias_r[r], bias_r[r], bias_r[r], bias_r[r]};
-    }
+    for (int r = 0; r < QR; ++r) part[0][r] = part[1][r] = turned[r] = v4f{0, 0, 0, 0};
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       v8h k[2];
-      codes_to_halves<kBiased>(raw[b], k[0], k[1]);
+      codes_to_halves(raw[b], k[0], k[1]);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll

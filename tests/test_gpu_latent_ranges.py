@@ -1,0 +1,64 @@
+"""Attention over the latents at the ends of its range: codes that a few channels leave
+small, queries and scales of any size, row tiles that are not cut.
+
+The tolerance is the one of test_gpu_latent.py, held to what each dimension's own tokens
+weigh: a weight off by a share e moves dimension d by at most e sum_j w_j |v_jd|, not by e
+times the largest value of all dimensions."""
+import math
+
+import pytest
+
+from gpu_util import DEV, note
+from test_gpu_latent import HALF_ULP, TYPES, Cache, check_latent, fx, h, run_latent  # noqa: F401 (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def weighed(cache, s, n, fresh, q, qr, scale):
+    """Of one sequence's causal queries, in 64 bits: weights, values, and of each query the
+    largest sum of a logit's magnitudes."""
+    _, v, k = cache.held(s, n)
+    seen = (torch.arange(n) <= (n - fresh + torch.arange(fresh))[:, None])[:, None]
+    x = torch.where(seen, (q @ v.t() + qr @ k.t()) * scale, -math.inf)
+    mag = (q.abs() @ v.abs().t() + qr.abs() @ k.abs().t()) * abs(scale) * seen
+    return torch.softmax(x, -1), v, mag.amax(-1, keepdim=True)
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("one_sign", [True, False], ids=["one sign", "both signs"])
+@pytest.mark.parametrize("rms", [1.0, 6.0])
+@pytest.mark.parametrize("latent,heads", [(512, 16), (512, 40), (256, 16), (256, 64)])
+def test_latent_attention_of_few_large_channels(fx, h, t, one_sign, rms, latent, heads):
+    """Two channels of every latent are +-127 and its scale follows them, the others have a
+    few steps; queries are small there, so that the logits (of deviation 8) come from the
+    small codes.  The error's norm against that of its parts: the result's rounding, the
+    weights' (2^-11, a share of each by itself), and the logits': fewer than 81 sums, each off
+    by 2^-24 of the magnitudes, at random 9 times that, for a weight and for the sum of all.
+    (Sums that start at or pass a constant of 1152 times the query are off by 0.05 here.)"""
+    note("few large channels", t, one_sign, rms, latent, heads)
+    lens = [700, 90]
+    cache = Cache(fx, lens, latent, 32, 64, seed=2)
+    cache.fill(lens, 17, spread=0.0)
+    g = torch.Generator().manual_seed(23)
+    few = [40, 200]
+    codes = (torch.randn(*cache.codes.shape, generator=g) * rms).round()
+    codes[..., few] = 127 * torch.randn(*cache.codes.shape[:2], 2, generator=g).sign()
+    cache.codes.copy_(codes)
+    make = (lambda *s: torch.rand(*s, generator=g) + 1) if one_sign else (lambda *s: torch.randn(*s, generator=g))
+    q, qr = make(2, heads, latent), 1e-3 * make(2, heads, 32)
+    q[..., few] *= 2.0 ** -10
+    q, qr = q.to(TYPES[t]), qr.to(TYPES[t])
+    _, v, _ = cache.held(0, lens[0])
+    scale = float(8 / (q[0].double() @ v.t()).std())
+    got = run_latent(fx, h, cache, [1, 1], lens, q, qr, scale, 1, t)
+    assert fx.sync_status(h) == 0
+    for s, n in enumerate(lens):
+        w, v, mag = weighed(cache, s, n, 1, q[s : s + 1].double(), qr[s : s + 1].double(), scale)
+        want = w @ v
+        rounding = (want.to(TYPES[t]).double() - want).norm()
+        uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+        logits = 2 * (9 * 2.0 ** -24 + (2.0 ** -22 if t == "f32" else 0)) * (mag * (w @ v.abs())).norm()
+        sums = 2 * (n + 64) * 2.0 ** -24 * (w @ v.abs()).norm()
+        assert (got[s : s + 1].double() - want).norm() <= rounding + uP * ((w * w) @ (v * v)).sqrt().norm() + logits + sums
