@@ -391,8 +391,9 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       top = max(top, (unsigned)lanes<0x141>((int)top));
       top = max(top, (unsigned)lanes<0x140>((int)top));
       const bool fine = top < 0x7F800000u;
-      const float step = __builtin_bit_cast(
-          float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u);
+      // 2^126 at most, whose inverse is a normal number: q stays below 2^15, which f16 holds
+      const float step = fminf(0x1p126f, __builtin_bit_cast(
+          float, __builtin_bit_cast(unsigned, fmaxf(fine ? __builtin_bit_cast(float, top) : 1.0f, kScaleFloor)) & 0x7F800000u));
       const float up = pow2_inverse(step) * 0x1p13f;
 #pragma unroll
       for (int k = 0; k < LB * 4 + 4; ++k) x[k] = fine ? x[k] * up : 0.0f;

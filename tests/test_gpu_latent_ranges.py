@@ -62,3 +62,33 @@ def test_latent_attention_of_few_large_channels(fx, h, t, one_sign, rms, latent,
         logits = 2 * (9 * 2.0 ** -24 + (2.0 ** -22 if t == "f32" else 0)) * (mag * (w @ v.abs())).norm()
         sums = 2 * (n + 64) * 2.0 ** -24 * (w @ v.abs()).norm()
         assert (got[s : s + 1].double() - want).norm() <= rounding + uP * ((w * w) @ (v * v)).sqrt().norm() + logits + sums
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("latent,heads", [(256, 4), (512, 20)])
+@pytest.mark.parametrize("power,scale,token", [(126, 2.0 ** -100, 1.0), (127, 2.0 ** -100, 1.0), (127, -(2.0 ** -90), 2.0 ** -14)])
+def test_latent_attention_of_the_largest_queries(fx, h, t, latent, heads, power, scale, token):
+    """Queries up to the end of their type.  Logits past 2^24 that differ by 2^-9 of their size
+    and more: one token takes all, as in the test of large logits."""
+    takes_the_largest(fx, h, t, latent, heads, 2.0 ** power, scale, token)
+
+
+def takes_the_largest(fx, h, t, latent, heads, size, scale, token):
+    note("one takes all", t, latent, heads, size, scale, token)
+    lens = [500]
+    cache = Cache(fx, lens, latent, 32, 64)
+    cache.fill(lens, 31, spread=0.6)
+    cache.scale *= token
+    g = torch.Generator().manual_seed(2)
+    q = (0.9 * torch.rand(1, heads, latent, generator=g) + 1) * torch.rand(1, heads, latent, generator=g).sub(0.5).sign()
+    q, qr = (q * size).to(TYPES[t]), torch.zeros(1, heads, 32).to(TYPES[t])
+    _, v, _ = cache.held(0, lens[0])
+    x = q[0].double() @ v.t() * scale
+    top = x.topk(2, -1)
+    told = (top.values[:, 0] - top.values[:, 1]) / x.abs().amax(-1) > 2.0 ** -9
+    assert told.sum() >= heads // 2 and x.abs().max() > 2.0 ** 24
+    want = v[top.indices[:, 0]]
+    got = run_latent(fx, h, cache, [1], lens, q, qr, scale, 1, t)[0].double()
+    assert fx.sync_status(h) == 0
+    uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+    assert ((got - want).abs() <= want.abs() * (uP + 8 * 2.0 ** -24 + 1.01 * HALF_ULP[t]))[told].all()
