@@ -187,7 +187,11 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   const float* latent_scale = p.a.c.scale;
   const float* key_scale = p.a.c.rope_scale;
   unsigned* flags = p.flags;
-  const float to_log2 = p.a.scale * 1.44269504088896340736f;
+  // The softmax's scale in two factors: its power of two goes to the rows with q's, the rest
+  // and q's 2^13 to the tokens.  Products of either with what it meets stay in fp32's range
+  // wherever the logits do, whichever of q, cache and scale is large.
+  const float unit = fminf(fmaxf(__builtin_bit_cast(float, __builtin_bit_cast(unsigned, p.a.scale) & 0x7F800000u), 0x1p-126f), 0x1p126f);
+  const float to_log2 = p.a.scale * pow2_inverse(unit) * (1.44269504088896340736f * 0x1p-13f);
 
   // Row tiles of one part of a cache are 8 ids apart: on one XCD, whose L2 they share.
   const unsigned oct = blockIdx.x / 8;
@@ -345,7 +349,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   lds_barrier();
 
   // q to f16, 16 threads a row, scaled by a power of two; the waves take their operands
-  // from LDS then.  rowq: the row's power of two, NaN where it holds a NaN or an infinity.
+  // from LDS then.  rowq: the row's power of two (with the softmax scale's), NaN where it holds a NaN or an infinity.
   float* rowq = tops;
   {
     const int sub = threadIdx.x & 15;
@@ -416,7 +420,7 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
           }
         }
       }
-      if (sub == 0) rowq[r] = fine ? step * 0x1p-13f : __builtin_nanf("");
+      if (sub == 0) rowq[r] = fine ? fminf(fmaxf(step * unit, 0x1p-149f), 0x1p127f) : __builtin_nanf("");
     }
   }
   if (threadIdx.x < 2) raised[threadIdx.x] = 0;

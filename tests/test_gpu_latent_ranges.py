@@ -92,3 +92,30 @@ def takes_the_largest(fx, h, t, latent, heads, size, scale, token):
     assert fx.sync_status(h) == 0
     uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
     assert ((got - want).abs() <= want.abs() * (uP + 8 * 2.0 ** -24 + 1.01 * HALF_ULP[t]))[told].all()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("latent,heads", [(256, 4), (512, 20)])
+@pytest.mark.parametrize("size,scale,token", [(1.0, 2.0 ** 14, 2.0 ** 100), (1.0, -(2.0 ** 20), 2.0 ** 94), (2.0 ** -90, 2.0 ** 40, 2.0 ** 95),
+                                              (2.0 ** 100, 2.0 ** 110, 2.0 ** -100), (2.0 ** 110, 2.0 ** -126, 2.0 ** 60)])
+def test_latent_attention_of_large_logits_of_any_factors(fx, h, t, latent, heads, size, scale, token):
+    """Logits that fp32 holds, whichever of query, latent and softmax scale they owe it to."""
+    takes_the_largest(fx, h, t, latent, heads, size, scale, token)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [4, 20])
+@pytest.mark.parametrize("size,scale,token", [(2.0 ** 120, 2.0 ** -60, 2.0 ** -60), (2.0 ** 100, 2.0 ** -110, 2.0 ** 10),
+                                              (2.0 ** -90, 2.0 ** 90, 1.0), (2.0 ** -60, 2.0 ** -30, 2.0 ** 90)])
+def test_latent_attention_of_ordinary_logits_of_any_factors(fx, h, t, heads, size, scale, token):
+    note("factors", t, heads, size, scale, token)
+    lens = [500]
+    cache = Cache(fx, lens, 256, 32, 64)
+    cache.fill(lens, 18)
+    cache.scale *= token
+    cache.rope_scale *= token
+    g = torch.Generator().manual_seed(4)
+    q, qr = ((torch.randn(1, heads, d, generator=g) * size).to(TYPES[t]) for d in (256, 32))
+    got = run_latent(fx, h, cache, [1], lens, q, qr, 0.2 * scale, 1, t)
+    assert fx.sync_status(h) == 0
+    check_latent(got, cache, lens, [1], q, qr, float(torch.tensor(0.2 * scale)), 1, t)
