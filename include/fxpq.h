@@ -801,6 +801,9 @@ fxpq_status fxpq_latent_read(fxpq_handle h, const fxpq_latent_cache* cache,
  * hdq, q_rope: `rope` reals at token * ldqr + head * hdqr, out: `latent` reals at
  * token * ldo + head * hdo (strides in any order; out's rows overlap neither each
  * other nor an input).  A query that sees no token gets 0, one that holds a NaN or an infinity NaN.
+ * Latents are taken against the largest scale among their sequence's tokens, seen or not: what lies
+ * below 2^-64 of it (2^-24 where logits pass 2^24) may count as 0.
+ * Weights are divided by their sum last: 2^16 * tokens * scale has to stay below 2^128.
  * workspace as for fxpq_token_gemm.
  */
 fxpq_status fxpq_latent_attention_workspace(fxpq_handle h, const fxpq_latent_cache* cache,
@@ -836,7 +839,8 @@ typedef struct {
  * own (the new tokens are the sequence's last rows).  q: rows of heads * (nope +
  * rope) reals, row stride ldq; out: rows of heads * vdim reals, row stride ldo, apart
  * from all inputs.  A query that sees no token gets 0; keys and values that a query does not see have no
- * part in its result, whatever they hold.  Of the batch start, length, seqs, tokens,
+ * part in its result, whatever they hold.  Weights are divided by their sum last: 2^8 *
+ * tokens * max |v| has to stay below 2^128.  Of the batch start, length, seqs, tokens,
  * max_new and max_len are used (table is not, and may be NULL).  A sequence whose
  * numbers contradict the bounds or kv->start is skipped and raises FXPQ_FLAG_RANGE.
  */

@@ -77,6 +77,9 @@ constexpr float kSlack = 8.0f;
 // largest keep all 11 bits and smaller ones lose at most 2^-31 of it.
 constexpr float kLift = 64.0f;
 constexpr float kLeastLog = -50.0f;  // of s_t / R, where it only moves the reference
+// A reference follows a growing R down until the sum of its row is 2^kMostSum.  2^30 tokens add
+// at most 2^(30 + kSlack - kLeastLog) to it.
+constexpr float kMostSum = 96.0f;
 constexpr float kFar = 0x1p24f;  // logits past this have steps above 1: s_t / R would be rounded
 
 __device__ inline void lds_barrier() {
@@ -154,7 +157,7 @@ struct LatentLds {
   static constexpr int kP = RT * 16 * kPRow;
   static constexpr int kWeights = kScales + kSlots * 4 * 256;  // [2][QT] P
   static constexpr int kStats = kWeights + 2 * QT * kP;
-  static constexpr int kBytes = kStats + 4 * RT * 16 * 4 + 64;
+  static constexpr int kBytes = kStats + 2 * 4 * RT * 16 * 4 + 64;
   // q as f16 lies in the slots behind the first until the waves have taken it
   static constexpr int kQRow = (LB * 64 + 64) * 2, kQ = RT * 16 * kQRow;
   static_assert(QT * kQ <= (kSlots - 1) * kSlot, "q fits");
@@ -177,7 +180,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
   static_assert(W == 4 || L::kLoads - kHalf + 1 == kHalf, "both halves wait for as many loads");
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
   float* tops = reinterpret_cast<float*>(lds + L::kStats);          // [4][kRows]
-  float* scales = tops + 4 * kRows;                                 // [4]
+  float* sums = tops + 4 * kRows;                                   // [4][kRows]
+  float* scales = sums + 4 * kRows;                                 // [4]
   volatile int* raised = reinterpret_cast<volatile int*>(scales + 4);  // [2]: chunk + 1 of the last that passed its reference
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tg = wave & 3, half = W == 8 ? wave >> 2 : 0;
@@ -596,7 +600,8 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       // the power of two above it
       most = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, most) & 0x7F800000u) + 0x00800000u);
       const float now_r = fmaxf(R, most);
-      const float ratio = R > 0.0f ? R * pow2_inverse(now_r) : 1.0f;  // at most 1
+      // what came before has 2^fall of the weight that it had against the old R
+      const int fall = R > 0.0f ? (int)(__builtin_bit_cast(unsigned, R) >> 23) - (int)(__builtin_bit_cast(unsigned, now_r) >> 23) : 0;
       R = now_r;
       // past kFar s_t / R (below 1) is left out of references: a logit's rounding would move it
       // by more than they may be off
@@ -611,7 +616,13 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
 #pragma unroll
       for (int r = 0; r < QR; ++r) {
         const float y = over_groups(top_of(r));
-        if (g == 0) tops[tg * kRows + (half * QR + r) * 16 + n] = y;
+        float sum = l[r];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (g == 0) {
+          tops[tg * kRows + (half * QR + r) * 16 + n] = y;
+          sums[tg * kRows + (half * QR + r) * 16 + n] = sum;
+        }
       }
       lds_barrier();
       float down[RT];
@@ -619,12 +630,13 @@ __global__ __launch_bounds__(W * 64, W == 8 || (RT == 1 && sizeof(T) == 2) ? 2 :
       for (int r = 0; r < RT; ++r) {
         const int row = r * 16 + n;
         const float top = fmaxf(fmaxf(tops[row], tops[kRows + row]), fmaxf(tops[2 * kRows + row], tops[3 * kRows + row]));
-        // what came before weighs `ratio` of what it did against the new R
-        const float before = m[r] == kNoMax ? kNoMax : m[r] + __builtin_amdgcn_logf(ratio);
+        const float sum = sums[row] + sums[kRows + row] + sums[2 * kRows + row] + sums[3 * kRows + row];
+        const float lower = fmaxf((float)fall, fminf(__builtin_amdgcn_logf(sum) - kMostSum, 0.0f));
+        const float before = m[r] == kNoMax ? kNoMax : m[r] + lower;
         const float now = top > before + kSlack ? top : before;
         down[r] = m[r] == kNoMax ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
         m[r] = now;
-        const float f = down[r] * ratio;
+        const float f = __builtin_amdgcn_ldexpf(down[r], fall);
 #pragma unroll
         for (int c = 0; c < CB; ++c) o[r][c] *= f;
       }

@@ -119,3 +119,37 @@ def test_latent_attention_of_ordinary_logits_of_any_factors(fx, h, t, heads, siz
     got = run_latent(fx, h, cache, [1], lens, q, qr, 0.2 * scale, 1, t)
     assert fx.sync_status(h) == 0
     check_latent(got, cache, lens, [1], q, qr, float(torch.tensor(0.2 * scale)), 1, t)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [1, 40, 560])
+@pytest.mark.parametrize("n,small,large", [(64, 0.0, 2.0 ** 20), (64, 0.0, 2.0 ** 90), (3000, 0.0, 2.0 ** 40), (256, 2.0 ** -90, 2.0 ** 30),
+                                           (256, 2.0 ** -40, 2.0 ** 90), (1000, 1.0, 2.0 ** 60), (300, 1.0, 2.0 ** 50), (65, 2.0 ** -20, 2.0 ** 30)])
+def test_latent_attention_of_scales_far_apart(fx, h, t, heads, n, small, large):
+    """The last token's scale is that many times the others'.  The query before it does not
+    see it: its result, and the last one's, are right by their own measure.  (small 0: tokens of
+    zeros as append writes them.)"""
+    note("scales apart", t, heads, n, small, large)
+    lens, new = [n + 1], [2]
+    cache = Cache(fx, lens, 256, 32, 64)
+    cache.fill(lens, 13)
+    last = torch.arange(n + 1)
+    page = torch.from_numpy(cache.table[0])[last // 64].long().to(DEV)
+    slot = (last % 64).to(DEV)
+    cache.scale[page[:n], slot[:n]] = small or 2.0 ** -100 / 127
+    if not small:
+        cache.codes[page[:n], slot[:n], :256] = 0
+    cache.scale[page[n], slot[n]] = large
+    g = torch.Generator().manual_seed(6)
+    q, qr = torch.zeros(2, heads, 256).to(TYPES[t]), torch.randn(2, heads, 32, generator=g).to(TYPES[t])
+    got = run_latent(fx, h, cache, new, lens, q, qr, 0.2, 1, t).double()
+    assert fx.sync_status(h) == 0
+    w, v, mag = weighed(cache, 0, n + 1, 2, q.double(), qr.double(), float(torch.tensor(0.2)))
+    d = mag * (40 * 2.0 ** -24 + (2.0 ** -22 if t == "f32" else 0)) + 4 * 2.0 ** -24 * mag
+    uP = 2.0 ** -22 if t == "f32" else 2.0 ** -11
+    for i in range(2):
+        vi = v[: n + i]
+        wi = w[i, :, : n + i]
+        tol = (2 * d[i] + 4 * 2.0 ** -23 + uP + 2 * (n + 64) * 2.0 ** -24) * (wi @ vi.abs()) + n * 2.0 ** -31 * vi.abs().max()
+        off = (got[i] - wi @ vi).abs()
+        assert (off <= tol + 1.01 * HALF_ULP[t] * (wi @ vi).abs()).all(), (i, float(off.max()))
