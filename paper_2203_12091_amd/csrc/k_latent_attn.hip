@@ -836,7 +836,9 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
   p.rt = rt;
   p.row_tiles = (int)((rows + rt * 16 - 1) / (rt * 16));
   p.rounds = 1;
-  p.shared = (int64_t)p.row_tiles * b.seqs < 4 * (int64_t)c.cus && b.seqs <= kMostSeqs && p.row_tiles <= c.cus / 8;
+  // (the kernel counts a cut's chunks in 32 bits)
+  p.shared = (int64_t)p.row_tiles * b.seqs < 4 * (int64_t)c.cus && b.seqs <= kMostSeqs && p.row_tiles <= c.cus / 8 &&
+             chunks * b.seqs < INT64_C(0x7FF00000);
   if (!p.shared) {
     p.groups = b.seqs;
     p.each = chunks;

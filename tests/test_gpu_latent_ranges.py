@@ -153,3 +153,14 @@ def test_latent_attention_of_scales_far_apart(fx, h, t, heads, n, small, large):
         tol = (2 * d[i] + 4 * 2.0 ** -23 + uP + 2 * (n + 64) * 2.0 ** -24) * (wi @ vi.abs()) + n * 2.0 ** -31 * vi.abs().max()
         off = (got[i] - wi @ vi).abs()
         assert (off <= tol + 1.01 * HALF_ULP[t] * (wi @ vi).abs()).all(), (i, float(off.max()))
+
+
+def test_latent_attention_of_bounds_past_what_is_counted(fx, h):
+    """Sequences of more than 2^31 chunks in all, by their bounds, are not cut: a cut's counts
+    would not fit 32 bits.  (Only the work space is asked for, which cut calls need.)"""
+    codes, scale = torch.zeros(1, 128, 288, dtype=torch.int8, device=DEV), torch.zeros(1, 128, device=DEV)
+    cache = fx.latent_cache(codes, scale, scale, 1, 128, 256, 32)
+    some = torch.zeros(257, dtype=torch.int32, device=DEV)
+    for seqs, most, cut in ((256, 1 << 30, False), (128, 1 << 30, False), (127, 1 << 30, True), (256, 1 << 28, True)):
+        batch = fx.kv_batch(some, some, some, seqs, 1 << 23, seqs, 1, most)
+        assert (fx.latent_attention_workspace(h, cache, batch, 1) > 0) == cut
