@@ -177,8 +177,9 @@ bool latent_batch_ok(const fxpq_kv_batch* b, const fxpq_latent_cache* c) {
 
 // Rows of `width` at token * ld + head * hd that do not overlap.
 bool apart(int64_t tokens, int64_t heads, int64_t width, int64_t ld, int64_t hd) {
+  // (2^31 tokens 2^40 apart do not fit 64 bits)
   return ld >= width && hd >= width && ld <= (INT64_C(1) << 40) && hd <= (INT64_C(1) << 40) &&
-         (ld >= (heads - 1) * hd + width || hd >= (tokens - 1) * ld + width);
+         (ld >= (heads - 1) * hd + width || (hd - width) / ld >= tokens - 1);
 }
 
 bool latent_heads_ok(int heads, const fxpq_kv_batch* b) {

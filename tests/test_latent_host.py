@@ -132,3 +132,10 @@ def test_calls_without_tokens_return_at_once(calls):
     n = C.c_int64(-1)
     assert calls.L.fxpq_latent_attention_workspace(calls.h, C.byref(calls.cache()), C.byref(none), 4, C.byref(n)) == calls.fx.OK
     assert n.value == 0
+
+
+def test_rows_that_overlap_whatever_the_strides(calls):
+    """2^31 - 1 tokens 2^33 apart: the last begins past 2^63, far behind the next head's first."""
+    batch = calls.batch(tokens=2 ** 31 - 1)
+    assert calls.attention(None, batch, ldo=2 ** 33, hdo=2 ** 34) == calls.fx.ERR_INVALID_ARG
+    assert calls.append(None, batch, ldqo=2 ** 33, hdqo=2 ** 34) == calls.fx.ERR_INVALID_ARG
