@@ -263,7 +263,12 @@ class LatentLayer(Layer):
 
     def __init__(self, hidden, heads, nope, rope, vdim, latent, experts, top, inner, positions=4096, seed=0,
                  dtype=torch.bfloat16, device="cuda:0"):
+        if latent not in (256, 512) or rope not in (16, 32, 48, 64) or nope % 16 or (heads * vdim) % 16 or min(nope, heads, vdim) < 1:
+            raise ValueError(f"{heads} heads of {nope} + {rope} and {vdim}, latents of {latent}: 256 or 512, a rotary part of 16, 32, 48 "
+                             "or 64, and sizes of products that 16 divides")
         self.heads, self.nope, self.rope, self.vdim, self.latent = heads, nope, rope, vdim, latent
+        # heads of other sizes have attention over the latents only, which is right for prompts too
+        self.expands = nope in (64, 128) and vdim in (64, 128) and rope in (32, 64)
         weight = self._begin(hidden, experts, top, inner, seed, dtype, device)
         self.q = quantize_rows(self.h, weight(heads * (nope + rope), hidden))
         self.into = quantize_rows(self.h, weight(latent + rope, hidden))
@@ -291,7 +296,7 @@ class LatentLayer(Layer):
                          self.latent + self.rope, turn, self.heads * width, width, turn, self.heads * width, width,
                          self.heads, dt)
         # (a batch made by hand does not say how many tokens its sequences hold)
-        few = batch.max_new <= self.FEW or not hasattr(batch, "held")
+        few = batch.max_new <= self.FEW or not self.expands or not hasattr(batch, "held")
         return self._linear((self.absorbed if few else self.expanded)(q, cache, batch), self.out)
 
     def absorbed(self, q, cache, batch):

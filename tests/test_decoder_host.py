@@ -219,3 +219,21 @@ def test_latent_layer_without_new_tokens_and_with_another_cache(latent):
     with pytest.raises(ValueError):
         other_layer.forward(torch.zeros(2, 64), cache, cache.extend([0], [2]))
     assert cache.length == {0: 7}  # that cache took its batch back
+
+
+@pytest.mark.parametrize("nope,rope,vdim", [(64, 16, 64), (64, 48, 64), (80, 32, 64), (64, 32, 32), (128, 64, 96)])
+def test_latent_layer_of_heads_that_are_not_expanded(latent, nope, rope, vdim):
+    """Prompts of any length go to the latents, as single tokens do."""
+    layer = latent.LatentLayer(64, 4, nope, rope, vdim, 256, experts=4, top=2, inner=48, dtype=torch.float32, device="cpu")
+    cache = latent.LatentCache(pages=8, page=16, latent=256, rope=rope, max_pages_per_seq=4, max_seqs=3, device="cpu")
+    latent.fx.calls.clear()
+    assert layer.forward(torch.zeros(layer.FEW + 1, 64), cache, cache.extend([0], [layer.FEW + 1])).shape == (layer.FEW + 1, 64)
+    assert "latent_attention" in latent.fx.names() and "expanded_attention" not in latent.fx.names()
+
+
+@pytest.mark.parametrize("kw", [dict(latent=384), dict(latent=0), dict(rope=24), dict(rope=80), dict(rope=0), dict(nope=40), dict(nope=0),
+                                dict(vdim=6), dict(vdim=0), dict(heads=0)], ids=str)
+def test_latent_layer_of_sizes_that_no_call_takes(latent, kw):
+    sizes = {**dict(heads=4, nope=64, rope=32, vdim=64, latent=256), **kw}
+    with pytest.raises(ValueError):
+        latent.LatentLayer(64, *sizes.values(), experts=4, top=2, inner=48, dtype=torch.float32, device="cpu")

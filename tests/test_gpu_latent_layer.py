@@ -286,3 +286,20 @@ def test_many_sequences_and_rows_behind_the_last(fx, dec, S):
             assert ((out[row].double() - want).abs() <= c.abs().max() * (60000 * 2.0 ** -24 + 2.0 ** -19)).all()
             row += 1
     h.close()
+
+
+@pytest.mark.parametrize("nope,rope,vdim", [(80, 16, 32), (64, 48, 96), (16, 32, 16)])
+def test_layer_of_heads_that_are_not_expanded(dec, fx, nope, rope, vdim):
+    """Heads that attention over keys and values does not take: a prompt in one call and in
+    small ones, over the latents both ways.  They differ in the order of fp32 sums, by which
+    a value may get the next code: one in 10^4 of them, of a step of 1 / 127 of the row's
+    largest (four times its rms), 3e-4 of a row's norm in each of four products."""
+    note("latent layer", nope, rope, vdim)
+    layer = dec.LatentLayer(256, 6, nope, rope, vdim, 256, experts=4, top=2, inner=160, dtype=torch.float32, seed=4)
+    caches = [dec.LatentCache(pages=60, page=16, latent=256, rope=rope, max_pages_per_seq=20, max_seqs=4) for _ in range(2)]
+    x = torch.randn(layer.FEW + 30, 256, generator=torch.Generator().manual_seed(5)).to(DEV)
+    whole = layer.attend(x, caches[0], caches[0].extend([0], [len(x)]))
+    parts = torch.cat([layer.attend(y, caches[1], caches[1].extend([0], [len(y)])) for y in x.split(16)])
+    assert fx.sync_status(layer.h) == 0
+    assert (whole - parts).norm() <= 1.2e-3 * whole.norm()
+    layer.h.close()
