@@ -78,13 +78,15 @@ class Pages:
             pages += [self.free.pop() for _ in range(m - len(pages))]
             self.length[s] = self.length.get(s, 0) + n
             table[i, : len(pages)] = torch.tensor(pages, dtype=torch.int32)
-        length = [self.length[s] for s in seqs]
-        start = torch.tensor([0] + list(new)).cumsum(0).to(torch.int32)
-        put = lambda t: t.to(self.device)  # noqa: E731
-        batch = fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(seqs),
-                            self.max_pages, sum(new), max(new), max(length))
+        batch = self._batch(list(new), [self.length[s] for s in seqs], table)
         batch.grown = dict(zip(seqs, new))
         return batch
+
+    def _batch(self, new, length, table):
+        start = torch.tensor([0] + new).cumsum(0).to(torch.int32)
+        put = lambda t: t.to(self.device)  # noqa: E731
+        return fx.kv_batch(put(start), put(torch.tensor(length, dtype=torch.int32)), put(table), len(new),
+                           self.max_pages, sum(new), max(new), max(length))
 
     def retract(self, batch):
         """Takes back the newest batch of its sequences, whose tokens were not computed:
@@ -126,12 +128,31 @@ class LatentCache(Pages):
         self.scale, self.rope_scale = torch.zeros(pages, page, device=device), torch.zeros(pages, page, device=device)
         self.desc = fx.latent_cache(self.codes, self.scale, self.rope_scale, pages, page, latent, rope)
 
-    def extend(self, seqs, new):
-        batch = super().extend(seqs, new)
+    def _batch(self, new, length, table):
+        batch = super()._batch(new, length, table)
         # all tokens of the sequences, and where each one's begin among them
-        rows = torch.tensor([0] + [self.length[s] for s in seqs]).cumsum(0)
+        rows = torch.tensor([0] + length).cumsum(0)
         batch.held, batch.rows = int(rows[-1]), rows.to(torch.int32).to(self.device)
+        batch.host = new, length, table
         return batch
+
+    def split(self, batch, few):
+        """The sequences of up to `few` new tokens and those of more, as batches of their own:
+        (batch, the rows of its tokens in the whole one's) for each, None where there are no
+        such tokens, the whole one and None where there are no others.  Kept with the batch,
+        which several layers use."""
+        kept = batch.__dict__.setdefault("halves", {})
+        if few not in kept:
+            new, length, table = batch.host
+            first = [sum(new[:i]) for i in range(len(new))]
+
+            def half(which):
+                if not which or len(which) == len(new):
+                    return (batch, None) if which else None
+                rows = torch.cat([torch.arange(first[i], first[i] + new[i]) for i in which])
+                return self._batch([new[i] for i in which], [length[i] for i in which], table[which]), rows.to(self.device)
+            kept[few] = (half([i for i, n in enumerate(new) if 0 < n <= few]), half([i for i, n in enumerate(new) if n > few]))
+        return kept[few]
 
 
 class Layer:
@@ -255,7 +276,7 @@ class LatentLayer(Layer):
     """The same with latent attention: `heads` heads of nope + rope dimensions with values
     of vdim, all made of one latent vector a token."""
 
-    # New tokens of a sequence up to which queries go to the latents rather than latents to
+    # New tokens of a sequence up to which its queries go to the latents rather than latents to
     # keys and values.  Eight sequences, 16 heads of 128 + 64 and 128, latents of 512, both ways
     # in us: 32 new tokens over 2048 107 and 125, 48 142 and 127; 32 over 8192 203 and 373, 64
     # 348 and 408, 96 619 and 393; 1 over 256 50 and 44.
@@ -295,9 +316,22 @@ class LatentLayer(Layer):
         fx.latent_append(self.h, cache.desc, batch, self.rotary, fx.SCALE_MAX, c, self.latent, cr[:, self.latent :],
                          self.latent + self.rope, turn, self.heads * width, width, turn, self.heads * width, width,
                          self.heads, dt)
-        # (a batch made by hand does not say how many tokens its sequences hold)
-        few = batch.max_new <= self.FEW or not self.expands or not hasattr(batch, "held")
-        return self._linear((self.absorbed if few else self.expanded)(q, cache, batch), self.out)
+        # Each sequence has the form that its own new tokens ask for, whatever its neighbours'.
+        # (A batch made by hand does not say how many tokens its sequences hold; one with `held`
+        # and `rows` is taken whole.)
+        if batch.max_new <= self.FEW or not self.expands or not hasattr(batch, "held"):
+            few, many = (batch, None), None
+        elif not hasattr(batch, "host"):
+            few, many = None, (batch, None)
+        else:
+            few, many = cache.split(batch, self.FEW)
+        if few is None or many is None:
+            y = self.absorbed(q, cache, few[0]) if few else self.expanded(q, cache, many[0])
+        else:
+            y = q.new_empty(t, self.heads * self.vdim)
+            for form, (part, rows) in ((self.absorbed, few), (self.expanded, many)):
+                y[rows] = form(q[rows], cache, part)
+        return self._linear(y, self.out)
 
     def absorbed(self, q, cache, batch):
         """Attention over the latents: [tokens][heads * vdim]."""

@@ -237,3 +237,39 @@ def test_latent_layer_of_sizes_that_no_call_takes(latent, kw):
     sizes = {**dict(heads=4, nope=64, rope=32, vdim=64, latent=256), **kw}
     with pytest.raises(ValueError):
         latent.LatentLayer(64, *sizes.values(), experts=4, top=2, inner=48, dtype=torch.float32, device="cpu")
+
+
+def test_latent_layer_of_prompts_and_single_tokens_together(latent):
+    """Each sequence by its own new tokens: only a prompt's context is read and expanded, a
+    sequence without new tokens is in neither half."""
+    layer, _ = make_latent(latent)
+    cache = latent.LatentCache(pages=40, page=16, latent=256, rope=32, max_pages_per_seq=8, max_seqs=6, device="cpu")
+    cache.extend([0, 1, 2, 3], [100, 20, 30, 90])
+    F = layer.FEW
+    batch = cache.extend([0, 4, 1, 2, 3], [1, F + 1, F + 5, 0, F])
+    latent.fx.calls.clear()
+    assert layer.forward(torch.zeros(batch.tokens, 64), cache, batch).shape == (batch.tokens, 64)
+    calls = dict(latent.fx.calls)
+    few, many = calls["latent_attention"][2], calls["latent_read"][2]
+    assert (few.seqs, few.tokens, few.max_new, few.max_len) == (2, F + 1, F, 90 + F)
+    assert (many.seqs, many.tokens, many.held) == (2, 2 * F + 6, F + 1 + 20 + F + 5)
+    assert calls["expanded_attention"][2] is many and many.rows.tolist() == [0, F + 1, many.held]
+    assert calls["latent_append"][2] is batch and latent.fx.names().count("latent_append") == 1
+    (a, at_few), (b, at_many) = cache.split(batch, F)
+    assert a is few and b is many  # the next layer's too
+    assert at_few.tolist() == [0, *range(2 * F + 7, 3 * F + 7)] and at_many.tolist() == list(range(1, 2 * F + 7))
+    # prompts alone are taken as they are, beside a sequence without new tokens in a batch of their own
+    batch = cache.extend([4, 5], [F + 1, F + 2])
+    assert cache.split(batch, F) == (None, (batch, None))
+    none, (part, rows) = cache.split(cache.extend([4, 0], [F + 1, 0]), F)
+    assert none is None and part.seqs == 1 and part.held == 3 * (F + 1) and len(rows) == F + 1
+
+
+def test_batch_made_by_hand_that_says_what_it_holds(latent):
+    layer, cache = make_latent(latent)
+    layer.forward(torch.zeros(40, 64), cache, cache.extend([0], [40]))
+    told = cache.extend([0], [layer.FEW - 30])
+    hand = types.SimpleNamespace(seqs=1, tokens=layer.FEW + 1, max_new=layer.FEW + 1, max_len=60, held=60, rows=told.rows)
+    latent.fx.calls.clear()
+    layer.attend(torch.zeros(hand.tokens, 64), cache, hand)
+    assert "expanded_attention" in latent.fx.names()

@@ -303,3 +303,25 @@ def test_layer_of_heads_that_are_not_expanded(dec, fx, nope, rope, vdim):
     assert fx.sync_status(layer.h) == 0
     assert (whole - parts).norm() <= 1.2e-3 * whole.norm()
     layer.h.close()
+
+
+def test_prompts_and_single_tokens_in_one_batch(dec, fx):
+    """Each sequence's result is what it is alone (the orders of fp32 sums differ: as above)."""
+    layer, cache = layer_of(dec, torch.float32)
+    g = torch.Generator().manual_seed(6)
+    make = lambda n: torch.randn(n, 256, generator=g).to(DEV)  # noqa: E731
+    layer.attend(make(150), cache, cache.extend([0, 1, 2], [50, 70, 30]))
+    new = [1, layer.FEW + 8, 0, layer.FEW]
+    x = make(sum(new))
+    batch = cache.extend([0, 1, 2, 3], new)
+    got = layer.attend(x, cache, batch).split(new)
+    start, length, table = batch._refs
+    for i, (n, y) in enumerate(zip(new, x.split(new))):
+        if not n:
+            continue
+        # the tokens are in the cache already: writing them again writes the same
+        one = cache._batch([n], [int(length[i])], table[i : i + 1].cpu())
+        want = layer.attend(y, cache, one)
+        assert (got[i] - want).norm() <= 1.2e-3 * want.norm()
+    assert fx.sync_status(layer.h) == 0
+    layer.h.close()
