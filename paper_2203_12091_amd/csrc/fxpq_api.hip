@@ -147,15 +147,7 @@ bool cache_ok(const fxpq_kv_cache* c) {
          c->heads <= kMaxHeads / 2 && c->dim >= 16 && c->dim <= 256 && c->dim % 16 == 0;
 }
 
-bool batch_ok(const fxpq_kv_batch* b, const fxpq_kv_cache* c) {
-  return b && b->start && b->length && b->table && aligned(b->start, 4) && aligned(b->length, 4) &&
-         aligned(b->table, 4) && b->seqs >= 1 && b->seqs <= 65535 && b->table_ld >= 1 && b->tokens >= 0 &&
-         b->max_new >= 0 && b->max_new <= b->tokens && (b->max_new > 0 || b->tokens == 0) &&
-         b->max_new <= (1 << 24) && b->max_len >= b->max_new && b->max_len <= (1 << 30) &&
-         (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
-}
-
-// The batch's numbers, for pages of `page` tokens.
+// The batch's numbers without its table.
 bool batch_sizes_ok(const fxpq_kv_batch* b) {
   return b && b->start && b->length && aligned(b->start, 4) && aligned(b->length, 4) && b->seqs >= 1 &&
          b->seqs <= 65535 && b->tokens >= 0 && b->max_new >= 0 && b->max_new <= b->tokens &&
@@ -163,16 +155,17 @@ bool batch_sizes_ok(const fxpq_kv_batch* b) {
          b->max_len <= (1 << 30);
 }
 
+// With the table of a cache of `page` tokens a page.
+bool batch_ok(const fxpq_kv_batch* b, int page) {
+  return batch_sizes_ok(b) && b->table && aligned(b->table, 4) && b->table_ld >= 1 &&
+         (b->max_len + (int64_t)page - 1) / page <= b->table_ld;
+}
+
 bool latent_ok(const fxpq_latent_cache* c) {
   return c && c->codes && c->scale && c->rope_scale && aligned(c->codes, 16) && aligned(c->scale, 16) &&
          aligned(c->rope_scale, 16) && c->pages >= 1 &&
          (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) &&
          (c->latent == 256 || c->latent == 512) && c->rope >= 16 && c->rope <= 64 && c->rope % 16 == 0;
-}
-
-bool latent_batch_ok(const fxpq_kv_batch* b, const fxpq_latent_cache* c) {
-  return batch_sizes_ok(b) && b->table && aligned(b->table, 4) && b->table_ld >= 1 &&
-         (b->max_len + (int64_t)c->page - 1) / c->page <= b->table_ld;
 }
 
 // Rows of `width` at token * ld + head * hd that do not overlap.
@@ -1022,7 +1015,7 @@ fxpq_status fxpq_cache_append(fxpq_handle h, const fxpq_kv_cache* cache,
                               const fxpq_kv_batch* batch, const fxpq_rotary* rot, const void* k,
                               int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq,
                               void* q_out, int64_t ldqo, int32_t q_heads, fxpq_dtype type) {
-  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache->page)) return FXPQ_ERR_INVALID_ARG;
   const int64_t width = (int64_t)cache->heads * cache->dim;
   if (ldk < width || ldv < width) return FXPQ_ERR_INVALID_ARG;
   if (rot && (rot->dims < 0 || rot->dims % 2 != 0 || rot->dims > cache->dim || rot->positions < 0 ||
@@ -1044,7 +1037,7 @@ fxpq_status fxpq_cache_append(fxpq_handle h, const fxpq_kv_cache* cache,
 
 fxpq_status fxpq_cache_read(fxpq_handle h, const fxpq_kv_cache* cache, const fxpq_kv_batch* batch,
                             void* k_out, void* v_out, fxpq_dtype type) {
-  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache->page)) return FXPQ_ERR_INVALID_ARG;
   if (!aligned(k_out, real_bytes(type)) || !aligned(v_out, real_bytes(type))) return FXPQ_ERR_INVALID_ARG;
   if (batch->tokens == 0 || (!k_out && !v_out)) return FXPQ_OK;
   DeviceGuard g(h->device);
@@ -1056,7 +1049,7 @@ fxpq_status fxpq_cache_attention_workspace(fxpq_handle h, const fxpq_kv_cache* c
                                            int64_t* bytes) {
   if (!bytes) return FXPQ_ERR_INVALID_ARG;
   *bytes = 0;
-  if (!h || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache, batch))
+  if (!h || !cache_ok(cache) || !batch_ok(batch, cache->page) || !heads_ok(q_heads, cache, batch))
     return FXPQ_ERR_INVALID_ARG;
   if (batch->tokens > 0) *bytes = cache_attention_workspace(ctx(h), *cache, *batch, q_heads);
   return FXPQ_OK;
@@ -1067,7 +1060,7 @@ fxpq_status fxpq_cache_attention(fxpq_handle h, const fxpq_kv_cache* cache,
                                  int32_t q_heads, float softmax_scale, int32_t causal, void* out,
                                  int64_t ldo, fxpq_dtype type, void* workspace,
                                  int64_t workspace_bytes) {
-  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache) || !heads_ok(q_heads, cache, batch))
+  if (!h || !is_real(type) || !cache_ok(cache) || !batch_ok(batch, cache->page) || !heads_ok(q_heads, cache, batch))
     return FXPQ_ERR_INVALID_ARG;
   const int64_t width = (int64_t)q_heads * cache->dim;
   if (ldq < width || ldo < width || !isfinite(softmax_scale)) return FXPQ_ERR_INVALID_ARG;
@@ -1087,7 +1080,7 @@ fxpq_status fxpq_latent_append(fxpq_handle h, const fxpq_latent_cache* cache,
                                const void* c, int64_t ldc, const void* r, int64_t ldr, const void* q,
                                int64_t ldq, int64_t hdq, void* q_out, int64_t ldqo, int64_t hdqo,
                                int32_t q_heads, fxpq_dtype type) {
-  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (!h || !is_real(type) || !latent_ok(cache) || !batch_ok(batch, cache->page)) return FXPQ_ERR_INVALID_ARG;
   if (rule != FXPQ_SCALE_MAX && rule != FXPQ_SCALE_DFX) return FXPQ_ERR_INVALID_ARG;
   if (ldc < cache->latent || ldr < cache->rope) return FXPQ_ERR_INVALID_ARG;
   if (rot && (rot->dims != cache->rope || rot->positions < 0 || !rot->cos || !rot->sin ||
@@ -1127,7 +1120,7 @@ fxpq_status fxpq_latent_read(fxpq_handle h, const fxpq_latent_cache* cache,
                              const fxpq_kv_batch* batch, const int32_t* kv_start, int32_t kv_tokens,
                              int8_t* codes, int64_t ld_codes, float* scale, void* latent,
                              int64_t ld_latent, void* key, int64_t ld_key, fxpq_dtype type) {
-  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache)) return FXPQ_ERR_INVALID_ARG;
+  if (!h || !is_real(type) || !latent_ok(cache) || !batch_ok(batch, cache->page)) return FXPQ_ERR_INVALID_ARG;
   if (kv_start ? kv_tokens < 0 || !aligned(kv_start, 4) : kv_tokens != batch->tokens) return FXPQ_ERR_INVALID_ARG;
   if ((codes && (!aligned(codes, 16) || ld_codes < cache->latent || ld_codes % 16 != 0)) ||
       (latent && ld_latent < cache->latent) || (key && ld_key < cache->rope))
@@ -1146,7 +1139,7 @@ fxpq_status fxpq_latent_attention_workspace(fxpq_handle h, const fxpq_latent_cac
                                             int64_t* bytes) {
   if (!bytes) return FXPQ_ERR_INVALID_ARG;
   *bytes = 0;
-  if (!h || !latent_ok(cache) || !latent_batch_ok(batch, cache) || !latent_heads_ok(q_heads, batch))
+  if (!h || !latent_ok(cache) || !batch_ok(batch, cache->page) || !latent_heads_ok(q_heads, batch))
     return FXPQ_ERR_INVALID_ARG;
   if (batch->tokens > 0) *bytes = latent_attention_workspace(ctx(h), *cache, *batch, q_heads);
   return FXPQ_OK;
@@ -1158,7 +1151,7 @@ fxpq_status fxpq_latent_attention(fxpq_handle h, const fxpq_latent_cache* cache,
                                   float softmax_scale, int32_t causal, void* out, int64_t ldo,
                                   int64_t hdo, fxpq_dtype type, void* workspace,
                                   int64_t workspace_bytes) {
-  if (!h || !is_real(type) || !latent_ok(cache) || !latent_batch_ok(batch, cache) ||
+  if (!h || !is_real(type) || !latent_ok(cache) || !batch_ok(batch, cache->page) ||
       !latent_heads_ok(q_heads, batch) || !isfinite(softmax_scale))
     return FXPQ_ERR_INVALID_ARG;
   if (ldq < cache->latent || hdq < cache->latent || ldqr < cache->rope || hdqr < cache->rope ||

@@ -164,3 +164,31 @@ def test_latent_attention_of_bounds_past_what_is_counted(fx, h):
     for seqs, most, cut in ((256, 1 << 30, False), (128, 1 << 30, False), (127, 1 << 30, True), (256, 1 << 28, True)):
         batch = fx.kv_batch(some, some, some, seqs, 1 << 23, seqs, 1, most)
         assert (fx.latent_attention_workspace(h, cache, batch, 1) > 0) == cut
+
+
+WHOLE = [  # more than 32 row tiles of a sequence, more than 256 sequences: (latent, rope, page, heads, new, lengths)
+    (512, 64, 64, 64, [20, 3], [300, 70]),
+    (512, 32, 16, 16, [70], [400]),
+    (512, 16, 32, 128, [9], [1000]),
+    (256, 64, 32, 128, [20], [900]),
+    (256, 48, 16, 33, [40, 0, 7], [41, 60, 500]),
+    (512, 64, 16, 16, [1] * 260, [(7 * i) % 90 + 1 for i in range(260)]),
+    (256, 32, 64, 70, [i % 3 for i in range(258)], [(5 * i) % 130 + 2 for i in range(258)]),
+    # four row tiles a block, cut
+    (256, 32, 128, 128, [4], [24600]),
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("case", WHOLE, ids=lambda c: f"{c[0]} {c[3]} heads {len(c[4])} x {max(c[4])} over {max(c[5])}")
+def test_latent_attention_of_many_row_tiles_or_sequences(fx, h, t, case):
+    latent, rope, page, heads, new, lens = case
+    note("many row tiles", t, case)
+    cache = Cache(fx, lens, latent, rope, page, seed=heads)
+    cache.fill(lens, 27)
+    g = torch.Generator().manual_seed(28)
+    q, qr = (torch.randn(sum(new), heads, d, generator=g).to(TYPES[t]) for d in (latent, rope))
+    for layout in ("token", "odd") if sum(lens) < 20000 else ("token",):
+        got = run_latent(fx, h, cache, new, lens, q, qr, 0.07, 1, t, layout)
+        assert fx.sync_status(h) == 0
+        check_latent(got, cache, lens, new, q, qr, 0.07, 1, t)
