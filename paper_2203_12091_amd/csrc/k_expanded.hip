@@ -13,10 +13,13 @@
 // panel's row the 16-byte pieces are swapped by the token's number, by the address that
 // each lane loads from, so that reads of 16 rows cover all banks.
 //
-// f16 and bf16 multiply as they are, P rounded to the same type (bf16: 2^-9 a weight, which
-// leaves the whole result's error at 1.3 times that of its own rounding; f16 with weights
-// lifted by 2^6, so that those down to 2^-20 of the largest keep 11 bits); f32 on the
-// f32 matrix instruction, whose products are exact.
+// f16 and bf16 multiply as they are, P as two terms of the same type (2^-16 of a weight and
+// less; f16 with weights lifted by 2^6, so that those down to 2^-20 of the largest keep 11 bits in
+// the first), which leaves the whole result the error of its own rounding alone: with one term
+// it was 1.4 times that (bf16 0.0023, f16 0.00027), and single tokens, whose weights have 11
+// bits, were more exact than the same tokens in a prompt.  4 x 1024 over up to 4000, bf16, 247 us,
+// with one term 200; 1 x 8192, f16, 449 and 342.  f32 is on the f32 matrix instruction, whose
+// products are exact.
 //
 // Where there are few rows the four waves take the same 16 and share the tokens of a chunk.
 //
@@ -151,6 +154,7 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
   constexpr int kSteps = D / 32, DT = VD / 16;
   constexpr int kRows = SPLIT ? 16 : NC * 64;
   constexpr int kPiece = 16 / S;  // reals of a 16-byte piece
+  constexpr int kTerms = S == 2 ? 2 : 1;  // of a weight
   typedef Panels<T, kTok> Pan;
   constexpr int KP = Pan::of(D), VP = Pan::of(VD), kStage = (KP + VP) * Pan::kBytes;
   extern __shared__ __attribute__((aligned(256))) int8_t lds[];
@@ -364,13 +368,14 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       }
       f = 1.0f;
     }
-    v8 w[NC][N / 8];
+    v8 w[kTerms][NC][N / 8];
     auto weigh = [&](int u, int i) __attribute__((always_inline)) {  // token i of the 8 of operand u
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const float e = __builtin_amdgcn_exp2f(fmaf(x[c][8 * u + i], f, ref[c]));
         l[c] += e;
-        w[c][u][i] = (T)e;
+        w[0][c][u][i] = (T)e;
+        if constexpr (kTerms == 2) w[1][c][u][i] = (T)(e - (float)w[0][c][u][i]);
       }
     };
     const LdsAt vb = stage;
@@ -399,7 +404,9 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       for (int k = 0; k < N / 8 * DT; ++k) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][k % DT] = mfma8(v[k % kAhead], w[c][k / DT], o[c][k % DT]);
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c][k % DT] = mfma8(v[k % kAhead], w[t][c][k / DT], o[c][k % DT]);
         const int ahead = k + kAhead;
         if (ahead < N / 8 * DT) v[k % kAhead] = value_operand<T, kTok>(vb + vat[ahead % kValueBases], ahead / DT, ahead % DT);
         if (N > 8 && k < DT)
@@ -418,7 +425,9 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[k] = finite((float)y[k]) ? y[k] : (T)0.0f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][j] = mfma8(y, u ? w[c][N / 8 - 1] : w[c][0], o[c][j]);
+          for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) o[c][j] = mfma8(y, u ? w[t][c][N / 8 - 1] : w[t][c][0], o[c][j]);
         }
 #pragma unroll 1
       for (int t = wtok; t < wtok + kOwn; ++t) {

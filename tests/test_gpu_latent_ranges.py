@@ -1,5 +1,5 @@
-"""Attention over the latents at the ends of its range: codes that a few channels leave
-small, queries and scales of any size, row tiles that are not cut.
+"""Latent attention at the ends of its range: codes that a few channels leave
+small, queries and scales of any size, row tiles that are not cut, values that cancel.
 
 The tolerance is the one of test_gpu_latent.py, held to what each dimension's own tokens
 weigh: a weight off by a share e moves dimension d by at most e sum_j w_j |v_jd|, not by e
@@ -9,7 +9,7 @@ import math
 import pytest
 
 from gpu_util import DEV, note
-from test_gpu_latent import HALF_ULP, TYPES, Cache, check_latent, fx, h, run_latent  # noqa: F401 (fixtures)
+from test_gpu_latent import HALF_ULP, TYPES, Cache, check_latent, fx, h, heads_of, run_expanded, run_latent  # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -192,3 +192,46 @@ def test_latent_attention_of_many_row_tiles_or_sequences(fx, h, t, case):
         got = run_latent(fx, h, cache, new, lens, q, qr, 0.07, 1, t, layout)
         assert fx.sync_status(h) == 0
         check_latent(got, cache, lens, new, q, qr, 0.07, 1, t)
+
+
+TERMS = [  # (nope, rope, vdim, heads, new, lengths): waves that share tokens, 64 and 128 rows a block
+    (128, 64, 128, 2, [16, 3], [700, 90]),
+    (64, 32, 64, 5, [9], [1500]),
+    (64, 32, 64, 20, [140, 60], [700, 90]),
+    (128, 32, 128, 24, [150], [900]),
+    (128, 64, 128, 70, [150, 129, 140, 1], [600, 129, 150, 300]),
+    (64, 64, 64, 128, [129, 100], [700, 130]),
+]
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("case", TERMS, ids=str)
+def test_expanded_attention_weights_in_more_bits_than_the_result(fx, h, t, case):
+    """Values that cancel to a small part of themselves tell weights of the result's own type
+    from two terms of it (2^-16 of a weight at most).  The error's norm against that of its
+    parts: the result's rounding; the weights' terms and exponentials, each by itself; the
+    logits' sums as above; sums of n products, at random the square root of their number."""
+    nope, rope, vdim, heads, new, lens = case
+    note("expanded terms", t, case)
+    c, scale = (nope, rope, vdim, heads, 1), 0.2 * (nope + rope) ** -0.5
+    q, k, key, v = heads_of(c, new, lens, t, 33)
+    got = run_expanded(fx, h, c, new, lens, q, k, key, v, scale, t)
+    assert fx.sync_status(h) == 0
+    at = first = 0
+    parts = torch.zeros(4, dtype=torch.float64)
+    off = torch.zeros((), dtype=torch.float64)
+    for n, fresh in zip(lens, new):
+        kk = torch.cat([k[first : first + n], key[first : first + n, None].expand(n, heads, rope)], -1).double().permute(1, 2, 0).contiguous()
+        vv = v[first : first + n].double().transpose(0, 1).contiguous()
+        qq = q[at : at + fresh].double().transpose(0, 1).contiguous()
+        seen = torch.arange(n) <= (n - fresh + torch.arange(fresh))[:, None]
+        w = torch.softmax((qq @ kk * scale).masked_fill(~seen, -math.inf), -1)
+        mag = ((qq.abs() @ kk.abs()) * scale * seen).amax(-1, keepdim=True)
+        want, size = w @ vv, w @ vv.abs()
+        off += (got[at : at + fresh].double().transpose(0, 1) - want).square().sum()
+        for i, x in enumerate((want.to(TYPES[t]).double() - want, (2.0 ** -16 + 2.0 ** -22) * ((w * w) @ (vv * vv)).sqrt(),
+                               2 * 9 * 2.0 ** -24 * mag * size, 2 * (n + 64) ** 0.5 * 2.0 ** -24 * size)):
+            parts[i] += x.square().sum()
+        at += fresh
+        first += n
+    assert off.sqrt() <= parts.sqrt().sum(), (float(off.sqrt()), parts.sqrt().tolist())
