@@ -24,11 +24,13 @@
 // Where there are few rows the four waves take the same 16 and share the tokens of a chunk.
 //
 // Bound by the products: 4 x 1024 over up to 4000, 32 heads of 128 + 64 and 128, bf16: 175
-// GFLOP in 198 us, 0.88 PFLOP/s, where one large product reaches 1.37; 1 x 8192, f16: 333 us,
-// 1.03 PFLOP/s.  Matrix instructions take 46% of the cycles, vector instructions (weights,
-// maxima, rounding) 42%; two blocks a CU overlap the two.  Of 245 us at first the loop of
-// its own for chunks that all rows see took 13, the priority and order of the instructions
-// 35.  64 rows a wave (one wave a SIMD) spill: 850 us.
+// GFLOP (with the weights' second terms 245) in 247 to 252 us, 0.70 PFLOP/s, where one large
+// product reaches 1.37; 1 x 8192, f16: 449 us, 0.77 PFLOP/s.  Matrix instructions take 51% of
+// the cycles, vector instructions (weights, maxima, rounding) 50%; two blocks a CU overlap the
+// two.  With 128 rows and values of 128 up to 62 registers spill, all in the loop of the chunks
+// that some rows see in part.  (Measured with one term: of 245 us at first the loop of its own
+// for chunks that all rows see took 13, the priority and order of the instructions 35; 64 rows
+// a wave, one wave a SIMD, spill: 850 us.)
 #include <type_traits>
 
 #include "kv.hpp"
@@ -528,13 +530,13 @@ hipError_t run_rows(const Ctx& c, const ExpandedRun& p) {
   if constexpr (sizeof(T) == 2) {
     // 128 rows of a block read half as much, 64 make twice as many blocks.  Two blocks run on
     // a CU; in us with 64 and 128 rows: 4 x 1024 over 4000, 16 heads (2 blocks of 128 rows a
-    // CU) 189 and 162, 1 x 1024 over 2048, 128 heads (4) 187 and 151, 1 x 4096, 16 heads (2)
-    // 114 and 119, 2 x 1024 over 2048 (1) 57.5 and 58.2, 4 x 128 over 2048 (1/4) 43 and 57
+    // CU) 222 and 211, 1 x 1024 over 2048, 128 heads (4) 215 and 186, 1 x 4096, 16 heads (2)
+    // 138 and 145, 2 x 1024 over 2048 (1) 65 and 70, 4 x 128 over 2048 (1/4) 48 and 68
     const int64_t blocks = ((int64_t)p.a.b.max_new + 127) / 128 * p.a.b.seqs * p.a.kv.heads;
     if (blocks >= 2 * (int64_t)c.cus) return run<T, D, VD, 2>(c, p);
     // where tiles of 16 rows do not fill the chip, the waves share the tokens: 1 x 64 over 8192,
-    // 16 heads, 75 us, 64 rows a block 141; 4 x 64 over 2048 29 and 43, 2 x 77 over 127 11.0 and
-    // 13.6, but 16 x 16 over 300 17.6 and 15.1.  (A token of f32 takes twice the LDS.)
+    // 16 heads, 80 us, 64 rows a block 160; 4 x 64 over 2048 32 and 48, 2 x 77 over 127 11.4 and
+    // 14.2, but 16 x 16 over 300 18.5 and 15.8.  (A token of f32 takes twice the LDS.)
     const int64_t tiles = ((int64_t)p.a.b.max_new + 15) / 16 * p.a.b.seqs * p.a.kv.heads;
     if (tiles <= c.cus) return run<T, D, VD, 1, true>(c, p);
   }

@@ -9,12 +9,17 @@
 // f16 (exact) and multiplies them with q in registers.  (Products with 1152 + code, whose
 // sums start from what that adds, would spare an operation for every two codes, 32 x 1 over
 // 4096, 128 heads in 69 us in place of 76; but where a few channels take the scale and leave
-// the other codes at some steps, such sums leave logits off by 0.05.)  q is f16 too: scaled by a power of
-// two of its row, so that a bf16 or f16 value is exact down to 2^-27 of the row's largest,
-// and f32 is two f16 terms.  P goes to LDS as f16 and after a barrier every wave multiplies
-// all 64 tokens with its own part of the latent's dimensions: O^T = C^T P^T.  The
-// conversion there is the transposition: a lane reads the same 2 to 8 dimensions of 8
-// tokens and pairs bytes of neighbouring tokens.
+// the other codes at some steps, such sums leave logits off by 0.05.)  q is f16 too: scaled
+// by a power of two of its row, so that a bf16 or f16 value is exact down to 2^-27 of the
+// row's largest, and f32 is two f16 terms.  P goes to LDS as f16 (f32: two terms) and after a
+// barrier every wave multiplies all 64 tokens with its own part of the latent's dimensions:
+// O^T = C^T P^T.  The conversion there is the transposition: a lane reads the same 2 to 8
+// dimensions of 8 tokens and pairs bytes of neighbouring tokens.
+//
+// One f16 term of P rounds a weight by 2^-11 at most, a quarter of bf16's own rounding.  An f16
+// result's rounding is as large: where many weights are alike the error is up to 1.4 times that
+// alone.  A second term would need the LDS of the second block of a CU: 64 x 1 over 8192, 16
+// heads, 91 us in place of 76, 32 x 1 over 4096, 128 heads, 115 in place of 100.
 //
 // A token's scale s_t belongs to both products.  With x_t the logit (base 2), m the
 // row's reference and R a power of two above every scale seen, P_t = 2^(x_t - m) s_t / R
@@ -22,13 +27,14 @@
 // when a row passes it by more than kSlack, so P_t is below 2^(kSlack + kLift) and most
 // chunks need neither a maximum across the waves nor further barriers.
 //
-// What it costs (16 heads, latents of 512 + 64, bf16): a block's start about 8 us (its
-// part, pages, q to f16), a chunk 1.8 us with four waves and one row tile, two blocks a CU,
-// 2.3 us with eight waves and two tiles.  The bytes are not the limit but the conversions:
-// 128 heads, 32 sequences up to 4096: vector instructions 53% of the cycles, matrix
-// instructions 16%, the rest waits at the chunk's two barriers, which one block a CU does
-// not fill.  64 x 1 over up to 8192, 16 heads: 158 MB in 38.6 us, 4.1 TB/s; 32 x 1 over
-// up to 4096, 128 heads: 66 us, 0.28 PFLOP/s; the join 6 us more in both.
+// What it costs (latents of 512 + 64, bf16): a block's start about 8 us (its part, pages, q to
+// f16); a chunk 1.8 us with four waves and one row tile, two blocks a CU (64 x 1 over 4096 and
+// 8192, 16 heads, 46 and 75 us), 2.1 us with eight waves and two tiles (32 x 1 over 2048 and 4096,
+// 128 heads, 65 and 99).  The bytes are not the limit but the conversions: 128 heads, 32
+// sequences up to 4096: vector instructions 56% of the cycles, matrix instructions 15%, the
+// rest waits at the chunk's two barriers, which one block a CU does not fill.  64 x 1 over up
+// to 8192, 16 heads: 158 MB in 41.5 us, 3.8 TB/s; 32 x 1 over up to 4096, 128 heads: 74 us,
+// 0.25 PFLOP/s; the join 6 us more in both.
 #include "kv.hpp"
 #include "ring.hpp"
 #include "values.hpp"
@@ -67,8 +73,8 @@ __device__ inline int part_chunks(int chunks, int share) {
   const int parts = (chunks + share - 1) / share;
   return parts == 0 ? 1 : (chunks + parts - 1) / parts;
 }
-// Sequences of a call that is shared, four a lane.  (With 512 every call's start takes 0.3 us
-// more; 400 x 1, 16 heads, over 1 to 4096 143 us in place of 173, 32 heads over 1024 149 of 94.)
+// Sequences of a call that is shared, four a lane.  (With 512 every call's start takes up to 1 us
+// more; 400 x 1, 16 heads, over 1 to 4096 144 us in place of 166, 32 heads over 1024 159 of 105.)
 constexpr int kMostSeqs = 256;
 
 constexpr float kNoMax = -3.40282347e38f;  // reference before any token
@@ -150,7 +156,7 @@ struct LatentLds {
   static constexpr int kLoads = kPieces * 16 / 64;  // 1 KB loads of a group
   static constexpr int kGroup = 16 * kRow, kSlot = 4 * kGroup;
   // one tile of a wide latent: two slots, so that two blocks fit a CU (64 x 1 over 8192, 16
-  // heads: 71 us; three slots and one block 75; 1 x 1 over 131072: 32.7 and 30.7)
+  // heads: 75 us; three slots and one block 85; 1 x 1 over 131072: 33.6 and 33.1)
   static constexpr int kSlots = LB == 8 && RT * QT == 1 ? 2 : 3;
   static constexpr int kScales = kSlots * kSlot;              // [slots][4 groups][64] floats
   static constexpr int kPRow = 144;                           // bytes of a row of P: 64 halves and a pad
@@ -845,14 +851,14 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
     return p;
   }
   // Parts whose blocks fit the chip at a time; two for each sequence, so that few long ones
-  // among many can be cut: 128 x 1, 128 heads, over 512 and one over 16384 104 us, whole
-  // 559; where all have 1024 the two ways take 111 and 94 us, which is why sequences are
-  // left whole from four blocks a CU on (200 x 1, 128 heads, over 1024: 243 and 184).
+  // among many can be cut: 128 x 1, 128 heads, over 512 and one over 16384 118 us, whole
+  // 645; where all have 1024 the two ways take 121 and 108 us, 200 of them 258 and 204, which
+  // is why sequences are left whole from four blocks a CU on.
   const int slots = rt == 1 && type != FXPQ_F32 ? 2 * c.cus : c.cus;
   p.groups = slots / 8 / p.row_tiles * 8;
   p.rounds = (2 * b.seqs + p.groups - 1) / p.groups;
-  // one chunk a part for few tiles: 1 x 1 over 300 13.3 us, two chunks 15.1; but 8 x 1 over
-  // 2048 19.6 and 18.5, 64 x 1 over 300 22.6 and 18.7
+  // one chunk a part for few tiles: 1 x 1 over 300 13.6 us, two chunks 15.4; but 8 x 1 over
+  // 2048 19.9 and 18.9, 64 x 1 over 300 23.4 and 19.1
   p.least = b.seqs * p.row_tiles <= 4 ? 1 : 2;
   p.each = chunks * b.seqs / p.groups;
   p.part = (int64_t)p.groups * p.rounds * p.row_tiles * rt * 16;
@@ -862,11 +868,12 @@ LatentPlan plan_with(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_bat
 
 // Row tiles of a block: more of them spare conversions of the codes, fewer make more parts
 // and shorter ones.  In us with 1, 2 and 4 tiles, 128 heads, bf16, latents of 256: 32 x 1
-// over 4096 (32 chunks a block with two tiles) 66, 61, 50; 8 x 1 over 4096 (8 chunks) 28.9,
-// 27.2, 30.5; 16 x 1 over 1024 (4) 22.4, 22.0, 26.2.  Latents of 512: 32 x 1 over 4096 98 and
-// 89, 2 x 1 rows of 16 heads over 8192 (0.5) 18 and 22; four tiles do not fit the registers
+// over 4096 (32 chunks a block with two tiles) 75, 70, 56; 8 x 1 over 4096 (8 chunks) 30.3,
+// 29.3, 33.2; 16 x 1 over 1024 (4) 23.4, 23.1, 27.7.  Latents of 512: 32 x 1 over 4096 115 and
+// 100, 2 x 1 rows of 16 heads over 8192 (0.5) 19 and 22; four tiles do not fit the registers
 // (174 us).  f32, whose q and P are twice as large, in one and two tiles: latents of 256,
-// 32 x 1 over 4096 110 and 80, 2 x 1 over 512 15 and 18; of 512 one only (163 and 196).
+// 32 x 1 over 4096 110 and 80, 2 x 1 of 32 heads over 512 12.8 and 15.2; of 512 one only (163
+// and 196).
 LatentPlan plan_latent(const Ctx& c, const fxpq_latent_cache& k, const fxpq_kv_batch& b, int heads, int type) {
   const int64_t rows = (int64_t)b.max_new * heads;
   for (int rt = type == FXPQ_F32 ? k.latent == 512 ? 1 : 2 : k.latent == 512 ? 2 : 4; rt > 1; rt /= 2) {

@@ -278,8 +278,9 @@ class LatentLayer(Layer):
 
     # New tokens of a sequence up to which its queries go to the latents rather than latents to
     # keys and values.  Eight sequences, 16 heads of 128 + 64 and 128, latents of 512, both ways
-    # in us: 32 new tokens over 2048 107 and 125, 48 142 and 127; 32 over 8192 203 and 373, 64
-    # 348 and 408, 96 619 and 393; 1 over 256 50 and 44.
+    # in us: 32 new tokens over 2048 112 and 125, 48 152 and 129; 32 over 8192 224 and 380, 64
+    # 392 and 413, 96 703 and 400; 1 over 256 50 and 44.  (Past 32 row tiles of a sequence, which
+    # 96 tokens are here and 9 of 128 heads, attention over the latents does not cut its cache.)
     FEW = 32
 
     def __init__(self, hidden, heads, nope, rope, vdim, latent, experts, top, inner, positions=4096, seed=0,
