@@ -141,17 +141,20 @@ class LatentCache(Pages):
         (batch, the rows of its tokens in the whole one's) for each, None where there are no
         such tokens, the whole one and None where there are no others.  Kept with the batch,
         which several layers use."""
+        new, length, table = batch.host
+        halves = [[i for i, n in enumerate(new) if 0 < n <= few], [i for i, n in enumerate(new) if n > few]]
+        if [] in halves and len(halves[0] + halves[1]) == len(new):
+            return tuple((batch, None) if half else None for half in halves)
         kept = batch.__dict__.setdefault("halves", {})
         if few not in kept:
-            new, length, table = batch.host
             first = [sum(new[:i]) for i in range(len(new))]
 
-            def half(which):
-                if not which or len(which) == len(new):
-                    return (batch, None) if which else None
+            def part(which):
+                if not which:
+                    return None
                 rows = torch.cat([torch.arange(first[i], first[i] + new[i]) for i in which])
                 return self._batch([new[i] for i in which], [length[i] for i in which], table[which]), rows.to(self.device)
-            kept[few] = (half([i for i, n in enumerate(new) if 0 < n <= few]), half([i for i, n in enumerate(new) if n > few]))
+            kept[few] = tuple(part(half) for half in halves)
         return kept[few]
 
 

@@ -273,3 +273,22 @@ def test_batch_made_by_hand_that_says_what_it_holds(latent):
     latent.fx.calls.clear()
     layer.attend(torch.zeros(hand.tokens, 64), cache, hand)
     assert "expanded_attention" in latent.fx.names()
+
+
+def test_batches_go_with_their_last_use(latent):
+    """A batch's halves do not keep it: its memory is free without a collection."""
+    import gc
+    import weakref
+    layer, cache = make_latent(latent)
+    gc.disable()
+    try:
+        for new in ([40], [40, 1], [1, 0]):
+            batch = cache.extend(list(range(len(new))), new)
+            layer.attend(torch.zeros(sum(new), 64), cache, batch)
+            latent.fx.calls.clear()
+            cache.retract(batch)
+            gone = weakref.ref(batch.rows)
+            del batch
+            assert gone() is None, new
+    finally:
+        gc.enable()
