@@ -491,6 +491,43 @@ __global__ __launch_bounds__(256, 2) void k_expanded_attention(const ExpandedRun
       for (int j = 0; j < kTiles; ++j) o[0][j] += f * parts[(w * DT + j0 + j) * 64 + lane];
     }
   }
+  if constexpr (kTerms == 2) {
+    // An infinite value times a weight's second term, which may be 0 or below it, is NaN.  Where a
+    // result is NaN and its weights are not, the values that are not finite are what it is made of.
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bad |= o[c][j][i] != o[c][j][i] && l[c] == l[c];
+    if (__any(bad)) {
+      v4f sum[NC][kTiles];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) sum[c][j] = v4f{0, 0, 0, 0};
+#pragma unroll 1
+      for (int t = 0; t < s.len; ++t) {
+        const T* at = reinterpret_cast<const T*>(values) + t * ldv + 16 * j0 + 4 * g;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = (float)at[16 * j + i];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+              if (t <= limit[c] && !finite(v)) sum[c][j][i] += v;
+          }
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[c][j][i] = sum[c][j][i] == 0.0f ? o[c][j][i] : sum[c][j][i];
+    }
+  }
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int row = wrow + c * 16 + n;

@@ -235,3 +235,29 @@ def test_expanded_attention_weights_in_more_bits_than_the_result(fx, h, t, case)
         at += fresh
         first += n
     assert off.sqrt() <= parts.sqrt().sum(), (float(off.sqrt()), parts.sqrt().tolist())
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("nope,rope,vdim,heads,new,lens", [(128, 64, 128, 2, [16], [700]), (64, 32, 64, 5, [70], [400]), (64, 32, 128, 40, [90], [300]),
+                                                           (128, 64, 128, 70, [150, 129, 140, 1], [600, 129, 150, 300])])
+def test_expanded_attention_of_infinite_values(fx, h, t, nope, rope, vdim, heads, new, lens):
+    """A query that sees an infinite value, in whatever chunk, has it in that dimension, NaN
+    where it sees both infinities or a NaN; its other dimensions and what does not see them
+    stay as they are."""
+    note("infinite values", t, nope, rope, vdim, heads, new, lens)
+    c, scale = (nope, rope, vdim, heads, 1), 0.05
+    q, k, key, v = heads_of(c, new, lens, t, 35)
+    want = run_expanded(fx, h, c, new, lens, q, k, key, v, scale, t)
+    put = [(3, 7, math.inf), (130, 9, -math.inf), (lens[0] - 5, 7, math.inf), (40, 11, math.inf), (60, 11, -math.inf), (80, 13, math.nan)]
+    seen = lens[0] - new[0] + torch.arange(new[0])  # the first sequence's queries
+    for at, d, x in put:
+        v[at, :, d] = x
+    for d in {d for _, d, _ in put}:
+        total = torch.zeros(new[0])
+        for at, e, x in put:
+            if e == d:
+                total = torch.where(seen >= at, total + x, total)
+        want[: new[0], :, d] = torch.where((total == 0)[:, None], want[: new[0], :, d].float(), total[:, None]).to(want.dtype)
+    got = run_expanded(fx, h, c, new, lens, q, k, key, v, scale, t)
+    assert fx.sync_status(h) == 0
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(0.0, math.inf, -math.inf), want.nan_to_num(0.0, math.inf, -math.inf))
